@@ -18,6 +18,8 @@
  *                    policies the paper compares (Algorithm 1, Algorithm 6, Section 3)
  *   svip_pair_stats  acceptance diagnostics per drafted position (Section 2.2, Appendix B)
  *   svip_warp_logits top-k / top-p filtering of logits rows ahead of those calls (not in the paper)
+ *   svip_quantize_blocks, svip_head_logits, svip_head_loss, svip_head_loss_grad   the layer that makes the logits: its product
+ *                    in 8 bits, and the cross entropy over its logits with the gradient (not in the paper)
  *   svip_draft_step_greedy, svip_verify_greedy    the same two steps under greedy decoding
  *                                                       (Algorithm 3 Verify, Algorithm 5 Correct)
  *
@@ -385,6 +387,95 @@ svip_status svip_loop_run(const svip_loop_config *config /* host */, int first_r
 svip_status svip_warp_logits(const void *logits_in, void *logits_out, int dtype, int B, int n_rows,
                              int V, long long seq_stride, long long row_stride, float temperature,
                              int top_k, double top_p, int *kept_out, void *hip_stream);
+
+/*
+ * The head: the matrix [V, D] that turns a model's hidden states into the logits all the calls above read.  The paper's models are
+ * out of this library's scope, but not this layer, which for a small drafter is most of the bytes of a step; here it is served
+ * in 8 bits and trained in the storage types of the logits.
+ *
+ * Their workspace: svip_head_workspace_bytes of the call's sizes or more, 256-byte aligned, that svip_workspace_reset has cleared
+ * once (for its flag word).  It is not the one of the calls above, it holds nothing between calls, and calls that run concurrently
+ * must use different ones.  Sizes: 1 <= N <= 2^20 rows of hidden states, 1 <= V <= 2^22, 1 <= D, K <= 2^17; row strides are at most
+ * 2^23 elements (8-bit matrices: 2^24).  Same inputs give bit-identical outputs.
+ */
+typedef enum {
+    SVIP_HEAD_LOGITS = 0,            /* svip_head_logits; dtype: of logits_out, D: K */
+    SVIP_HEAD_LOSS = 1,              /* svip_head_loss */
+    SVIP_HEAD_LOSS_GRAD = 2          /* svip_head_loss_grad; enough for svip_head_loss of the same sizes too */
+} svip_head_call;
+/* Pure host function; 0 on bad arguments. */
+size_t svip_head_workspace_bytes(int call, int dtype, int N, int V, int D);
+
+/*
+ * A matrix [rows, cols] in 8 bits with a scale for each block of block_rows x 128 values (block_rows 1: hidden states, 128: weights).
+ * K = cols filled up to a multiple of 128 with zeros.  For each block, over its finite values,
+ *   e = the least integer >= -127 with max |x| <= 448 * 2^e   (0 for a block of zeros)
+ *   q_out[r, c] = x[r, c] / 2^e rounded to e4m3 (OCP: 4 exponent bits, 3 mantissa bits, no infinity), ties to even
+ *   scale_out[r / block_rows, c / 128] = e + 127              (e8m0: a power of two)
+ * so that the value kept is q * 2^e.  A value that is not finite becomes the code 0x7f (NaN).  Bytes of q_out past column K and of
+ * scale_out past column K / 128 are not written.  No workspace.
+ */
+svip_status svip_quantize_blocks(
+    const void *x, int dtype,        /* device, row r at element offset r * row_stride; 16-byte aligned rows */
+    int rows, int cols, long long row_stride,
+    int block_rows,                  /* 1 or 128, else SVIP_ERR_PARAM */
+    void *q_out, long long q_stride, /* device [rows, K], bytes; 16-byte aligned rows */
+    void *scale_out, long long scale_stride,   /* device [ceil(rows / block_rows), K / 128], bytes */
+    void *hip_stream);
+
+/*
+ * Logits of hidden states and weight in 8 bits:
+ *   logits_out[n, v] = sum over blocks b of 2^(s_n,b + s_v,b) * sum over k in block b of hidden_q[n, k] * weight_q[v, k]
+ * with the scales of hidden_scale[n, b] (blocks of 1 x 128) and weight_scale[v / 128, b] (blocks of 128 x 128), as
+ * svip_quantize_blocks writes them.  K is a multiple of 128.  Sums in fp32, rounded once to dtype.  logits_out has the layout
+ * that the calls above take: rows of V values, 16-byte aligned, row n at element offset n * row_stride.
+ */
+svip_status svip_head_logits(
+    const void *hidden_q, const void *hidden_scale,    /* device [N, K] e4m3, [N, K / 128] e8m0 */
+    const void *weight_q, const void *weight_scale,    /* device [V, K] e4m3, [ceil(V / 128), K / 128] e8m0 */
+    int N, int V, int K,
+    long long hidden_stride, long long hidden_scale_stride,    /* bytes */
+    long long weight_stride, long long weight_scale_stride,
+    void *logits_out, int dtype, long long row_stride,
+    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Cross entropy of hidden states against target tokens, over the logits z[n, v] = (hidden[n] . weight[v]) / temperature, which are
+ * never stored:
+ *   lse_out[n]  = logsumexp over v of z[n, v]
+ *   loss_out[n] = lse_out[n] - z[n, targets[n]],  0 where targets[n] is negative (a row without a target)
+ * A target >= V counts as no target and sets SVIP_FLAG_BAD_TOKEN in the workspace.  Products and sums in fp32 (fp32 inputs: as two
+ * 11-bit parts each, of a product all but low x low), joined in fp64.  D is a multiple of 16 bytes' worth of elements.
+ * hidden and weight are finite numbers; rows without a target may hold anything, and only their own lse_out depends on it.
+ */
+svip_status svip_head_loss(
+    const void *hidden,              /* device [N, D], row n at element offset n * hidden_stride */
+    const void *weight,              /* device [V, D], row v at element offset v * weight_stride */
+    int dtype, int N, int V, int D, long long hidden_stride, long long weight_stride,
+    float temperature,
+    const int *targets,              /* device [N] */
+    float *loss_out, float *lse_out, /* device [N] */
+    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Its gradient, for a loss of sum over n of grad_loss[n] * loss_out[n] (a mean over the rows with a target: 1 / their number):
+ *   G[n, v] = (exp(z[n, v] - lse[n]) - [v = targets[n]]) * grad_loss[n] / temperature,  0 in rows without a target
+ *   grad_hidden_out = G weight        grad_weight_out = G^T hidden
+ * Either output may be NULL and is then not computed (a frozen head).  lse is svip_head_loss's; the logits are computed again, in pieces of the vocabulary, and the
+ * difference of softmax and one-hot is held for one piece, in bf16 (bf16 inputs), in fp16 times 2^15 (fp16) or in two such
+ * parts (fp32).  Rows without a target get gradients of zero and add none, whatever they and their grad_loss hold.
+ * The outputs must not overlap the inputs.
+ */
+svip_status svip_head_loss_grad(
+    const void *hidden, const void *weight,
+    int dtype, int N, int V, int D, long long hidden_stride, long long weight_stride,
+    float temperature,
+    const int *targets,
+    const float *lse,                /* device [N] */
+    const float *grad_loss,          /* device [N] */
+    void *grad_hidden_out, long long grad_hidden_stride,   /* device [N, D] of dtype, or NULL */
+    void *grad_weight_out, long long grad_weight_stride,   /* device [V, D] of dtype, or NULL */
+    void *workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -21,7 +21,8 @@ _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 # every symbol include/svip.h declares
 EXPORTS = ("svip_status_string", "svip_workspace_bytes", "svip_workspace_needed", "svip_workspace_reset",
            "svip_workspace_flags", "svip_draft_step", "svip_draft_step_static", "svip_verify", "svip_draft_step_greedy",
-           "svip_verify_greedy", "svip_pair_stats", "svip_warp_logits", "svip_loop_workspace_bytes", "svip_loop_init", "svip_loop_run")
+           "svip_verify_greedy", "svip_pair_stats", "svip_warp_logits", "svip_loop_workspace_bytes", "svip_loop_init", "svip_loop_run",
+           "svip_head_workspace_bytes", "svip_quantize_blocks", "svip_head_logits", "svip_head_loss", "svip_head_loss_grad")
 # every symbol include/svip_bench.h declares (benchmark and experiment hooks, not the product ABI)
 BENCH_EXPORTS = ("svip_bench_time_kernels", "svip_bench_events_used", "svip_bench_set_tuning",
                  "svip_bench_warp_routes", "svip_bench_empty_kernel", "svip_bench_stream_sink_words", "svip_bench_stream_read")
@@ -98,6 +99,16 @@ def load():
     lib.svip_loop_init.argtypes = [ctypes.POINTER(LoopConfig)]
     lib.svip_loop_run.restype = i
     lib.svip_loop_run.argtypes = [ctypes.POINTER(LoopConfig), i, i, ctypes.POINTER(i), ctypes.POINTER(i)]
+    lib.svip_head_workspace_bytes.restype = sz
+    lib.svip_head_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.svip_quantize_blocks.restype = i
+    lib.svip_quantize_blocks.argtypes = [vp, i, i, i, ll, i, vp, ll, vp, ll, vp]
+    lib.svip_head_logits.restype = i
+    lib.svip_head_logits.argtypes = [vp, vp, vp, vp, i, i, i, ll, ll, ll, ll, vp, i, ll, vp, sz, vp]
+    lib.svip_head_loss.restype = i
+    lib.svip_head_loss.argtypes = [vp, vp, i, i, i, i, ll, ll, f, vp, vp, vp, vp, sz, vp]
+    lib.svip_head_loss_grad.restype = i
+    lib.svip_head_loss_grad.argtypes = [vp, vp, i, i, i, i, ll, ll, f, vp, vp, vp, vp, ll, vp, ll, vp, sz, vp]
     lib.svip_bench_time_kernels.restype = i
     lib.svip_bench_time_kernels.argtypes = [i, ctypes.POINTER(vp), ctypes.POINTER(vp), i]
     lib.svip_bench_events_used.restype = i
@@ -427,6 +438,121 @@ class Loop:
 
     def flags(self) -> int:
         return workspace_flags(self.workspace)
+
+
+HEAD_LOGITS, HEAD_LOSS, HEAD_LOSS_GRAD = 0, 1, 2
+HEAD_BLOCK = 128
+
+
+def head_workspace_bytes(call: int, dtype, N: int, V: int, D: int) -> int:
+    """svip_head_workspace_bytes; dtype a torch dtype, call HEAD_LOGITS, HEAD_LOSS or HEAD_LOSS_GRAD."""
+    return int(load().svip_head_workspace_bytes(int(call), _DTYPES.get(dtype, -1), int(N), int(V), int(D)))
+
+
+def new_head_workspace(call: int, dtype, N: int, V: int, D: int, device="cuda", stream=None) -> torch.Tensor:
+    """Allocate a workspace for a call of the head (HEAD_LOSS_GRAD: for the loss of the same sizes too) and zero its flag word."""
+    n = head_workspace_bytes(call, dtype, N, V, D)
+    if n == 0:
+        raise SvipError(2, "svip_head_workspace_bytes: bad call, dtype, N, V or D")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    with torch.cuda.device(ws.device):
+        _check(load().svip_workspace_reset(ws.data_ptr(), n, _stream(stream)))
+    return ws
+
+
+def _rows(t, shape, dtype, name):
+    """Pointer and row stride of a matrix with unit stride along its rows."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be a matrix" + (f" {list(shape)}" if shape is not None else ""))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} needs unit stride along its rows")
+    return _ptr(t, dtype, name), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _vector(t, n, dtype, name):
+    if tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous [{n}]")
+    return _ptr(t, dtype, name)
+
+
+def _on_one_device(**tensors):
+    """The device of all of them, to be made current for the call."""
+    devices = {name: t.device for name, t in tensors.items() if t is not None}
+    if len(set(devices.values())) > 1:
+        raise ValueError("tensors on several devices: " + ", ".join(f"{n} on {d}" for n, d in devices.items()))
+    device = next(iter(devices.values()))
+    if device.type != "cuda":
+        raise ValueError(f"{next(iter(devices))} must be a device tensor")
+    return torch.cuda.device(device)
+
+
+def quantize_blocks(x, *, block_rows=1, q_out, scale_out, stream=None):
+    """svip_quantize_blocks.  x [rows, cols] float32, bfloat16 or float16; q_out [rows, K] float8_e4m3fn, K = cols filled up to a
+    multiple of 128; scale_out [ceil(rows / block_rows), K / 128] float8_e8m0fnu."""
+    if x.dtype not in _DTYPES:
+        raise SvipError(3, "x must be float32, bfloat16 or float16")
+    if block_rows not in (1, HEAD_BLOCK):
+        raise SvipError(6, "block_rows must be 1 or 128")
+    px, sx = _rows(x, None, None, "x") if x.is_cuda else (None, 0)
+    with _on_one_device(x=x, q_out=q_out, scale_out=scale_out):
+        rows, cols = x.shape
+        kb = -(-cols // HEAD_BLOCK)
+        pq, sq = _rows(q_out, (rows, kb * HEAD_BLOCK), torch.float8_e4m3fn, "q_out")
+        ps, ss = _rows(scale_out, (-(-rows // block_rows), kb), torch.float8_e8m0fnu, "scale_out")
+        _check(load().svip_quantize_blocks(px, _DTYPES[x.dtype], rows, cols, sx, int(block_rows), pq, sq, ps, ss, _stream(stream)))
+
+
+def head_logits(hidden_q, hidden_scale, weight_q, weight_scale, *, logits_out, workspace, stream=None):
+    """svip_head_logits.  hidden_q [N, K], weight_q [V, K] float8_e4m3fn; hidden_scale [N, K / 128], weight_scale [ceil(V / 128), K / 128]
+    float8_e8m0fnu; logits_out [N, V] float32, bfloat16 or float16."""
+    if logits_out.dtype not in _DTYPES:
+        raise SvipError(3, "logits_out must be float32, bfloat16 or float16")
+    with _on_one_device(hidden_q=hidden_q, hidden_scale=hidden_scale, weight_q=weight_q, weight_scale=weight_scale, logits_out=logits_out,
+                        workspace=workspace):
+        ph, sh = _rows(hidden_q, None, torch.float8_e4m3fn, "hidden_q")
+        N, K = hidden_q.shape
+        pw, sw = _rows(weight_q, (weight_q.shape[0], K), torch.float8_e4m3fn, "weight_q")
+        V, kb = weight_q.shape[0], K // HEAD_BLOCK
+        phs, shs = _rows(hidden_scale, (N, kb), torch.float8_e8m0fnu, "hidden_scale")
+        pws, sws = _rows(weight_scale, (-(-V // HEAD_BLOCK), kb), torch.float8_e8m0fnu, "weight_scale")
+        po, so = _rows(logits_out, (N, V), None, "logits_out")
+        _check(load().svip_head_logits(ph, phs, pw, pws, N, V, K, sh, shs, sw, sws, po, _DTYPES[logits_out.dtype], so,
+                                       _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+
+
+def _head_args(hidden, weight, targets, temperature):
+    if hidden.dtype not in _DTYPES or weight.dtype != hidden.dtype:
+        raise SvipError(3, "hidden and weight must both be float32, bfloat16 or float16")
+    ph, sh = _rows(hidden, None, None, "hidden")
+    N, D = hidden.shape
+    pw, sw = _rows(weight, (weight.shape[0], D), None, "weight")
+    V = weight.shape[0]
+    return (ph, pw, _DTYPES[hidden.dtype], N, V, D, sh, sw, float(temperature), _vector(targets, N, torch.int32, "targets"))
+
+
+def head_loss(hidden, weight, targets, *, temperature=1.0, loss_out, lse_out, workspace, stream=None):
+    """svip_head_loss.  hidden [N, D], weight [V, D] of one type (float32, bfloat16 or float16); targets int32 [N], negative for rows without a
+    target; loss_out, lse_out float32 [N]."""
+    with _on_one_device(hidden=hidden, weight=weight, targets=targets, loss_out=loss_out, lse_out=lse_out, workspace=workspace):
+        head = _head_args(hidden, weight, targets, temperature)
+        N = hidden.shape[0]
+        _check(load().svip_head_loss(*head, _vector(loss_out, N, torch.float32, "loss_out"), _vector(lse_out, N, torch.float32, "lse_out"),
+                                     _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+
+
+def head_loss_grad(hidden, weight, targets, *, temperature=1.0, lse, grad_loss, grad_hidden_out=None, grad_weight_out=None, workspace,
+                   stream=None):
+    """svip_head_loss_grad.  lse float32 [N] as head_loss wrote it, grad_loss float32 [N]; grad_hidden_out [N, D] and grad_weight_out [V, D]
+    of hidden's type, or None."""
+    with _on_one_device(hidden=hidden, weight=weight, targets=targets, lse=lse, grad_loss=grad_loss, grad_hidden_out=grad_hidden_out,
+                        grad_weight_out=grad_weight_out, workspace=workspace):
+        head = _head_args(hidden, weight, targets, temperature)
+        N = hidden.shape[0]
+        outs = []
+        for t, like, name in ((grad_hidden_out, hidden, "grad_hidden_out"), (grad_weight_out, weight, "grad_weight_out")):
+            outs += _rows(t, tuple(like.shape), hidden.dtype, name) if t is not None else (None, 0)
+        _check(load().svip_head_loss_grad(*head, _vector(lse, N, torch.float32, "lse"), _vector(grad_loss, N, torch.float32, "grad_loss"), *outs,
+                                          _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
 
 
 def bench_time_kernels(kernel_class: int, start_events, stop_events):

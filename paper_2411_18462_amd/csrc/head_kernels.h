@@ -1,0 +1,808 @@
+// Kernels of the head's operators: the matrix that turns hidden states into logits, in 8 bits for serving, and the cross entropy over
+// its logits with the gradient for training.  The products are those of head_tile.h with m = vocabulary (or hidden channel) and
+// n = rows of hidden states (or vocabulary), so that a lane's four results are neighbours in memory.
+#pragma once
+#include "../../include/svip.h"
+#include "head_tile.h"
+#include "wave_ops.h"
+
+namespace svip {
+
+constexpr float HEAD_LOG2E = 1.4426950408889634f;
+constexpr double HEAD_LN2 = 0.69314718055994530942;
+
+// ---- values in and out ---------------------------------------------------------------------------------------------------------------
+
+template <int DT> struct Stored;       // by svip_dtype
+template <> struct Stored<0> {
+    using type = float;
+    static constexpr int VEC = 4;
+    __device__ static __forceinline__ float get(const float *p) { return *p; }
+    __device__ static __forceinline__ void put4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+};
+template <> struct Stored<1> {
+    using type = __bf16;
+    static constexpr int VEC = 8;
+    __device__ static __forceinline__ void put4(__bf16 *p, f32x4 v)
+    {
+        typedef __bf16 v4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<v4 *>(p) = __builtin_convertvector(v, v4);
+    }
+};
+template <> struct Stored<2> {
+    using type = _Float16;
+    static constexpr int VEC = 8;
+    __device__ static __forceinline__ void put4(_Float16 *p, f32x4 v)
+    {
+        typedef _Float16 v4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<v4 *>(p) = __builtin_convertvector(v, v4);
+    }
+};
+// v[0..count) at p, which is aligned for four
+template <int DT>
+__device__ __forceinline__ void put_up_to_4(typename Stored<DT>::type *p, f32x4 v, int count)
+{
+    if (count >= 4) {
+        Stored<DT>::put4(p, v);
+    } else {
+        for (int e = 0; e < count; ++e) p[e] = (typename Stored<DT>::type)v[e];
+    }
+}
+
+// ---- 8 bits with a scale for each block ------------------------------------------------------------------------------------------------
+//
+// The scale is 2^e with the least e >= -127 that brings the block's largest finite magnitude to 448, the largest e4m3 number, or below: the
+// matrix cores multiply by such scales themselves, and dividing by one is exact, so a code is x / 2^e rounded once.  (With a scale of
+// amax / 448 a block's largest value would be a code without error; e4m3 keeps three mantissa bits at any magnitude, so all that a power
+// of two costs is up to one bit at the small end of 2^15 : 1.)  Values that are not finite do not count for e and become the code of NaN.
+
+constexpr int QBLOCK = 128;
+
+__device__ __forceinline__ unsigned finite_magnitude(float x)
+{
+    const unsigned a = __float_as_uint(x) & 0x7fffffffu;
+    return a < 0x7f800000u ? a : 0u;
+}
+__device__ __forceinline__ int scale_code(unsigned amax)            // e + 127; 127 for a block of zeros
+{
+    if (amax == 0u) return 127;
+    const int e = (int)(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u);        // 448 = 1.75 * 2^8
+    return e < 0 ? 0 : e;
+}
+__device__ __forceinline__ float inverse_scale(int code) { return __uint_as_float((unsigned)(254 - code) << 23); }
+__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, float inv)
+{
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, r, true);
+    unsigned u = (unsigned)r;
+    const float x[4] = {a, b, c, d};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u) u = (u & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));
+    return u;
+}
+
+struct QuantizeArgs {
+    const void *x;
+    long long row_stride;      // elements
+    int rows, cols, kb;        // kb: blocks of 128 columns
+    unsigned char *q;
+    long long q_stride;
+    unsigned char *scale;
+    long long scale_stride;
+};
+
+// 16 bytes of x from column c of row r on, as floats, zeros past the last column.
+template <int DT>
+__device__ __forceinline__ void load_chunk(const QuantizeArgs &a, long long r, int c, float (&v)[Stored<DT>::VEC])
+{
+    constexpr int VEC = Stored<DT>::VEC;
+    using X = typename Stored<DT>::type;
+    const X *p = static_cast<const X *>(a.x) + r * a.row_stride + c;
+    if (c + VEC <= a.cols) {
+        typedef X vec __attribute__((ext_vector_type(VEC)));
+        const vec w = *reinterpret_cast<const vec *>(p);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = (float)w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = c + i < a.cols ? (float)p[i] : 0.f;
+    }
+}
+template <int DT>
+__device__ __forceinline__ void store_codes(unsigned char *p, const float (&v)[Stored<DT>::VEC], float inv)
+{
+    if constexpr (Stored<DT>::VEC == 8) {
+        uint2 u;
+        u.x = codes4(v[0], v[1], v[2], v[3], inv);
+        u.y = codes4(v[4], v[5], v[6], v[7], inv);
+        *reinterpret_cast<uint2 *>(p) = u;
+    } else {
+        *reinterpret_cast<unsigned *>(p) = codes4(v[0], v[1], v[2], v[3], inv);
+    }
+}
+
+// Blocks of 1 x 128: 16 lanes (fp32: 32) a block.
+constexpr int QUANT_WG = 256;
+template <int DT>
+__global__ __launch_bounds__(QUANT_WG) void k_quantize_rows(QuantizeArgs a)
+{
+    constexpr int VEC = Stored<DT>::VEC, LANES = QBLOCK / VEC, PER_WG = QUANT_WG / LANES;
+    const long long block = (long long)blockIdx.x * PER_WG + threadIdx.x / LANES;
+    if (block >= (long long)a.rows * a.kb) return;
+    const long long r = block / a.kb;
+    const int kb = (int)(block - r * a.kb), lane = threadIdx.x % LANES;
+    float v[VEC];
+    load_chunk<DT>(a, r, kb * QBLOCK + lane * VEC, v);
+    unsigned m = 0u;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) m = max(m, finite_magnitude(v[i]));
+#pragma unroll
+    for (int o = LANES / 2; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
+    const int code = scale_code(m);
+    store_codes<DT>(a.q + r * a.q_stride + kb * QBLOCK + lane * VEC, v, inverse_scale(code));
+    if (lane == 0) a.scale[r * a.scale_stride + kb] = (unsigned char)code;
+}
+
+// Blocks of 128 x 128: a workgroup each, the block in registers between its two uses.
+template <int DT>
+__global__ __launch_bounds__(QUANT_WG) void k_quantize_blocks(QuantizeArgs a)
+{
+    constexpr int VEC = Stored<DT>::VEC, LANES = QBLOCK / VEC, ROWS = QUANT_WG / LANES, ROUNDS = QBLOCK / ROWS;
+    const int kb = blockIdx.x % (unsigned)a.kb, rb = blockIdx.x / (unsigned)a.kb;
+    const int c = kb * QBLOCK + (threadIdx.x % LANES) * VEC, r0 = rb * QBLOCK + threadIdx.x / LANES;
+    float v[ROUNDS][VEC];
+    unsigned m = 0u;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+        if (r0 + i * ROWS < a.rows)
+            load_chunk<DT>(a, r0 + i * ROWS, c, v[i]);
+        else
+            for (int j = 0; j < VEC; ++j) v[i][j] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) m = max(m, finite_magnitude(v[i][j]));
+#pragma unroll
+    for (int o = 32; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
+    __shared__ unsigned top[QUANT_WG / 64];
+    if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = max(max(top[0], top[1]), max(top[2], top[3]));
+    const int code = scale_code(m);
+    const float inv = inverse_scale(code);
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i)
+        if (r0 + i * ROWS < a.rows) store_codes<DT>(a.q + (long long)(r0 + i * ROWS) * a.q_stride + c, v[i], inv);
+    if (threadIdx.x == 0) a.scale[rb * a.scale_stride + kb] = (unsigned char)code;
+}
+
+// ---- which tile a workgroup makes --------------------------------------------------------------------------------------------------------
+
+// Workgroups b, b + 8, ... run on one XCD: it gets a contiguous range of tiles, in groups of GROUP columns of tiles (n) by all of m, n
+// first, so that the 32 tiles an XCD works on at a time are about 8 x 4 and share their operands in its L2.
+struct Tiles {
+    int m, n;
+};
+__device__ __forceinline__ void tile_of(unsigned block, Tiles t, int group, int &tm, int &tn)
+{
+    const unsigned total = (unsigned)t.m * (unsigned)t.n, xcd = block & 7u, per = total >> 3, more = total & 7u;
+    const unsigned i = xcd * per + (xcd < more ? xcd : more) + (block >> 3);
+    const unsigned in_group = (unsigned)group * (unsigned)t.m, g = i / in_group, left = (unsigned)t.n - g * (unsigned)group;
+    const unsigned width = left < (unsigned)group ? left : (unsigned)group, j = i - g * in_group;
+    tm = (int)(j / width);
+    tn = (int)(g * (unsigned)group + j % width);
+}
+
+// ---- logits from 8-bit matrices ------------------------------------------------------------------------------------------------------------
+
+struct HeadLogitsArgs {
+    Operand weight, hidden;    // codes; m = vocabulary, n = rows
+    const unsigned char *weight_scale, *hidden_scale;
+    long long weight_scale_stride, hidden_scale_stride;
+    int N, V, K;
+    Tiles tiles;
+    void *out;
+    long long out_stride;      // elements
+};
+
+constexpr int SCALE_STEPS = 64;                        // steps whose scales are in LDS at a time
+constexpr int SCALE_PITCH = SCALE_STEPS + 4;
+
+// A step is 128 values of K: one block of each operand.
+// For 16-bit logits the matrix cores multiply the codes, and take the scales as they are (16x16x128, one scale per 32 values; here all
+// of a step's are the same).  Their sums are not quite fp32: of 8 products next to one another along K, what lies below 2^-13 of the
+// largest is dropped (found with single products; random codes are off by 5e-5 of a sum's rms), which is nothing beside the
+// rounding of the result to 8 or 11 bits.  For fp32 logits the codes become bf16, which holds them exactly, at half the rate: a call
+// of few rows, which waits for the weight's bytes, loses nothing by it.
+__device__ __forceinline__ s16x8 codes_to_bf16(int lo, int hi)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, 1.f, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, 1.f, true)};
+    return __builtin_bit_cast(s16x8, v);
+}
+template <typename S, int DT>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_logits(HeadLogitsArgs a)
+{
+    constexpr int WEIGHT_BLOCKS = (S::BM + QBLOCK - 1) / QBLOCK;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    __shared__ unsigned char hs[S::BN * SCALE_PITCH], ws[WEIGHT_BLOCKS * SCALE_PITCH];
+    int tm, tn;
+    tile_of(blockIdx.x, a.tiles, 4, tm, tn);
+    const int v0 = tm * S::BM, n0 = tn * S::BN;
+    Operand w = a.weight, h = a.hidden;
+    w.base += (long long)v0 * w.stride;
+    h.base += (long long)n0 * h.stride;
+    Stager<KC, S::BM, S::THREADS> sa;
+    Stager<KC, S::BN, S::THREADS> sb;
+    sa.init(w, a.V - v0);
+    sb.init(h, a.N - n0);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
+    static_assert(QBLOCK % S::WM == 0, "a wave's rows of the weight share a scale");
+    Reader<KC, S::BM> ra;
+    Reader<KC, S::BN> rb;
+    ra.init(lane);
+    rb.init(lane);
+    f32x4 acc[S::FM][S::FN];
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    constexpr int COPIES = decltype(sa)::ROUNDS + decltype(sb)::ROUNDS;
+    const int steps = a.K / QBLOCK;
+    const unsigned lds0 = (unsigned)(uintptr_t)smem;
+    auto copy = [&](int s) {
+        const unsigned at = lds0 + (unsigned)(s % S::STAGES) * S::STAGE_BYTES;
+        sa.template copy<1>(at, s * QBLOCK, a.K, 0);
+        sb.template copy<1>(at + S::BM * STEP_BYTES, s * QBLOCK, a.K, 0);
+    };
+    auto scales = [&](int s0) {
+        const int count = steps - s0 < SCALE_STEPS ? steps - s0 : SCALE_STEPS;
+        for (int i = threadIdx.x; i < S::BN * count; i += S::THREADS) {
+            const int r = i / count, s = i - r * count, n = n0 + r < a.N ? n0 + r : a.N - 1;
+            hs[r * SCALE_PITCH + s] = a.hidden_scale[n * a.hidden_scale_stride + s0 + s];
+        }
+        for (int i = threadIdx.x; i < WEIGHT_BLOCKS * count; i += S::THREADS) {
+            const int r = i / count, s = i - r * count, b = v0 / QBLOCK + r, last = (a.V - 1) / QBLOCK;
+            ws[r * SCALE_PITCH + s] = a.weight_scale[(b < last ? b : last) * a.weight_scale_stride + s0 + s];
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s)
+        if (s < steps) copy(s);
+    const int w_row = (v0 % QBLOCK + wm) / QBLOCK;
+    for (int s = 0; s < steps; ++s) {
+        if (s % SCALE_STEPS == 0) {
+            if (s) __syncthreads();
+            scales(s);                     // (the barrier below publishes them)
+        }
+        if (s + S::STAGES - 2 < steps)
+            wait_copies_and_meet<(S::STAGES - 2) * COPIES>();
+        else
+            wait_copies_and_meet<0>();
+        if (s + S::STAGES - 1 < steps) copy(s + S::STAGES - 1);
+        const char *ta = smem + (s % S::STAGES) * S::STAGE_BYTES, *tb = ta + S::BM * STEP_BYTES;
+        const int at = s % SCALE_STEPS;
+        const int sca = ws[w_row * SCALE_PITCH + at];
+        int scb[S::FN];
+        i32x8 fa[S::FM], fb[S::FN];
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            scb[j] = hs[(wn + 16 * j + (lane & 15)) * SCALE_PITCH + at];
+            fb[j] = rb.whole(tb, wn + 16 * j);
+        }
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) fa[i] = ra.whole(ta, wm + 16 * i);
+        if constexpr (DT != SVIP_F32) {
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 0, 0, 0, sca, 0, scb[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) {
+                s16x8 b[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) b[q] = codes_to_bf16(fb[j][2 * q], fb[j][2 * q + 1]);
+#pragma unroll
+                for (int i = 0; i < S::FM; ++i) {
+                    f32x4 block = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) block = Bf16::mfma(codes_to_bf16(fa[i][2 * q], fa[i][2 * q + 1]), b[q], block);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] += __builtin_amdgcn_ldexpf(block[e], sca + scb[j] - 254);
+                }
+            }
+        }
+    }
+    using X = typename Stored<DT>::type;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = n0 + wn + 16 * j + (lane & 15);
+        if (n >= a.N) continue;
+        X *row = static_cast<X *>(a.out) + n * a.out_stride;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int v = v0 + wm + 16 * i + 4 * (lane >> 4);
+            if (v < a.V) put_up_to_4<DT>(row + v, acc[i][j], a.V - v);
+        }
+    }
+}
+
+// ---- cross entropy -------------------------------------------------------------------------------------------------------------------------
+
+// What the calls of a loss and its gradient compute once for all tiles, in the workspace.
+struct HeadScalars {
+    float to_log2;             // accumulated products -> logits / T in units of log 2
+    float grad_top;            // largest |grad_loss| of a row that counts
+    float hidden_mult;         // accumulated G' W -> gradient of the hidden states per grad_loss
+    float weight_mult;         // accumulated G'^T (H grad_loss / grad_top) -> gradient of the weight
+    float hidden_parts, weight_parts;      // fp32: what the parts of the weighted hidden states and of the weight are multiplied by
+    unsigned hidden_max, weight_max;       // fp32: largest finite magnitudes (bits), of hidden states in rows that count
+};
+
+struct HeadArgs {
+    Operand weight, hidden;    // of the tile kernels: m = vocabulary of the piece, n = rows
+    int N, V, D;               // V: rows of the weight in this piece; D: elements of K
+    int v0;                    // the piece's first token
+    Tiles tiles;
+    const HeadScalars *sc;
+    const float *row_inv;      // fp32 [N]: one over what a row's parts are multiplied by
+    const int *targets;
+    float2 *part;              // [tiles of the vocabulary][N] (largest, sum of exp2 relative to it), base 2
+    float *target_logit;       // [N] logits / T of the targets, base 2
+    const float *lse;          // [N]
+    char *grad;                // [planes][N][grad_stride] 16-bit: softmax - one-hot of the piece
+    long long grad_stride;     // elements
+    long long grad_plane;      // bytes
+    int vocab;                 // tokens in all
+    unsigned *flags;
+};
+
+__device__ __forceinline__ bool counts(int target, int vocab) { return target >= 0 && target < vocab; }
+
+// Statistics of a tile of logits: per row the largest and the sum of exponentials over the tile's tokens.
+template <typename T, typename S, int TERMS>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_stats(HeadArgs a)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    int tm, tn;
+    tile_of(blockIdx.x, a.tiles, 4, tm, tn);
+    const int v0 = tm * S::BM, n0 = tn * S::BN;
+    Operand w = a.weight, h = a.hidden;
+    w.base += (long long)v0 * w.stride;
+    h.base += (long long)n0 * h.stride;
+    f32x4 acc[S::FM][S::FN];
+    multiply16<T, S, KC, KC, TERMS>(w, a.V - v0, h, a.N - n0, 0, a.D, smem, acc);
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
+    const float to_log2 = a.sc->to_log2;
+    const bool whole = v0 + S::BM <= a.V;
+    __syncthreads();
+    float2 *red = reinterpret_cast<float2 *>(smem);        // [WAVES_M][BN]
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = n0 + wn + 16 * j + (lane & 15);
+        const int t = n < a.N ? a.targets[n] - a.v0 : -1;
+        const int first = v0 + wm + 4 * (lane >> 4);
+        const float c = TERMS == 3 && n < a.N ? to_log2 * a.row_inv[n] : to_log2;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float z = acc[i][j][e] * c;
+                const int v = first + 16 * i + e;
+                if (v == t && v < a.V) a.target_logit[n] = z;
+                if (!whole && v >= a.V) z = -INFINITY;
+                acc[i][j][e] = z;
+                top = fmaxf(top, z);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(acc[i][j][e] - base);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 16) red[(wave % S::WAVES_M) * S::BN + wn + 16 * j + lane] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::BN && n0 + i < a.N; i += S::THREADS) {
+        float2 r = red[i];
+#pragma unroll
+        for (int k = 1; k < S::WAVES_M; ++k) {
+            const float2 o = red[k * S::BN + i];
+            const float m = fmaxf(r.x, o.x), base = m == -INFINITY ? 0.f : m;
+            r = make_float2(m, r.y * __builtin_amdgcn_exp2f(r.x - base) + o.y * __builtin_amdgcn_exp2f(o.x - base));
+        }
+        a.part[(long long)(a.v0 / S::BM + tm) * a.N + n0 + i] = r;
+    }
+}
+
+struct HeadFinishArgs {
+    const float2 *part;
+    int records, N, vocab;
+    const float *target_logit;
+    const int *targets;
+    float *loss, *lse;
+    unsigned *flags;
+};
+// A row's records joined in 64 bits: 16 rows a workgroup, 16 threads a row.
+constexpr int FINISH_ROWS = 16, FINISH_WG = 256;
+__global__ __launch_bounds__(FINISH_WG) static void k_head_finish(HeadFinishArgs a)
+{
+    __shared__ float top[FINISH_WG];
+    __shared__ double sums[FINISH_WG];
+    const int r = threadIdx.x % FINISH_ROWS, k = threadIdx.x / FINISH_ROWS, n = blockIdx.x * FINISH_ROWS + r;
+    constexpr int SLICES = FINISH_WG / FINISH_ROWS;
+    float m = -INFINITY;
+    double s = 0.0;
+    if (n < a.N)
+        for (int i = k; i < a.records; i += SLICES) {
+            const float2 p = a.part[(long long)i * a.N + n];
+            if (p.x > m) {
+                s = s * (double)__builtin_amdgcn_exp2f(m - p.x) + (double)p.y;
+                m = p.x;
+            } else if (p.x == m || m == -INFINITY) {         // (also NaN first)
+                s += (double)p.y;
+                m = m == -INFINITY ? p.x : m;
+            } else {
+                s += (double)(p.y * __builtin_amdgcn_exp2f(p.x - m));
+            }
+        }
+    top[threadIdx.x] = m;
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (k != 0 || n >= a.N) return;
+    float best = m;
+    for (int i = 1; i < SLICES; ++i) best = fmaxf(best, top[i * FINISH_ROWS + r]);
+    double sum = 0.0;
+    for (int i = 0; i < SLICES; ++i) {
+        const float t = top[i * FINISH_ROWS + r];
+        if (t != -INFINITY) sum += sums[i * FINISH_ROWS + r] * (double)(t == best ? 1.f : __builtin_amdgcn_exp2f(t - best));
+    }
+    const double lse2 = (double)best + log2(sum);
+    const int t = a.targets[n];
+    const bool use = counts(t, a.vocab);
+    if (t >= a.vocab) atomicOr(a.flags, (unsigned)SVIP_FLAG_BAD_TOKEN);
+    a.lse[n] = (float)(lse2 * HEAD_LN2);
+    a.loss[n] = use ? (float)((lse2 - (double)a.target_logit[n]) * HEAD_LN2) : 0.f;
+}
+
+// ---- its gradient ------------------------------------------------------------------------------------------------------------------------
+
+// G' = softmax - one-hot of a tile of recomputed logits, rows without a target zero, in the products' type.  Its entries reach from 1 down to
+// nothing: fp16 (and the two parts of an fp32 value) carry them times 2^15, which keeps 11 bits down to 2^-29.  bf16 keeps its 8 bits
+// at any magnitude: its rounding, 2^-9 of a value, is of the size of the rounding of the gradients themselves.
+constexpr float GRAD_SCALE_F16 = 32768.f;
+
+template <typename T> struct GradOf;
+template <> struct GradOf<Bf16> {
+    using type = __bf16;
+    static constexpr float SCALE = 1.f;
+};
+template <> struct GradOf<F16> {
+    using type = _Float16;
+    static constexpr float SCALE = GRAD_SCALE_F16;
+};
+
+template <typename T, typename S, int TERMS>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_softmax(HeadArgs a)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    int tm, tn;
+    tile_of(blockIdx.x, a.tiles, 4, tm, tn);
+    const int v0 = tm * S::BM, n0 = tn * S::BN;
+    Operand w = a.weight, h = a.hidden;
+    w.base += (long long)v0 * w.stride;
+    h.base += (long long)n0 * h.stride;
+    f32x4 acc[S::FM][S::FN];
+    multiply16<T, S, KC, KC, TERMS>(w, a.V - v0, h, a.N - n0, 0, a.D, smem, acc);
+
+    using X = typename GradOf<T>::type;
+    typedef X x4 __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = n0 + wn + 16 * j + (lane & 15);
+        if (n >= a.N) continue;
+        const float c = TERMS == 3 ? a.sc->to_log2 * a.row_inv[n] : a.sc->to_log2;
+        const int t = a.targets[n];
+        const bool use = counts(t, a.vocab);
+        const float base = a.lse[n] * HEAD_LOG2E;
+        char *row = a.grad + 2 * ((long long)n * a.grad_stride);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int v = v0 + wm + 16 * i + 4 * (lane >> 4);
+            if (v >= a.grad_stride) continue;               // (a multiple of 64)
+            x4 g, low;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float p = __builtin_amdgcn_exp2f(acc[i][j][e] * c - base);
+                if (v + e == t - a.v0) p -= 1.f;
+                p = use && v + e < a.V ? p * GradOf<T>::SCALE : 0.f;
+                g[e] = (X)p;
+                if (TERMS == 3) low[e] = (X)(p - (float)g[e]);
+            }
+            *reinterpret_cast<x4 *>(row + 2 * v) = g;
+            if (TERMS == 3) *reinterpret_cast<x4 *>(row + a.grad_plane + 2 * v) = low;
+        }
+    }
+}
+
+struct HeadHiddenArgs {
+    Operand weight, grad;      // m = hidden channels (k strided), n = rows (k contiguous); k = tokens of the piece
+    int N, D, V;
+    Tiles tiles;
+    int splits, per_split;     // tokens of a split, a multiple of the step
+    int first;                 // the first piece: nothing to add to
+    float *sum;                // [splits][N][D]
+};
+// Gradient of the hidden states: G' W over the tokens of a piece, added to what the pieces before it gave.
+template <typename T, typename S, int TERMS>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_grad_hidden(HeadHiddenArgs a)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    const unsigned tiles = (unsigned)a.tiles.m * (unsigned)a.tiles.n, split = blockIdx.x / tiles;
+    int tm, tn;
+    tile_of(blockIdx.x - split * tiles, a.tiles, 4, tm, tn);
+    const int d0 = tm * S::BM, n0 = tn * S::BN, k0 = (int)split * a.per_split, k_end = min(a.V, k0 + a.per_split);
+    Operand w = a.weight, g = a.grad;
+    w.base += 2 * d0;
+    g.base += (long long)n0 * g.stride;
+    f32x4 acc[S::FM][S::FN];
+    multiply16<T, S, KS, KC, TERMS>(w, a.D - d0, g, a.N - n0, k0, k_end, smem, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
+    float *sum = a.sum + (long long)split * a.N * a.D;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = n0 + wn + 16 * j + (lane & 15);
+        if (n >= a.N) continue;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int d = d0 + wm + 16 * i + 4 * (lane >> 4);
+            if (d >= a.D) continue;
+            f32x4 *p = reinterpret_cast<f32x4 *>(sum + (long long)n * a.D + d);
+            *p = a.first ? acc[i][j] : *p + acc[i][j];
+        }
+    }
+}
+
+struct HeadHiddenFinishArgs {
+    const float *sum;
+    int splits, N, D, Dp;      // D of the output, Dp of the sums (both multiples of 4)
+    const HeadScalars *sc;
+    const int *targets;
+    const float *grad_loss;
+    int vocab;
+    void *out;
+    long long out_stride;
+};
+template <int DT>
+__global__ __launch_bounds__(256) void k_head_hidden_finish(HeadHiddenFinishArgs a)
+{
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4, per_row = a.D;
+    const long long n = i / per_row;
+    const int d = (int)(i - n * per_row);
+    if (n >= a.N) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    float m = 0.f;
+    if (counts(a.targets[n], a.vocab)) {
+        m = a.grad_loss[n] * a.sc->hidden_mult;
+        for (int k = 0; k < a.splits; ++k) s += *reinterpret_cast<const f32x4 *>(a.sum + ((long long)k * a.N + n) * a.Dp + d);
+    }
+    Stored<DT>::put4(static_cast<typename Stored<DT>::type *>(a.out) + n * a.out_stride + d, s * m);
+}
+
+struct HeadWeightArgs {
+    Operand hidden, grad;      // m = hidden channels, n = tokens of the piece, both k strided; k = rows
+    int N, D, V, Dp;           // D: channels of the output, Dp: of the operand
+    Tiles tiles;
+    const HeadScalars *sc;
+    void *out;                 // row 0: the piece's first token
+    long long out_stride;
+};
+// Gradient of the weight: G'^T (H grad_loss / grad_top).
+template <typename T, typename S, int TERMS, int DT>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_grad_weight(HeadWeightArgs a)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    int tm, tn;
+    tile_of(blockIdx.x, a.tiles, 4, tm, tn);
+    const int d0 = tm * S::BM, v0 = tn * S::BN;
+    Operand h = a.hidden, g = a.grad;
+    h.base += 2 * d0;
+    g.base += 2 * v0;
+    f32x4 acc[S::FM][S::FN];
+    multiply16<T, S, KS, KS, TERMS>(h, a.Dp - d0, g, (int)(g.stride / 2) - v0, 0, a.N, smem, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
+    const float m = a.sc->weight_mult;
+    using X = typename Stored<DT>::type;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int v = v0 + wn + 16 * j + (lane & 15);
+        if (v >= a.V) continue;
+        X *row = static_cast<X *>(a.out) + v * a.out_stride;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int d = d0 + wm + 16 * i + 4 * (lane >> 4);
+            if (d < a.D) Stored<DT>::put4(row + d, acc[i][j] * m);
+        }
+    }
+}
+
+// ---- what goes before the products -----------------------------------------------------------------------------------------------------------
+
+// fp32 values as two fp16 parts: x 2^s = high + low, with 2^s bringing the largest magnitude of the row (hidden states in the logits) or of the matrix
+// (where rows are summed over) to [2^14, 2^15).  Together they keep 22 bits of a value down to 2^-17 of that largest one, and 2^-40 of it
+// below; of a product all but low x low is taken.  Products of three bf16 parts would need no scale, but six products for 24 bits.
+__device__ __forceinline__ float part_scale(unsigned max_bits)
+{
+    if (max_bits == 0u) return 1.f;
+    const int e = 127 + 14 - ((int)(max_bits >> 23) - 127);
+    return __uint_as_float((unsigned)min(max(e, 1), 253) << 23);
+}
+__device__ __forceinline__ void store_parts(char *out, long long plane, const float (&v)[8], float s)
+{
+    f16x8 high, low;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        high[e] = (_Float16)(v[e] * s);
+        low[e] = (_Float16)(v[e] * s - (float)high[e]);
+    }
+    *reinterpret_cast<f16x8 *>(out) = high;
+    *reinterpret_cast<f16x8 *>(out + plane) = low;
+}
+
+struct HeadMaxArgs {
+    const float *x;
+    long long stride;
+    int rows, cols;            // cols: a multiple of 4
+    const int *targets;        // null, or rows without a target do not count
+    int vocab;
+    unsigned *out;             // starts at 0
+};
+// Largest finite magnitude of a matrix (bits), joined by an integer maximum, whose order does not matter.
+__global__ __launch_bounds__(256) static void k_head_max(HeadMaxArgs a)
+{
+    const int per_row = a.cols / 4;
+    const long long total = (long long)a.rows * per_row;
+    unsigned m = 0u;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+        const long long r = i / per_row;
+        if (a.targets && !counts(a.targets[r], a.vocab)) continue;
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.x + r * a.stride + (i - r * per_row) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = max(m, finite_magnitude(v[e]));
+    }
+#pragma unroll
+    for (int o = 32; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
+    if ((threadIdx.x & 63) == 0 && m) atomicMax(a.out, m);
+}
+struct HeadClearArgs {
+    HeadScalars *sc;
+};
+__global__ static void k_head_clear(HeadClearArgs a) { a.sc->hidden_max = a.sc->weight_max = 0u; }
+
+struct HeadScalarsArgs {
+    HeadScalars *sc;
+    int fp32;
+    int N, vocab;
+    float temperature;
+    const int *targets;
+    const float *grad_loss;    // null: a loss alone
+    float grad_scale;          // of G'
+    unsigned *flags;
+};
+constexpr int SCALARS_WG = 1024;
+__global__ __launch_bounds__(SCALARS_WG) static void k_head_scalars(HeadScalarsArgs a)
+{
+    __shared__ float tops[SCALARS_WG / 64];
+    float top = 0.f;
+    bool bad = false;
+    if (a.grad_loss)
+        for (int n = threadIdx.x; n < a.N; n += SCALARS_WG) {
+            const int t = a.targets[n];
+            bad |= t >= a.vocab;
+            if (counts(t, a.vocab)) top = fmaxf(top, fabsf(a.grad_loss[n]));
+        }
+    top = wave_reduce(top, OpMax{});
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    if (bad) atomicOr(a.flags, (unsigned)SVIP_FLAG_BAD_TOKEN);
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int i = 1; i < SCALARS_WG / 64; ++i) top = fmaxf(top, tops[i]);
+    // grad_loss / grad_top is at most 1 in magnitude, so the largest weighted hidden state is at most the largest hidden state
+    const float hs = a.fp32 ? part_scale(a.sc->hidden_max) : 1.f, ws = a.fp32 ? part_scale(a.sc->weight_max) : 1.f;
+    const double t = 1.0 / (double)a.temperature;
+    a.sc->hidden_parts = hs;
+    a.sc->weight_parts = ws;
+    a.sc->to_log2 = (float)(1.4426950408889634 * t / (double)ws);
+    a.sc->grad_top = top;
+    a.sc->hidden_mult = (float)(t / ((double)a.grad_scale * (double)ws));
+    a.sc->weight_mult = (float)((double)top * t / ((double)a.grad_scale * (double)hs));
+}
+
+struct HeadPackArgs {
+    const void *x;
+    long long stride;          // elements
+    int rows, cols, cols_p;    // cols_p: of the packed rows, a multiple of 8
+    char *out;                 // [planes][rows][cols_p] 16-bit
+    long long plane;           // bytes
+    const HeadScalars *sc;
+    const int *targets;        // hidden states for the gradient of the weight: rows weighted by grad_loss / grad_top, 0 where they do not count
+    const float *grad_loss;
+    int vocab;
+    float *row_inv;            // hidden states for the logits: parts of their own scale for each row
+};
+template <int DT>
+__device__ __forceinline__ void load_columns(const HeadPackArgs &a, long long r, int c, float (&v)[8])
+{
+    const auto *x = static_cast<const typename Stored<DT>::type *>(a.x) + r * a.stride + c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < a.cols ? (float)x[e] : 0.f;
+}
+// Eight columns a thread: a weight (fp32), or hidden states weighted for the gradient of the weight.
+template <int DT>
+__global__ __launch_bounds__(256) void k_head_pack(HeadPackArgs a)
+{
+    const int per_row = a.cols_p / 8;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, r = i / per_row;
+    if (r >= a.rows) return;
+    const int c = (int)(i - r * per_row) * 8;
+    float v[8];
+    load_columns<DT>(a, r, c, v);
+    if (a.targets) {
+        const bool use = counts(a.targets[r], a.vocab);
+        const float top = a.sc->grad_top, w = top > 0.f ? a.grad_loss[r] / top : a.grad_loss[r];       // (else 0 or NaN)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = use ? v[e] * w : 0.f;
+    }
+    char *out = a.out + (r * a.cols_p + c) * 2;
+    if constexpr (DT == SVIP_F32) {
+        store_parts(out, a.plane, v, a.targets ? a.sc->hidden_parts : a.sc->weight_parts);
+    } else {
+        using X = typename Stored<DT>::type;
+        typedef X x8 __attribute__((ext_vector_type(8)));
+        x8 y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (X)v[e];
+        *reinterpret_cast<x8 *>(out) = y;
+    }
+}
+// fp32 hidden states for the logits, a wave each row: one that does not count may hold anything and costs the others nothing.
+__global__ __launch_bounds__(256) static void k_head_pack_rows(HeadPackArgs a)
+{
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (r >= a.rows) return;
+    unsigned m = 0u;
+    float v[8];
+    for (int c = lane * 8; c < a.cols_p; c += 512) {
+        load_columns<SVIP_F32>(a, r, c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, finite_magnitude(v[e]));
+    }
+#pragma unroll
+    for (int o = 32; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
+    const float s = part_scale(m);
+    for (int c = lane * 8; c < a.cols_p; c += 512) {
+        load_columns<SVIP_F32>(a, r, c, v);
+        store_parts(a.out + ((long long)r * a.cols_p + c) * 2, a.plane, v, s);
+    }
+    if (lane == 0) a.row_inv[r] = 1.f / s;
+}
+
+}  // namespace svip

@@ -1,0 +1,231 @@
+// Products of two matrices on the matrix cores, tile by tile: the core of the head's operators (head_kernels.h).
+//
+//   C[m, n] = sum over k of A(m, k) B(n, k)
+//
+// A workgroup of WAVES_M x WAVES_N waves makes a BM x BN tile of C; a wave holds its (BM / WAVES_M) x (BN / WAVES_N) part as
+// 16 x 16 fragments in registers.  K goes by in steps of 128 bytes (64 16-bit values or 128 8-bit ones) that are copied from memory
+// straight into LDS (global_load_lds_dwordx4, no registers on the way), STAGES deep: while the waves multiply one step, the next
+// STAGES - 1 are on their way, and one barrier per step both publishes a step and frees the oldest buffer.
+//
+// An operand comes in one of two layouts:
+//   KC  k contiguous (rows of m or n): the LDS tile is [rows][128 bytes]; a fragment is read with ds_read_b128.  16-byte chunk c of
+//       row r lies at chunk c ^ (r / 2 % 8), so that the 16 rows of a fragment, of which two span the 64 banks, meet no bank twice.
+//   KS  k strided (rows of k, 16-bit values): the LDS tile is [64][columns]; a fragment is read with ds_read_b64_tr_b16, which
+//       gives lane i of 16 the column i of a 4 x 16 block.  The four rows of a block would lie in the same banks: chunk c of
+//       row k lies at chunk c ^ (2 (k % 4) + 8 (k / 8 % 2)).
+// The copy into LDS writes lane after lane, so the permutation is made by which chunk a lane asks for.
+//
+// Rows past the end of an operand are read as its last row (their results are not stored); positions past the end of K are read
+// from a line of zeros in both operands, so that nothing outside the operands is ever multiplied.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace svip {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int STEP_BYTES = 128;                   // of K per step
+
+// Zeros that lanes past the end of K read (the largest read is 16 bytes a lane).
+__device__ __attribute__((aligned(256))) static const unsigned zero_line[64] = {};
+
+enum { KC = 0, KS = 1 };
+
+struct Operand {
+    const char *base;          // element (0, 0) of the tile's operand
+    long long stride;          // bytes between its rows (of m or n: KC, of k: KS)
+    long long plane;           // bytes between its planes (see TERMS)
+};
+
+// Copies 16 bytes a lane into LDS at `lds` (wave-uniform) + 16 * lane.  Written as assembly so that the compiler does not wait for
+// the copy before every LDS read that might alias it; wait_copies() is the wait.
+__device__ __forceinline__ void copy_to_lds(const char *base, unsigned voff, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void copy_to_lds(const char *lane_address, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_address) : "memory", "m0");
+}
+// All but the last `LEFT` copies of this wave have landed and its LDS reads have returned; then the barrier.
+template <int LEFT>
+__device__ __forceinline__ void wait_copies_and_meet()
+{
+    static_assert(LEFT < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// One operand's part of a workgroup's tile: ROWS rows (KC) or columns (KS).
+template <int LAYOUT, int ROWS, int THREADS>
+struct Stager {
+    static constexpr int CHUNKS = ROWS * STEP_BYTES / 16;
+    static constexpr int ROUNDS = CHUNKS > THREADS ? CHUNKS / THREADS : 1;      // (fewer chunks than threads: some are copied twice)
+    static constexpr int BYTES = ROWS * STEP_BYTES;
+    static constexpr int PER_ROW = ROWS / 8;                                   // KS: chunks in a row
+    static_assert(CHUNKS % 64 == 0 && (CHUNKS >= THREADS ? CHUNKS % THREADS == 0 : THREADS % CHUNKS == 0), "whole waves copy");
+
+    Operand op;
+    unsigned voff[ROUNDS];
+    unsigned lds[ROUNDS];      // wave-uniform
+
+    // rows: of the operand from the tile's first on, at least 1 (KS: columns, a multiple of 8)
+    __device__ void init(const Operand &o, int rows)
+    {
+        op = o;
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int c = (r * THREADS + (int)threadIdx.x) % CHUNKS;
+            lds[r] = (unsigned)__builtin_amdgcn_readfirstlane(c & ~63) * 16u;
+            if (LAYOUT == KC) {
+                const int row = c >> 3, chunk = (c & 7) ^ ((row >> 1) & 7);
+                voff[r] = (unsigned)(row < rows ? row : rows - 1) * (unsigned)op.stride + (unsigned)chunk * 16u;
+            } else {
+                const int k = c / PER_ROW, chunk = (c % PER_ROW) ^ twist(k);
+                voff[r] = (unsigned)k * (unsigned)op.stride + (unsigned)(chunk < rows / 8 ? chunk : 0) * 16u;
+            }
+        }
+    }
+    __device__ static int twist(int k) { return (((k & 3) << 1) | (k & 8)) & (PER_ROW - 1); }
+
+    // Step at `k` (element index, a multiple of the step) of plane `plane` into the buffer at `at`; k_end: elements of K.
+    template <int ESIZE>
+    __device__ __forceinline__ void copy(unsigned at, int k, int k_end, int plane) const
+    {
+        constexpr int STEP = STEP_BYTES / ESIZE;
+        const char *base = op.base + plane * op.plane + (LAYOUT == KC ? (long long)k * ESIZE : k * op.stride);
+        if (k + STEP <= k_end) {
+#pragma unroll
+            for (int r = 0; r < ROUNDS; ++r) copy_to_lds(base, voff[r], at + lds[r]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < ROUNDS; ++r) {
+                const int c = (r * THREADS + (int)threadIdx.x) % CHUNKS;
+                const int mine = LAYOUT == KC ? k + ((c & 7) ^ ((c >> 4) & 7)) * (16 / ESIZE) : k + c / PER_ROW;
+                const char *p = mine < k_end ? base + voff[r] : reinterpret_cast<const char *>(zero_line);
+                copy_to_lds(p, at + lds[r]);
+            }
+        }
+    }
+};
+
+// Reads fragments of an operand's LDS tile: 16 rows of m or n from `row0` (a multiple of 16) and half a step of 16-bit values, or a whole step
+// of 8-bit ones.  Lane l has row l % 16; of K it has, for 16 bits, the 8 values from 8 (l / 16) on in half h.
+template <int LAYOUT, int ROWS>
+struct Reader {
+    unsigned at[2];
+    __device__ void init(int lane)
+    {
+        const int row = lane & 15, g = lane >> 4;
+        if (LAYOUT == KC) {
+            at[0] = (unsigned)(row * STEP_BYTES + (((g) ^ (row >> 1)) & 7) * 16);
+            at[1] = (unsigned)(row * STEP_BYTES + (((4 + g) ^ (row >> 1)) & 7) * 16);
+        } else {
+            const int k = 8 * g + (row >> 2);
+            at[0] = (unsigned)(k * ROWS * 2 + (row & 1) * 8);
+            at[1] = (unsigned)((((row & 3) >> 1)) ^ Stager<KS, ROWS, 64>::twist(k));
+        }
+    }
+    __device__ __forceinline__ s16x8 half(const char *tile, int row0, int h) const
+    {
+        if (LAYOUT == KC) return *reinterpret_cast<const s16x8 *>(tile + at[h] + row0 * STEP_BYTES);
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const unsigned a = at[0] + (((unsigned)(row0 / 8)) ^ at[1]) * 16u;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + a + (32 * h) * ROWS * 2));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + a + (32 * h + 4) * ROWS * 2));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    __device__ __forceinline__ i32x8 whole(const char *tile, int row0) const
+    {
+        const i32x4 lo = *reinterpret_cast<const i32x4 *>(tile + at[0] + row0 * STEP_BYTES);
+        const i32x4 hi = *reinterpret_cast<const i32x4 *>(tile + at[1] + row0 * STEP_BYTES);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+struct Bf16 {
+    __device__ static __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+struct F16 {
+    __device__ static __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, int STAGES_>
+struct TileShape {
+    static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, STAGES = STAGES_;
+    static constexpr int THREADS = 64 * WAVES_M * WAVES_N;
+    static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FM = WM / 16, FN = WN / 16;
+    static constexpr int STAGE_BYTES = (BM + BN) * STEP_BYTES;
+    static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
+    static_assert(WM % 16 == 0 && WN % 16 == 0, "whole fragments");
+};
+
+// The loop over K of 16-bit operands.  TERMS = 1: one plane each.  TERMS = 3: two planes (high and low part) each, and the products
+// low x high, high x low and high x high, the small ones first.
+template <typename T, typename S, int LA, int LB, int TERMS>
+__device__ __forceinline__ void multiply16(const Operand &a, int a_rows, const Operand &b, int b_rows, int k0, int k_end, char *smem,
+                                           f32x4 (&acc)[S::FM][S::FN])
+{
+    Stager<LA, S::BM, S::THREADS> sa;
+    Stager<LB, S::BN, S::THREADS> sb;
+    sa.init(a, a_rows);
+    sb.init(b, b_rows);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
+    Reader<LA, S::BM> ra;
+    Reader<LB, S::BN> rb;
+    ra.init(lane);
+    rb.init(lane);
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    constexpr int STEP = STEP_BYTES / 2, COPIES = decltype(sa)::ROUNDS + decltype(sb)::ROUNDS;
+    const int per_term = (k_end - k0 + STEP - 1) / STEP, steps = TERMS * per_term;
+    const unsigned lds0 = (unsigned)(uintptr_t)smem;
+    auto copy = [&](int s) {
+        const int term = TERMS == 1 ? 0 : s / per_term;
+        const int k = k0 + (s - term * per_term) * STEP;
+        const unsigned at = lds0 + (unsigned)(s % S::STAGES) * S::STAGE_BYTES;
+        sa.template copy<2>(at, k, k_end, TERMS == 1 ? 0 : (term == 0));       // plane 0: high, 1: low
+        sb.template copy<2>(at + S::BM * STEP_BYTES, k, k_end, TERMS == 1 ? 0 : (term == 1));
+    };
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s)
+        if (s < steps) copy(s);
+    for (int s = 0; s < steps; ++s) {
+        if (s + S::STAGES - 2 < steps)
+            wait_copies_and_meet<(S::STAGES - 2) * COPIES>();
+        else
+            wait_copies_and_meet<0>();
+        if (s + S::STAGES - 1 < steps) copy(s + S::STAGES - 1);
+        const char *ta = smem + (s % S::STAGES) * S::STAGE_BYTES, *tb = ta + S::BM * STEP_BYTES;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            s16x8 fa[S::FM], fb[S::FN];
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) fb[j] = rb.half(tb, wn + 16 * j, h);
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) fa[i] = ra.half(ta, wm + 16 * i, h);
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j) acc[i][j] = T::mfma(fa[i], fb[j], acc[i][j]);
+        }
+    }
+}
+
+}  // namespace svip

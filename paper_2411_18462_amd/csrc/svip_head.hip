@@ -1,0 +1,444 @@
+// The head's operators: entry points, shapes and workspaces (kernels: head_kernels.h, products: head_tile.h).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "head_kernels.h"
+
+namespace svip {
+
+static bool dtype_ok(int d) { return d == SVIP_F32 || d == SVIP_BF16 || d == SVIP_F16; }
+static int size_of(int d) { return d == SVIP_F32 ? 4 : 2; }
+static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+static int up(int n, int to) { return (n + to - 1) / to * to; }
+static int ceil_div(long long n, long long d) { return (int)((n + d - 1) / d); }
+
+constexpr int HEAD_MAX_ROWS = 1 << 20;                 // of hidden states
+constexpr int HEAD_MAX_VOCAB = 1 << 22;
+constexpr int HEAD_MAX_WIDTH = 1 << 17;                // hidden channels
+constexpr long long HEAD_MAX_STRIDE = 1 << 23;         // elements: 256 rows of a tile lie within 32 bits of bytes
+
+// A matrix of rows x cols of dtype: stride of a row in whole 16 bytes, within reach of a tile's 32-bit offsets.
+static svip_status check_matrix(const void *p, int dtype, int cols, long long stride)
+{
+    if (stride < cols || stride > HEAD_MAX_STRIDE) return SVIP_ERR_SHAPE;
+    return aligned16(p) && stride * size_of(dtype) % 16 == 0 ? SVIP_OK : SVIP_ERR_ALIGN;
+}
+
+template <typename A>
+static bool launch(void (*kernel)(A), long long grid, unsigned block, hipStream_t st, const A &args)
+{
+    A copy = args;
+    void *argv[] = {&copy};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)grid), dim3(block), argv, 0, st) == hipSuccess;
+}
+
+template <typename F>
+static bool by_dtype(int d, F f)
+{
+    if (d == SVIP_F32) return f(std::integral_constant<int, SVIP_F32>{});
+    if (d == SVIP_BF16) return f(std::integral_constant<int, SVIP_BF16>{});
+    return f(std::integral_constant<int, SVIP_F16>{});
+}
+
+// ---- shapes of the tiles -------------------------------------------------------------------------------------------------------------------
+
+using Large = TileShape<256, 256, 2, 4, 2>;
+using Middle = TileShape<128, 128, 2, 2, 3>;           // (fp32 logits of 8-bit matrices: the tile's bf16 fragments need the registers)
+using Small = TileShape<128, 64, 4, 1, 3>;
+
+// f with the shape for `rows` rows of hidden states (n of the tiles).
+template <typename F>
+static bool by_rows(int rows, F f)
+{
+    if (rows > 64) return f(Large{});
+    return f(Small{});
+}
+
+// f with the products' type and terms of a dtype: fp32 values go as two fp16 parts.
+template <typename F>
+static bool by_product(int dtype, F f)
+{
+    if (dtype == SVIP_F32) return f(F16{}, std::integral_constant<int, 3>{}, std::integral_constant<int, SVIP_F32>{});
+    if (dtype == SVIP_BF16) return f(Bf16{}, std::integral_constant<int, 1>{}, std::integral_constant<int, SVIP_BF16>{});
+    return f(F16{}, std::integral_constant<int, 1>{}, std::integral_constant<int, SVIP_F16>{});
+}
+
+// ---- workspace ---------------------------------------------------------------------------------------------------------------------------------
+
+constexpr size_t HEAD_HEADER = 512;                    // flag word (256 bytes), HeadScalars
+constexpr int TILE_MAX = 256;
+constexpr size_t PIECE_BYTES = (size_t)256 << 20;      // of a piece's softmax: what the memory-side cache holds
+constexpr int LEAST_PIECE = 2048;                      // tokens
+
+struct HeadPlan {
+    int planes, width;         // fp32: 2; channels of packed rows
+    int piece;                 // tokens of a piece of the vocabulary, a multiple of TILE_MAX
+    int splits, per_split;     // of a piece's tokens in the gradient of the hidden states
+    size_t part, target, rows, hidden, weighted, weight, grad, sum, bytes;     // offsets
+    long long grad_stride;
+};
+
+static HeadPlan plan(int call, int dtype, int N, int V, int D)
+{
+    HeadPlan p = {};
+    const bool f32 = dtype == SVIP_F32, grad = call == SVIP_HEAD_LOSS_GRAD;
+    p.planes = f32 ? 2 : 1;
+    p.width = up(D, 8);
+    const int least = N > 64 ? Large::BM : Small::BM;
+    // pieces: of the softmax in the gradient, of the weight's parts in fp32; equal, so that none is a sliver
+    long long most = V;
+    if (grad) most = (long long)(PIECE_BYTES / ((size_t)N * 2 * p.planes));
+    if (f32) most = most < (long long)(PIECE_BYTES / ((size_t)p.width * 4)) ? most : (long long)(PIECE_BYTES / ((size_t)p.width * 4));
+    if (most < LEAST_PIECE) most = LEAST_PIECE;
+    p.piece = up(ceil_div(V, ceil_div(V, most)), TILE_MAX);
+    if (p.piece > up(V, TILE_MAX)) p.piece = up(V, TILE_MAX);
+    p.grad_stride = p.piece;
+    size_t at = HEAD_HEADER;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up256(bytes);
+        return here;
+    };
+    if (call == SVIP_HEAD_LOGITS) {
+        p.bytes = at;
+        return p;
+    }
+    const size_t packed = (size_t)p.planes * N * p.width * 2;
+    // (a loss and its gradient may use one workspace of either's size or more, one after the other: nothing is kept between them)
+    p.part = take((size_t)ceil_div(V, least) * N * sizeof(float2));
+    p.target = take((size_t)N * sizeof(float));
+    if (f32) {
+        p.rows = take((size_t)N * sizeof(float));
+        p.hidden = take(packed);
+        p.weight = take((size_t)2 * p.piece * p.width * 2);
+    }
+    if (grad) {
+        p.weighted = take(packed);
+        p.grad = take((size_t)p.planes * N * p.grad_stride * 2);
+        // enough workgroups to fill the chip twice over where the gradient of the hidden states has few tiles
+        const long long tiles = N > 64 ? (long long)ceil_div(p.width, Large::BM) * ceil_div(N, Large::BN)
+                                       : (long long)ceil_div(p.width, Small::BM) * ceil_div(N, Small::BN);
+        const int steps = p.piece / 64;
+        long long splits = 512 / tiles;
+        if (splits > steps / 8) splits = steps / 8;
+        if (splits < 1) splits = 1;
+        p.per_split = ceil_div(steps, splits) * 64;
+        p.splits = ceil_div(p.piece, p.per_split);
+        p.sum = take((size_t)p.splits * N * p.width * sizeof(float));
+    }
+    p.bytes = at;
+    return p;
+}
+
+static svip_status check_sizes(int N, int V, int D)
+{
+    return N <= 0 || N > HEAD_MAX_ROWS || V <= 0 || V > HEAD_MAX_VOCAB || D <= 0 || D > HEAD_MAX_WIDTH ? SVIP_ERR_SHAPE : SVIP_OK;
+}
+static svip_status check_workspace(const void *ws, size_t bytes, size_t need)
+{
+    return !ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || bytes < need ? SVIP_ERR_WORKSPACE : SVIP_OK;
+}
+
+// ---- loss and gradient -----------------------------------------------------------------------------------------------------------------------------
+
+struct LossCall {
+    const void *hidden, *weight;
+    int dtype, N, V, D;
+    long long hidden_stride, weight_stride;
+    float temperature;
+    const int *targets;
+    char *ws;
+    hipStream_t st;
+};
+
+static svip_status check_loss(const LossCall &c, const void *out, int call, size_t ws_bytes)
+{
+    if (!c.hidden || !c.weight || !c.targets || !out) return SVIP_ERR_NULL;
+    if (!dtype_ok(c.dtype)) return SVIP_ERR_DTYPE;
+    if (svip_status s = check_sizes(c.N, c.V, c.D)) return s;
+    if (svip_status s = check_matrix(c.hidden, c.dtype, c.D, c.hidden_stride)) return s;
+    if (svip_status s = check_matrix(c.weight, c.dtype, c.D, c.weight_stride)) return s;
+    if (c.D * size_of(c.dtype) % 16 != 0) return SVIP_ERR_ALIGN;
+    if (!(c.temperature > 0.f) || !isfinite(c.temperature)) return SVIP_ERR_PARAM;
+    return check_workspace(c.ws, ws_bytes, plan(call, c.dtype, c.N, c.V, c.D).bytes);
+}
+
+static HeadScalars *scalars(const LossCall &c) { return reinterpret_cast<HeadScalars *>(c.ws + 256); }
+
+// The scalars that the tiles use, and in fp32 the parts of the hidden states.
+static bool prepare(const LossCall &c, const HeadPlan &p, const float *grad_loss, float grad_scale)
+{
+    const bool f32 = c.dtype == SVIP_F32;
+    HeadScalars *sc = scalars(c);
+    if (f32) {
+        if (!launch(k_head_clear, 1, 1, c.st, HeadClearArgs{sc})) return false;
+        auto largest = [&](const void *x, long long stride, int rows, const int *targets, unsigned *out) {
+            HeadMaxArgs m = {static_cast<const float *>(x), stride, rows, c.D, targets, c.V, out};
+            const long long groups = ceil_div((long long)rows * (c.D / 4), 256 * 8);
+            return launch(k_head_max, groups < 2048 ? groups : 2048, 256, c.st, m);
+        };
+        if (!largest(c.weight, c.weight_stride, c.V, nullptr, &sc->weight_max)) return false;
+        if (grad_loss && !largest(c.hidden, c.hidden_stride, c.N, c.targets, &sc->hidden_max)) return false;
+    }
+    HeadScalarsArgs a = {sc, f32, c.N, c.V, c.temperature, c.targets, grad_loss, grad_scale, reinterpret_cast<unsigned *>(c.ws)};
+    if (!launch(k_head_scalars, 1, SCALARS_WG, c.st, a)) return false;
+    if (!f32) return true;
+    HeadPackArgs h = {};
+    h.x = c.hidden;
+    h.stride = c.hidden_stride;
+    h.rows = c.N;
+    h.cols = c.D;
+    h.cols_p = p.width;
+    h.out = c.ws + p.hidden;
+    h.plane = (long long)c.N * p.width * 2;
+    h.row_inv = reinterpret_cast<float *>(c.ws + p.rows);
+    return launch(k_head_pack_rows, ceil_div(c.N, 4), 256, c.st, h);
+}
+
+// The arguments of a piece's tiles of logits; fp32: after the piece's parts have been laid out.
+static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, HeadArgs *out)
+{
+    HeadArgs a = {};
+    const int size = size_of(c.dtype);
+    const char *rows = static_cast<const char *>(c.weight) + (long long)v0 * c.weight_stride * size;
+    if (c.dtype == SVIP_F32) {
+        HeadPackArgs w = {};
+        w.x = rows;
+        w.stride = c.weight_stride;
+        w.rows = count;
+        w.cols = c.D;
+        w.cols_p = p.width;
+        w.out = c.ws + p.weight;
+        w.plane = (long long)p.piece * p.width * 2;
+        w.sc = scalars(c);
+        if (!launch(k_head_pack<SVIP_F32>, ceil_div((long long)count * (p.width / 8), 256), 256, c.st, w)) return false;
+        a.weight = {w.out, (long long)p.width * 2, w.plane};
+        a.hidden = {c.ws + p.hidden, (long long)p.width * 2, (long long)c.N * p.width * 2};
+        a.row_inv = reinterpret_cast<const float *>(c.ws + p.rows);
+    } else {
+        a.weight = {rows, c.weight_stride * size, 0};
+        a.hidden = {static_cast<const char *>(c.hidden), c.hidden_stride * size, 0};
+    }
+    a.N = c.N;
+    a.V = count;
+    a.D = p.width;
+    a.v0 = v0;
+    a.sc = scalars(c);
+    a.targets = c.targets;
+    a.part = reinterpret_cast<float2 *>(c.ws + p.part);
+    a.target_logit = reinterpret_cast<float *>(c.ws + p.target);
+    a.vocab = c.V;
+    a.flags = reinterpret_cast<unsigned *>(c.ws);
+    *out = a;
+    return true;
+}
+
+static bool run_loss(const LossCall &c, const HeadPlan &p, float *loss, float *lse)
+{
+    if (!prepare(c, p, nullptr, 1.f)) return false;
+    const int whole = c.dtype == SVIP_F32 ? p.piece : c.V;
+    int records = 0;
+    for (int v0 = 0; v0 < c.V; v0 += whole) {
+        const int count = c.V - v0 < whole ? c.V - v0 : whole;
+        HeadArgs a;
+        if (!piece_args(c, p, v0, count, &a)) return false;
+        const bool ok = by_product(c.dtype, [&](auto type, auto terms, auto) {
+            return by_rows(c.N, [&](auto shape) {
+                using S = decltype(shape);
+                a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
+                records = v0 / S::BM + a.tiles.m;
+                return launch(k_head_stats<decltype(type), S, decltype(terms)::value>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
+            });
+        });
+        if (!ok) return false;
+    }
+    HeadFinishArgs f = {reinterpret_cast<const float2 *>(c.ws + p.part), records, c.N, c.V, reinterpret_cast<const float *>(c.ws + p.target), c.targets,
+                        loss, lse, reinterpret_cast<unsigned *>(c.ws)};
+    return launch(k_head_finish, ceil_div(c.N, FINISH_ROWS), FINISH_WG, c.st, f);
+}
+
+struct GradOut {
+    void *hidden, *weight;
+    long long hidden_stride, weight_stride;
+};
+
+static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, const float *grad_loss, const GradOut &out)
+{
+    const float scale = c.dtype == SVIP_BF16 ? 1.f : GRAD_SCALE_F16;
+    if (!prepare(c, p, grad_loss, scale)) return false;
+    const int size = size_of(c.dtype);
+    const long long packed_plane = (long long)c.N * p.width * 2, grad_plane = (long long)c.N * p.grad_stride * 2;
+    if (out.weight) {
+        HeadPackArgs h = {};
+        h.x = c.hidden;
+        h.stride = c.hidden_stride;
+        h.rows = c.N;
+        h.cols = c.D;
+        h.cols_p = p.width;
+        h.out = c.ws + p.weighted;
+        h.plane = packed_plane;
+        h.sc = scalars(c);
+        h.targets = c.targets;
+        h.grad_loss = grad_loss;
+        h.vocab = c.V;
+        if (!by_dtype(c.dtype, [&](auto dt) {
+                return launch(k_head_pack<decltype(dt)::value>, ceil_div((long long)c.N * (p.width / 8), 256), 256, c.st, h);
+            }))
+            return false;
+    }
+    for (int v0 = 0; v0 < c.V; v0 += p.piece) {
+        const int count = c.V - v0 < p.piece ? c.V - v0 : p.piece;
+        HeadArgs a;
+        if (!piece_args(c, p, v0, count, &a)) return false;
+        a.lse = lse;
+        a.grad = c.ws + p.grad;
+        a.grad_stride = p.grad_stride;
+        a.grad_plane = grad_plane;
+        const Operand grad = {c.ws + p.grad, p.grad_stride * 2, grad_plane};
+        const bool ok = by_product(c.dtype, [&](auto type, auto terms_, auto dt) {
+            using T = decltype(type);
+            constexpr int TERMS = decltype(terms_)::value, DT = decltype(dt)::value;
+            return by_rows(c.N, [&](auto shape) {
+                using S = decltype(shape);
+                a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
+                if (!launch(k_head_softmax<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a)) return false;
+                if (out.hidden) {
+                    HeadHiddenArgs g = {};
+                    g.weight = a.weight;
+                    g.grad = grad;
+                    g.N = c.N;
+                    g.D = p.width;
+                    g.V = count;
+                    g.tiles = {ceil_div(p.width, S::BM), ceil_div(c.N, S::BN)};
+                    g.splits = ceil_div(count, p.per_split);
+                    g.per_split = p.per_split;
+                    g.first = v0 == 0;
+                    g.sum = reinterpret_cast<float *>(c.ws + p.sum);
+                    if (!launch(k_head_grad_hidden<T, S, TERMS>, (long long)g.tiles.m * g.tiles.n * g.splits, S::THREADS, c.st, g)) return false;
+                }
+                if (out.weight) {
+                    HeadWeightArgs g = {};
+                    g.hidden = {c.ws + p.weighted, (long long)p.width * 2, packed_plane};
+                    g.grad = grad;
+                    g.N = c.N;
+                    g.D = c.D;
+                    g.Dp = p.width;
+                    g.V = count;
+                    g.tiles = {ceil_div(p.width, S::BM), ceil_div(count, S::BN)};
+                    g.sc = scalars(c);
+                    g.out = static_cast<char *>(out.weight) + (long long)v0 * out.weight_stride * size;
+                    g.out_stride = out.weight_stride;
+                    if (!launch(k_head_grad_weight<T, S, TERMS, DT>, (long long)g.tiles.m * g.tiles.n, S::THREADS, c.st, g)) return false;
+                }
+                return true;
+            });
+        });
+        if (!ok) return false;
+    }
+    if (!out.hidden) return true;
+    const int splits = ceil_div(c.V < p.piece ? c.V : p.piece, p.per_split);           // (of the first piece: those that were written)
+    HeadHiddenFinishArgs f = {reinterpret_cast<const float *>(c.ws + p.sum), splits, c.N, c.D, p.width, scalars(c), c.targets, grad_loss, c.V, out.hidden,
+                              out.hidden_stride};
+    return by_dtype(c.dtype, [&](auto dt) {
+        return launch(k_head_hidden_finish<decltype(dt)::value>, ceil_div((long long)c.N * c.D / 4, 256), 256, c.st, f);
+    });
+}
+
+}  // namespace svip
+
+// ---- C ABI -------------------------------------------------------------------------------------------------------------------------------------------
+
+using namespace svip;
+
+size_t svip_head_workspace_bytes(int call, int dtype, int N, int V, int D)
+{
+    if (call < SVIP_HEAD_LOGITS || call > SVIP_HEAD_LOSS_GRAD || !dtype_ok(dtype) || check_sizes(N, V, D)) return 0;
+    return plan(call, dtype, N, V, D).bytes;
+}
+
+svip_status svip_quantize_blocks(const void *x, int dtype, int rows, int cols, long long row_stride, int block_rows, void *q_out,
+                                 long long q_stride, void *scale_out, long long scale_stride, void *hip_stream)
+{
+    if (!x || !q_out || !scale_out) return SVIP_ERR_NULL;
+    if (!dtype_ok(dtype)) return SVIP_ERR_DTYPE;
+    if (rows <= 0 || rows > HEAD_MAX_VOCAB || cols <= 0 || cols > HEAD_MAX_WIDTH || row_stride < cols) return SVIP_ERR_SHAPE;
+    const int kb = ceil_div(cols, QBLOCK);
+    if (q_stride < (long long)kb * QBLOCK || scale_stride < kb) return SVIP_ERR_SHAPE;
+    if (!aligned16(x) || row_stride * size_of(dtype) % 16 != 0 || !aligned16(q_out) || q_stride % 16 != 0) return SVIP_ERR_ALIGN;
+    if (block_rows != 1 && block_rows != QBLOCK) return SVIP_ERR_PARAM;
+    QuantizeArgs a = {x, row_stride, rows, cols, kb, static_cast<unsigned char *>(q_out), q_stride, static_cast<unsigned char *>(scale_out), scale_stride};
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const bool ok = by_dtype(dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (block_rows == 1) return launch(k_quantize_rows<DT>, ceil_div((long long)rows * kb, QUANT_WG * Stored<DT>::VEC / QBLOCK), QUANT_WG, st, a);
+        return launch(k_quantize_blocks<DT>, (long long)ceil_div(rows, QBLOCK) * kb, QUANT_WG, st, a);
+    });
+    return ok ? SVIP_OK : SVIP_ERR_HIP;
+}
+
+svip_status svip_head_logits(const void *hidden_q, const void *hidden_scale, const void *weight_q, const void *weight_scale, int N, int V, int K,
+                             long long hidden_stride, long long hidden_scale_stride, long long weight_stride, long long weight_scale_stride,
+                             void *logits_out, int dtype, long long row_stride, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!hidden_q || !hidden_scale || !weight_q || !weight_scale || !logits_out) return SVIP_ERR_NULL;
+    if (!dtype_ok(dtype)) return SVIP_ERR_DTYPE;
+    if (svip_status s = check_sizes(N, V, K)) return s;
+    if (K % QBLOCK != 0 || hidden_scale_stride < K / QBLOCK || weight_scale_stride < K / QBLOCK || row_stride < V) return SVIP_ERR_SHAPE;
+    if (hidden_stride < K || hidden_stride > 2 * HEAD_MAX_STRIDE || weight_stride < K || weight_stride > 2 * HEAD_MAX_STRIDE) return SVIP_ERR_SHAPE;
+    if (!aligned16(hidden_q) || !aligned16(weight_q) || !aligned16(logits_out) || hidden_stride % 16 != 0 || weight_stride % 16 != 0 ||
+        row_stride * size_of(dtype) % 16 != 0)
+        return SVIP_ERR_ALIGN;
+    if (svip_status s = check_workspace(workspace, workspace_bytes, plan(SVIP_HEAD_LOGITS, dtype, N, V, K).bytes)) return s;
+    HeadLogitsArgs a = {};
+    a.weight = {static_cast<const char *>(weight_q), weight_stride, 0};
+    a.hidden = {static_cast<const char *>(hidden_q), hidden_stride, 0};
+    a.weight_scale = static_cast<const unsigned char *>(weight_scale);
+    a.hidden_scale = static_cast<const unsigned char *>(hidden_scale);
+    a.weight_scale_stride = weight_scale_stride;
+    a.hidden_scale_stride = hidden_scale_stride;
+    a.N = N;
+    a.V = V;
+    a.K = K;
+    a.out = logits_out;
+    a.out_stride = row_stride;
+    const bool ok = by_dtype(dtype, [&](auto dt) {
+        return by_rows(N, [&](auto shape) {
+            using S = std::conditional_t<decltype(dt)::value == SVIP_F32 && std::is_same<decltype(shape), Large>::value, Middle, decltype(shape)>;
+            a.tiles = {ceil_div(V, S::BM), ceil_div(N, S::BN)};
+            return launch(k_head_logits<S, decltype(dt)::value>, (long long)a.tiles.m * a.tiles.n, S::THREADS, static_cast<hipStream_t>(hip_stream), a);
+        });
+    });
+    return ok ? SVIP_OK : SVIP_ERR_HIP;
+}
+
+svip_status svip_head_loss(const void *hidden, const void *weight, int dtype, int N, int V, int D, long long hidden_stride, long long weight_stride,
+                           float temperature, const int *targets, float *loss_out, float *lse_out, void *workspace, size_t workspace_bytes,
+                           void *hip_stream)
+{
+    const LossCall c = {hidden, weight, dtype, N, V, D, hidden_stride, weight_stride, temperature, targets, static_cast<char *>(workspace),
+                        static_cast<hipStream_t>(hip_stream)};
+    if (!lse_out) return SVIP_ERR_NULL;
+    if (svip_status s = check_loss(c, loss_out, SVIP_HEAD_LOSS, workspace_bytes)) return s;
+    return run_loss(c, plan(SVIP_HEAD_LOSS, dtype, N, V, D), loss_out, lse_out) ? SVIP_OK : SVIP_ERR_HIP;
+}
+
+svip_status svip_head_loss_grad(const void *hidden, const void *weight, int dtype, int N, int V, int D, long long hidden_stride,
+                                long long weight_stride, float temperature, const int *targets, const float *lse, const float *grad_loss,
+                                void *grad_hidden_out, long long grad_hidden_stride, void *grad_weight_out, long long grad_weight_stride,
+                                void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const LossCall c = {hidden, weight, dtype, N, V, D, hidden_stride, weight_stride, temperature, targets, static_cast<char *>(workspace),
+                        static_cast<hipStream_t>(hip_stream)};
+    if (!lse || !grad_loss) return SVIP_ERR_NULL;
+    if (svip_status s = check_loss(c, grad_hidden_out ? grad_hidden_out : grad_weight_out, SVIP_HEAD_LOSS_GRAD, workspace_bytes)) return s;
+    if (grad_hidden_out)
+        if (svip_status s = check_matrix(grad_hidden_out, dtype, D, grad_hidden_stride)) return s;
+    if (grad_weight_out)
+        if (svip_status s = check_matrix(grad_weight_out, dtype, D, grad_weight_stride)) return s;
+    const GradOut out = {grad_hidden_out, grad_weight_out, grad_hidden_stride, grad_weight_stride};
+    return run_grad(c, plan(SVIP_HEAD_LOSS_GRAD, dtype, N, V, D), lse, grad_loss, out) ? SVIP_OK : SVIP_ERR_HIP;
+}
