@@ -224,10 +224,10 @@ __device__ __forceinline__ s16x8 codes_to_bf16(int lo, int hi)
     return __builtin_bit_cast(s16x8, v);
 }
 template <typename S, int DT>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_logits(HeadLogitsArgs a)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_logits(HeadLogitsArgs a)
 {
     constexpr int WEIGHT_BLOCKS = (S::BM + QBLOCK - 1) / QBLOCK;
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
     __shared__ unsigned char hs[S::BN * SCALE_PITCH], ws[WEIGHT_BLOCKS * SCALE_PITCH];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
@@ -368,9 +368,9 @@ __device__ __forceinline__ bool counts(int target, int vocab) { return target >=
 
 // Statistics of a tile of logits: per row the largest and the sum of exponentials over the tile's tokens.
 template <typename T, typename S, int TERMS>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_stats(HeadArgs a)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_stats(HeadArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
     const int v0 = tm * S::BM, n0 = tn * S::BN;
@@ -497,9 +497,9 @@ template <> struct GradOf<F16> {
 };
 
 template <typename T, typename S, int TERMS>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_softmax(HeadArgs a)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_softmax(HeadArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
     const int v0 = tm * S::BM, n0 = tn * S::BN;
@@ -551,9 +551,9 @@ struct HeadHiddenArgs {
 };
 // Gradient of the hidden states: G' W over the tokens of a piece, added to what the pieces before it gave.
 template <typename T, typename S, int TERMS>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_grad_hidden(HeadHiddenArgs a)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_grad_hidden(HeadHiddenArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
     const unsigned tiles = (unsigned)a.tiles.m * (unsigned)a.tiles.n, split = blockIdx.x / tiles;
     int tm, tn;
     tile_of(blockIdx.x - split * tiles, a.tiles, 4, tm, tn);
@@ -616,9 +616,9 @@ struct HeadWeightArgs {
 };
 // Gradient of the weight: G'^T (H grad_loss / grad_top).
 template <typename T, typename S, int TERMS, int DT>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_head_grad_weight(HeadWeightArgs a)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_grad_weight(HeadWeightArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
     const int d0 = tm * S::BM, v0 = tn * S::BN;

@@ -4,8 +4,8 @@
 //
 // A workgroup of WAVES_M x WAVES_N waves makes a BM x BN tile of C; a wave holds its (BM / WAVES_M) x (BN / WAVES_N) part as
 // 16 x 16 fragments in registers.  K goes by in steps of 128 bytes (64 16-bit values or 128 8-bit ones) that are copied from memory
-// straight into LDS (global_load_lds_dwordx4, no registers on the way), STAGES deep: while the waves multiply one step, the next
-// STAGES - 1 are on their way, and one barrier per step both publishes a step and frees the oldest buffer.
+// straight into LDS (global_load_lds_dwordx4, no registers on the way), STAGES deep, with one barrier per step, which both
+// publishes a step and frees the buffer of the one before.
 //
 // An operand comes in one of two layouts:
 //   KC  k contiguous (rows of m or n): the LDS tile is [rows][128 bytes]; a fragment is read with ds_read_b128.  16-byte chunk c of
@@ -20,6 +20,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 namespace svip {
 
@@ -94,24 +96,31 @@ struct Stager {
     }
     __device__ static int twist(int k) { return (((k & 3) << 1) | (k & 8)) & (PER_ROW - 1); }
 
-    // Step at `k` (element index, a multiple of the step) of plane `plane` into the buffer at `at`; k_end: elements of K.
+    template <int ESIZE>
+    __device__ __forceinline__ const char *step_base(int k, int plane) const
+    {
+        return op.base + plane * op.plane + (LAYOUT == KC ? (long long)k * ESIZE : k * op.stride);
+    }
+    // Round r of the copy of the step at `k` (element index, a multiple of the step), whose base is `base`, into the buffer at `at`; k_end:
+    // elements of K.
+    template <int ESIZE>
+    __device__ __forceinline__ void copy_round(int r, const char *base, unsigned at, int k, int k_end) const
+    {
+        if (k + STEP_BYTES / ESIZE <= k_end) {
+            copy_to_lds(base, voff[r], at + lds[r]);
+        } else {
+            const int c = (r * THREADS + (int)threadIdx.x) % CHUNKS;
+            const int mine = LAYOUT == KC ? k + ((c & 7) ^ ((c >> 4) & 7)) * (16 / ESIZE) : k + c / PER_ROW;
+            copy_to_lds(mine < k_end ? base + voff[r] : reinterpret_cast<const char *>(zero_line), at + lds[r]);
+        }
+    }
+    __device__ __forceinline__ void copy_whole_round(int r, const char *base, unsigned at) const { copy_to_lds(base, voff[r], at + lds[r]); }
     template <int ESIZE>
     __device__ __forceinline__ void copy(unsigned at, int k, int k_end, int plane) const
     {
-        constexpr int STEP = STEP_BYTES / ESIZE;
-        const char *base = op.base + plane * op.plane + (LAYOUT == KC ? (long long)k * ESIZE : k * op.stride);
-        if (k + STEP <= k_end) {
+        const char *base = step_base<ESIZE>(k, plane);
 #pragma unroll
-            for (int r = 0; r < ROUNDS; ++r) copy_to_lds(base, voff[r], at + lds[r]);
-        } else {
-#pragma unroll
-            for (int r = 0; r < ROUNDS; ++r) {
-                const int c = (r * THREADS + (int)threadIdx.x) % CHUNKS;
-                const int mine = LAYOUT == KC ? k + ((c & 7) ^ ((c >> 4) & 7)) * (16 / ESIZE) : k + c / PER_ROW;
-                const char *p = mine < k_end ? base + voff[r] : reinterpret_cast<const char *>(zero_line);
-                copy_to_lds(p, at + lds[r]);
-            }
-        }
+        for (int r = 0; r < ROUNDS; ++r) copy_round<ESIZE>(r, base, at, k, k_end);
     }
 };
 
@@ -169,6 +178,8 @@ struct TileShape {
     static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FM = WM / 16, FN = WN / 16;
     static constexpr int STAGE_BYTES = (BM + BN) * STEP_BYTES;
     static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
+    static constexpr int LDS_ALL = LDS_BYTES;
+    static constexpr int WAVES_PER_EU = FM * FN > 32 ? 1 : 2;          // (registers for one wave, or two)
     static_assert(WM % 16 == 0 && WN % 16 == 0, "whole fragments");
 };
 
@@ -196,36 +207,112 @@ __device__ __forceinline__ void multiply16(const Operand &a, int a_rows, const O
     constexpr int STEP = STEP_BYTES / 2, COPIES = decltype(sa)::ROUNDS + decltype(sb)::ROUNDS;
     const int per_term = (k_end - k0 + STEP - 1) / STEP, steps = TERMS * per_term;
     const unsigned lds0 = (unsigned)(uintptr_t)smem;
-    auto copy = [&](int s) {
+    // The copy of a step in COPIES parts.
+    struct {
+        const char *a, *b;
+        unsigned at;
+        int k;
+    } next = {};
+    auto aim = [&](int s, int buffer) {
         const int term = TERMS == 1 ? 0 : s / per_term;
-        const int k = k0 + (s - term * per_term) * STEP;
-        const unsigned at = lds0 + (unsigned)(s % S::STAGES) * S::STAGE_BYTES;
-        sa.template copy<2>(at, k, k_end, TERMS == 1 ? 0 : (term == 0));       // plane 0: high, 1: low
-        sb.template copy<2>(at + S::BM * STEP_BYTES, k, k_end, TERMS == 1 ? 0 : (term == 1));
+        next.k = k0 + (s - term * per_term) * STEP;
+        next.at = lds0 + (unsigned)buffer * S::STAGE_BYTES;
+        next.a = sa.template step_base<2>(next.k, TERMS == 1 ? 0 : (term == 0));       // plane 0: high, 1: low
+        next.b = sb.template step_base<2>(next.k, TERMS == 1 ? 0 : (term == 1));
+    };
+    auto copy_part = [&](int p, auto whole) {
+        constexpr int A = decltype(sa)::ROUNDS;
+        if constexpr (decltype(whole)::value) {
+            if (p < A)
+                sa.copy_whole_round(p, next.a, next.at);
+            else
+                sb.copy_whole_round(p - A, next.b, next.at + S::BM * STEP_BYTES);
+        } else {
+            if (p < A)
+                sa.template copy_round<2>(p, next.a, next.at, next.k, k_end);
+            else
+                sb.template copy_round<2>(p - A, next.b, next.at + S::BM * STEP_BYTES, next.k, k_end);
+        }
+    };
+    auto copy = [&](int s, int buffer) {
+        aim(s, buffer);
+#pragma unroll
+        for (int p = 0; p < COPIES; ++p) copy_part(p, std::false_type{});
+    };
+    // Step s is multiplied in two halves of K.  Its second half is read into registers while the first is multiplied, the next step's first
+    // half while the second is: a row's fragment of A is replaced as soon as the row's products are under way.  Between the two, when every
+    // wave has all of step s in registers, one barrier: the next step has landed, and the buffer of this one is copied over.  The
+    // barrier comes LAG rows into the second half, which cover the last reads of it.  The copy that it allows is issued in parts, one or two
+    // to a row: all at once they would fill the queue of the address unit (16 cycles each) and hold up the wave's products.
+    constexpr int LAG = S::FM / 4;
+    s16x8 fa[S::FM], fb[2][S::FN];
+    const char *tile = smem;
+    auto read_a = [&](int i, int h) { fa[i] = ra.half(tile, wm + 16 * i, h); };
+    auto read_b = [&](int h) {
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) fb[h][j] = rb.half(tile + S::BM * STEP_BYTES, wn + 16 * j, h);
+    };
+    auto row = [&](int i, int h) {
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) acc[i][j] = T::mfma(fa[i], fb[h][j], acc[i][j]);
     };
 #pragma unroll
-    for (int s = 0; s < S::STAGES - 1; ++s)
-        if (s < steps) copy(s);
-    for (int s = 0; s < steps; ++s) {
-        if (s + S::STAGES - 2 < steps)
+    for (int s = 0; s < S::STAGES; ++s)
+        if (s < steps) copy(s, s);
+    if (steps >= S::STAGES)
+        wait_copies_and_meet<(S::STAGES - 1) * COPIES>();
+    else
+        wait_copies_and_meet<0>();
+    read_b(0);
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i) read_a(i, 0);
+    int buffer = 0;
+    constexpr int PER_ROW = (COPIES + S::FM - 1) / S::FM, FIRST_ROWS = S::FM - LAG;
+    bool more = false;
+    int s = 0;
+    // MAIN: a step behind which a whole one is copied; what its first rows carry is the rest of the copy begun in the step before it, also whole.
+    auto step = [&](auto main) {
+        constexpr bool MAIN = decltype(main)::value;
+        read_b(1);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            row(i, 0);
+            read_a(i, 1);
+#pragma unroll
+            for (int p = (FIRST_ROWS + i) * PER_ROW; p < (FIRST_ROWS + i + 1) * PER_ROW; ++p)
+                if (p < COPIES && (MAIN || more)) copy_part(p, main);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < LAG; ++i) row(i, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (MAIN || s + S::STAGES <= steps)
             wait_copies_and_meet<(S::STAGES - 2) * COPIES>();
         else
             wait_copies_and_meet<0>();
-        if (s + S::STAGES - 1 < steps) copy(s + S::STAGES - 1);
-        const char *ta = smem + (s % S::STAGES) * S::STAGE_BYTES, *tb = ta + S::BM * STEP_BYTES;
+        more = MAIN || s + S::STAGES < steps;
+        if (more) aim(s + S::STAGES, buffer);
+        buffer = buffer + 1 == S::STAGES ? 0 : buffer + 1;
+        tile = smem + buffer * S::STAGE_BYTES;
+        read_b(0);                         // (after the last step: of what the buffer held before, and not used)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            s16x8 fa[S::FM], fb[S::FN];
+        for (int i = LAG; i < S::FM; ++i) {
+            row(i, 1);
+            read_a(i - LAG, 0);
 #pragma unroll
-            for (int j = 0; j < S::FN; ++j) fb[j] = rb.half(tb, wn + 16 * j, h);
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i) fa[i] = ra.half(ta, wm + 16 * i, h);
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FN; ++j) acc[i][j] = T::mfma(fa[i], fb[j], acc[i][j]);
+            for (int p = (i - LAG) * PER_ROW; p < (i - LAG + 1) * PER_ROW; ++p)
+                if (p < COPIES && (MAIN || more)) copy_part(p, main);
+            __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int i = S::FM - LAG; i < S::FM; ++i) read_a(i, 0);
+    };
+    if (steps > 0) step(std::false_type{}), ++s;
+    if (TERMS == 1 || (k_end - k0) % STEP == 0) {
+        const int last = k0 + (steps - 1) * STEP + STEP <= k_end || TERMS != 1 ? steps : steps - 1;      // whole steps end here
+        for (; s + S::STAGES < last; ++s) step(std::true_type{});
     }
+    for (; s < steps; ++s) step(std::false_type{});
 }
 
 }  // namespace svip

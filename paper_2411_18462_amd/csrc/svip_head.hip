@@ -46,7 +46,10 @@ static bool by_dtype(int d, F f)
 
 // ---- shapes of the tiles -------------------------------------------------------------------------------------------------------------------
 
-using Large = TileShape<256, 256, 2, 4, 2>;
+#ifndef HEAD_LARGE
+#define HEAD_LARGE 256, 256, 2, 4, 2
+#endif
+using Large = TileShape<HEAD_LARGE>;
 using Middle = TileShape<128, 128, 2, 2, 3>;           // (fp32 logits of 8-bit matrices: the tile's bf16 fragments need the registers)
 using Small = TileShape<128, 64, 4, 1, 3>;
 
