@@ -227,7 +227,7 @@ template <typename S, int DT>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_logits(HeadLogitsArgs a)
 {
     constexpr int WEIGHT_BLOCKS = (S::BM + QBLOCK - 1) / QBLOCK;
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
     __shared__ unsigned char hs[S::BN * SCALE_PITCH], ws[WEIGHT_BLOCKS * SCALE_PITCH];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
@@ -235,15 +235,15 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     Operand w = a.weight, h = a.hidden;
     w.base += (long long)v0 * w.stride;
     h.base += (long long)n0 * h.stride;
-    Stager<KC, S::BM, S::THREADS> sa;
-    Stager<KC, S::BN, S::THREADS> sb;
+    Stager<KC, S::BM, S::THREADS, 1> sa;
+    Stager<KC, S::BN, S::THREADS, 1> sb;
     sa.init(w, a.V - v0);
     sb.init(h, a.N - n0);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
     static_assert(QBLOCK % S::WM == 0, "a wave's rows of the weight share a scale");
-    Reader<KC, S::BM> ra;
-    Reader<KC, S::BN> rb;
+    Reader<KC, S::BM, 1> ra;
+    Reader<KC, S::BN, 1> rb;
     ra.init(lane);
     rb.init(lane);
     f32x4 acc[S::FM][S::FN];
@@ -257,8 +257,8 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     const unsigned lds0 = (unsigned)(uintptr_t)smem;
     auto copy = [&](int s) {
         const unsigned at = lds0 + (unsigned)(s % S::STAGES) * S::STAGE_BYTES;
-        sa.template copy<1>(at, s * QBLOCK, a.K, 0);
-        sb.template copy<1>(at + S::BM * STEP_BYTES, s * QBLOCK, a.K, 0);
+        sa.copy(at, s * QBLOCK, a.K, 0);
+        sb.copy(at + S::BM * STEP_BYTES, s * QBLOCK, a.K, 0);
     };
     auto scales = [&](int s0) {
         const int count = steps - s0 < SCALE_STEPS ? steps - s0 : SCALE_STEPS;
@@ -352,12 +352,13 @@ struct HeadArgs {
     int v0;                    // the piece's first token
     Tiles tiles;
     const HeadScalars *sc;
+    float to_log2;             // where the products are of the values themselves: logits_scale()
     const float *row_inv;      // fp32 [N]: one over what a row's parts are multiplied by
     const int *targets;
     float2 *part;              // [tiles of the vocabulary][N] (largest, sum of exp2 relative to it), base 2
     float *target_logit;       // [N] logits / T of the targets, base 2
     const float *lse;          // [N]
-    char *grad;                // [planes][N][grad_stride] 16-bit: softmax - one-hot of the piece
+    char *grad;                // [planes][N][grad_stride]: softmax - one-hot of the piece
     long long grad_stride;     // elements
     long long grad_plane;      // bytes
     int vocab;                 // tokens in all
@@ -366,11 +367,27 @@ struct HeadArgs {
 
 __device__ __forceinline__ bool counts(int target, int vocab) { return target >= 0 && target < vocab; }
 
+// Accumulated products -> logits / T in units of log 2 (parts: of a row's own scale besides).
+template <int TERMS>
+__device__ __forceinline__ float logits_scale(const HeadArgs &a)
+{
+    return TERMS == 3 ? a.sc->to_log2 : a.to_log2;
+}
+// The four 16-lane rows of a wave, lane by lane.
+template <typename Op>
+__device__ __forceinline__ float across_rows(float v, Op op)
+{
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(h[0]), __uint_as_float(h[1]));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // Statistics of a tile of logits: per row the largest and the sum of exponentials over the tile's tokens.
 template <typename T, typename S, int TERMS>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_stats(HeadArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
     const int v0 = tm * S::BM, n0 = tn * S::BN;
@@ -378,43 +395,62 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     w.base += (long long)v0 * w.stride;
     h.base += (long long)n0 * h.stride;
     f32x4 acc[S::FM][S::FN];
-    multiply16<T, S, KC, KC, TERMS>(w, a.V - v0, h, a.N - n0, 0, a.D, smem, acc);
+    multiply<T, S, KC, KC, TERMS>(w, a.V - v0, h, a.N - n0, 0, a.D, smem, acc);
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
-    const float to_log2 = a.sc->to_log2;
-    const bool whole = v0 + S::BM <= a.V;
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN, first = v0 + wm + 4 * (lane >> 4);
+    const float to_log2 = logits_scale<TERMS>(a);
+    float c[S::FN], top[S::FN], sum[S::FN];
+    int t[S::FN];                          // where a row's target is among this lane's tokens: 16 i + e
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = n0 + wn + 16 * j + (lane & 15), m = n < a.N ? n : a.N - 1;
+        t[j] = n < a.N ? a.targets[m] - a.v0 - first : -1;
+        c[j] = TERMS == 3 ? to_log2 * a.row_inv[m] : to_log2;
+    }
+    if (v0 + S::BM > a.V) {                // the last tile: nothing behind the vocabulary
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (first + 16 * i + e >= a.V)
+#pragma unroll
+                    for (int j = 0; j < S::FN; ++j) acc[i][j][e] = -INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        top[j] = acc[0][j][0];
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top[j] = fmaxf(top[j], acc[i][j][e]);
+        if ((unsigned)t[j] < (unsigned)S::WM && (t[j] & 12) == 0) {
+            float z = 0.f;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z = t[j] == 16 * i + e ? acc[i][j][e] : z;
+            if (first + t[j] < a.V) a.target_logit[n0 + wn + 16 * j + (lane & 15)] = z * c[j];
+        }
+    }
+    // (c is positive: the largest product is the largest logit)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) top[j] = across_rows(top[j], OpMax{}) * c[j];
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const float base = top[j] == -INFINITY ? 0.f : top[j];
+        sum[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], c[j], -base));
+    }
     __syncthreads();
     float2 *red = reinterpret_cast<float2 *>(smem);        // [WAVES_M][BN]
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
-        const int n = n0 + wn + 16 * j + (lane & 15);
-        const int t = n < a.N ? a.targets[n] - a.v0 : -1;
-        const int first = v0 + wm + 4 * (lane >> 4);
-        const float c = TERMS == 3 && n < a.N ? to_log2 * a.row_inv[n] : to_log2;
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float z = acc[i][j][e] * c;
-                const int v = first + 16 * i + e;
-                if (v == t && v < a.V) a.target_logit[n] = z;
-                if (!whole && v >= a.V) z = -INFINITY;
-                acc[i][j][e] = z;
-                top = fmaxf(top, z);
-            }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(acc[i][j][e] - base);
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (lane < 16) red[(wave % S::WAVES_M) * S::BN + wn + 16 * j + lane] = make_float2(top, sum);
+        sum[j] = across_rows(sum[j], OpSum{});
+        if (lane < 16) red[(wave % S::WAVES_M) * S::BN + wn + 16 * j + lane] = make_float2(top[j], sum[j]);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < S::BN && n0 + i < a.N; i += S::THREADS) {
@@ -437,41 +473,43 @@ struct HeadFinishArgs {
     float *loss, *lse;
     unsigned *flags;
 };
-// A row's records joined in 64 bits: 16 rows a workgroup, 16 threads a row.
-constexpr int FINISH_ROWS = 16, FINISH_WG = 256;
+// A row's records joined in 64 bits: 16 rows a workgroup, 16 threads a row, eight records of each at a time.
+constexpr int FINISH_ROWS = 16, FINISH_WG = 256, FINISH_BATCH = 8;
 __global__ __launch_bounds__(FINISH_WG) static void k_head_finish(HeadFinishArgs a)
 {
-    __shared__ float top[FINISH_WG];
+    __shared__ float tops[FINISH_WG];
     __shared__ double sums[FINISH_WG];
-    const int r = threadIdx.x % FINISH_ROWS, k = threadIdx.x / FINISH_ROWS, n = blockIdx.x * FINISH_ROWS + r;
+    const int r = threadIdx.x % FINISH_ROWS, k = threadIdx.x / FINISH_ROWS, row = blockIdx.x * FINISH_ROWS + r;
+    const int n = row < a.N ? row : a.N - 1;
     constexpr int SLICES = FINISH_WG / FINISH_ROWS;
-    float m = -INFINITY;
-    double s = 0.0;
-    if (n < a.N)
-        for (int i = k; i < a.records; i += SLICES) {
-            const float2 p = a.part[(long long)i * a.N + n];
-            if (p.x > m) {
-                s = s * (double)__builtin_amdgcn_exp2f(m - p.x) + (double)p.y;
-                m = p.x;
-            } else if (p.x == m || m == -INFINITY) {         // (also NaN first)
-                s += (double)p.y;
-                m = m == -INFINITY ? p.x : m;
-            } else {
-                s += (double)(p.y * __builtin_amdgcn_exp2f(p.x - m));
-            }
-        }
-    top[threadIdx.x] = m;
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    if (k != 0 || n >= a.N) return;
-    float best = m;
-    for (int i = 1; i < SLICES; ++i) best = fmaxf(best, top[i * FINISH_ROWS + r]);
+    float top = -INFINITY;
     double sum = 0.0;
-    for (int i = 0; i < SLICES; ++i) {
-        const float t = top[i * FINISH_ROWS + r];
-        if (t != -INFINITY) sum += sums[i * FINISH_ROWS + r] * (double)(t == best ? 1.f : __builtin_amdgcn_exp2f(t - best));
+    for (int i = k; i < a.records; i += SLICES * FINISH_BATCH) {
+        float2 p[FINISH_BATCH];
+#pragma unroll
+        for (int q = 0; q < FINISH_BATCH; ++q) {
+            const int at = i + q * SLICES;
+            p[q] = a.part[(long long)(at < a.records ? at : k) * a.N + n];
+            if (at >= a.records) p[q] = make_float2(-INFINITY, 0.f);
+        }
+        float m = top;
+#pragma unroll
+        for (int q = 0; q < FINISH_BATCH; ++q) m = fmaxf(m, p[q].x);
+        const float base = m == -INFINITY ? 0.f : m;
+        sum *= (double)__builtin_amdgcn_exp2f(top - base);
+#pragma unroll
+        for (int q = 0; q < FINISH_BATCH; ++q) sum += (double)(p[q].y * __builtin_amdgcn_exp2f(p[q].x - base));
+        top = m;
     }
-    const double lse2 = (double)best + log2(sum);
+    tops[threadIdx.x] = top;
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (k != 0 || row >= a.N) return;
+    for (int i = 1; i < SLICES; ++i) top = fmaxf(top, tops[i * FINISH_ROWS + r]);
+    const float base = top == -INFINITY ? 0.f : top;
+    sum = 0.0;
+    for (int i = 0; i < SLICES; ++i) sum += sums[i * FINISH_ROWS + r] * (double)__builtin_amdgcn_exp2f(tops[i * FINISH_ROWS + r] - base);
+    const double lse2 = (double)top + log2(sum);
     const int t = a.targets[n];
     const bool use = counts(t, a.vocab);
     if (t >= a.vocab) atomicOr(a.flags, (unsigned)SVIP_FLAG_BAD_TOKEN);
@@ -495,11 +533,15 @@ template <> struct GradOf<F16> {
     using type = _Float16;
     static constexpr float SCALE = GRAD_SCALE_F16;
 };
+template <> struct GradOf<F32> {
+    using type = float;
+    static constexpr float SCALE = 1.f;
+};
 
 template <typename T, typename S, int TERMS>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_softmax(HeadArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
     const int v0 = tm * S::BM, n0 = tn * S::BN;
@@ -507,7 +549,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     w.base += (long long)v0 * w.stride;
     h.base += (long long)n0 * h.stride;
     f32x4 acc[S::FM][S::FN];
-    multiply16<T, S, KC, KC, TERMS>(w, a.V - v0, h, a.N - n0, 0, a.D, smem, acc);
+    multiply<T, S, KC, KC, TERMS>(w, a.V - v0, h, a.N - n0, 0, a.D, smem, acc);
 
     using X = typename GradOf<T>::type;
     typedef X x4 __attribute__((ext_vector_type(4)));
@@ -517,11 +559,11 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     for (int j = 0; j < S::FN; ++j) {
         const int n = n0 + wn + 16 * j + (lane & 15);
         if (n >= a.N) continue;
-        const float c = TERMS == 3 ? a.sc->to_log2 * a.row_inv[n] : a.sc->to_log2;
-        const int t = a.targets[n];
-        const bool use = counts(t, a.vocab);
+        const float c = TERMS == 3 ? logits_scale<TERMS>(a) * a.row_inv[n] : logits_scale<TERMS>(a);
+        const int target = a.targets[n], first = v0 + wm + 4 * (lane >> 4), t = target - a.v0 - first;
+        const bool use = counts(target, a.vocab);
         const float base = a.lse[n] * HEAD_LOG2E;
-        char *row = a.grad + 2 * ((long long)n * a.grad_stride);
+        char *row = a.grad + T::SIZE * ((long long)n * a.grad_stride);
 #pragma unroll
         for (int i = 0; i < S::FM; ++i) {
             const int v = v0 + wm + 16 * i + 4 * (lane >> 4);
@@ -529,13 +571,13 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
             x4 g, low;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float p = __builtin_amdgcn_exp2f(acc[i][j][e] * c - base);
-                if (v + e == t - a.v0) p -= 1.f;
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], c, -base));
+                if (t == 16 * i + e) p -= 1.f;
                 p = use && v + e < a.V ? p * GradOf<T>::SCALE : 0.f;
                 g[e] = (X)p;
                 if (TERMS == 3) low[e] = (X)(p - (float)g[e]);
             }
-            *reinterpret_cast<x4 *>(row + 2 * v) = g;
+            *reinterpret_cast<x4 *>(row + T::SIZE * v) = g;
             if (TERMS == 3) *reinterpret_cast<x4 *>(row + a.grad_plane + 2 * v) = low;
         }
     }
@@ -553,16 +595,16 @@ struct HeadHiddenArgs {
 template <typename T, typename S, int TERMS>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_grad_hidden(HeadHiddenArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
     const unsigned tiles = (unsigned)a.tiles.m * (unsigned)a.tiles.n, split = blockIdx.x / tiles;
     int tm, tn;
     tile_of(blockIdx.x - split * tiles, a.tiles, 4, tm, tn);
     const int d0 = tm * S::BM, n0 = tn * S::BN, k0 = (int)split * a.per_split, k_end = min(a.V, k0 + a.per_split);
     Operand w = a.weight, g = a.grad;
-    w.base += 2 * d0;
+    w.base += T::SIZE * d0;
     g.base += (long long)n0 * g.stride;
     f32x4 acc[S::FM][S::FN];
-    multiply16<T, S, KS, KC, TERMS>(w, a.D - d0, g, a.N - n0, k0, k_end, smem, acc);
+    multiply<T, S, KS, KC, TERMS>(w, a.D - d0, g, a.N - n0, k0, k_end, smem, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
     float *sum = a.sum + (long long)split * a.N * a.D;
@@ -618,15 +660,15 @@ struct HeadWeightArgs {
 template <typename T, typename S, int TERMS, int DT>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_grad_weight(HeadWeightArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_ALL];
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
     const int d0 = tm * S::BM, v0 = tn * S::BN;
     Operand h = a.hidden, g = a.grad;
-    h.base += 2 * d0;
-    g.base += 2 * v0;
+    h.base += T::SIZE * d0;
+    g.base += T::SIZE * v0;
     f32x4 acc[S::FM][S::FN];
-    multiply16<T, S, KS, KS, TERMS>(h, a.Dp - d0, g, (int)(g.stride / 2) - v0, 0, a.N, smem, acc);
+    multiply<T, S, KS, KS, TERMS>(h, a.Dp - d0, g, (int)(g.stride / T::SIZE) - v0, 0, a.N, smem, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
     const float m = a.sc->weight_mult;
@@ -675,22 +717,23 @@ struct HeadMaxArgs {
     int vocab;
     unsigned *out;             // starts at 0
 };
-// Largest finite magnitude of a matrix (bits), joined by an integer maximum, whose order does not matter.
+// Largest finite magnitude of a matrix (bits), joined by an integer maximum, whose order does not matter.  A wave takes rows.
 __global__ __launch_bounds__(256) static void k_head_max(HeadMaxArgs a)
 {
-    const int per_row = a.cols / 4;
-    const long long total = (long long)a.rows * per_row;
+    const int lane = threadIdx.x & 63;
     unsigned m = 0u;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long r = i / per_row;
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += gridDim.x * 4) {
         if (a.targets && !counts(a.targets[r], a.vocab)) continue;
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.x + r * a.stride + (i - r * per_row) * 4);
+        const float *x = a.x + r * a.stride;
+        for (int c = lane * 4; c < a.cols; c += 256) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(x + c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) m = max(m, finite_magnitude(v[e]));
+            for (int e = 0; e < 4; ++e) m = max(m, finite_magnitude(v[e]));
+        }
     }
 #pragma unroll
     for (int o = 32; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
-    if ((threadIdx.x & 63) == 0 && m) atomicMax(a.out, m);
+    if (lane == 0 && m) atomicMax(a.out, m);
 }
 struct HeadClearArgs {
     HeadScalars *sc;
@@ -747,6 +790,7 @@ struct HeadPackArgs {
     const float *grad_loss;
     int vocab;
     float *row_inv;            // hidden states for the logits: parts of their own scale for each row
+    int whole;                 // fp32 as it is, no parts
 };
 template <int DT>
 __device__ __forceinline__ void load_columns(const HeadPackArgs &a, long long r, int c, float (&v)[8])
@@ -772,7 +816,11 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadPackArgs a)
         for (int e = 0; e < 8; ++e) v[e] = use ? v[e] * w : 0.f;
     }
     char *out = a.out + (r * a.cols_p + c) * 2;
-    if constexpr (DT == SVIP_F32) {
+    if (DT == SVIP_F32 && a.whole) {
+        float *p = reinterpret_cast<float *>(a.out) + r * a.cols_p + c;
+        *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4 *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    } else if constexpr (DT == SVIP_F32) {
         store_parts(out, a.plane, v, a.targets ? a.sc->hidden_parts : a.sc->weight_parts);
     } else {
         using X = typename Stored<DT>::type;

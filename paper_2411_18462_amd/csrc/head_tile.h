@@ -10,9 +10,10 @@
 // An operand comes in one of two layouts:
 //   KC  k contiguous (rows of m or n): the LDS tile is [rows][128 bytes]; a fragment is read with ds_read_b128.  16-byte chunk c of
 //       row r lies at chunk c ^ (r / 2 % 8), so that the 16 rows of a fragment, of which two span the 64 banks, meet no bank twice.
-//   KS  k strided (rows of k, 16-bit values): the LDS tile is [64][columns]; a fragment is read with ds_read_b64_tr_b16, which
-//       gives lane i of 16 the column i of a 4 x 16 block.  The four rows of a block would lie in the same banks: chunk c of
-//       row k lies at chunk c ^ (2 (k % 4) + 8 (k / 8 % 2)).
+//   KS  k strided (rows of k): the LDS tile is [k][columns].  A fragment of 16-bit values is read with ds_read_b64_tr_b16, which
+//       gives lane i of 16 the column i of a 4 x 16 block; the four rows of a block would lie in the same banks, so chunk c of
+//       row k lies at chunk c ^ (2 (k % 4) + 8 (k / 8 % 2)).  fp32 values are read one by one, 16 columns of rows k, k + 4, k + 8 and k + 12
+//       at a time: chunk c ^ 4 (k / 4 % 4).
 // The copy into LDS writes lane after lane, so the permutation is made by which chunk a lane asks for.
 //
 // Rows past the end of an operand are read as its last row (their results are not stored); positions past the end of K are read
@@ -65,19 +66,20 @@ __device__ __forceinline__ void wait_copies_and_meet()
 }
 
 // One operand's part of a workgroup's tile: ROWS rows (KC) or columns (KS).
-template <int LAYOUT, int ROWS, int THREADS>
+template <int LAYOUT, int ROWS, int THREADS, int ESIZE>
 struct Stager {
     static constexpr int CHUNKS = ROWS * STEP_BYTES / 16;
     static constexpr int ROUNDS = CHUNKS > THREADS ? CHUNKS / THREADS : 1;      // (fewer chunks than threads: some are copied twice)
     static constexpr int BYTES = ROWS * STEP_BYTES;
-    static constexpr int PER_ROW = ROWS / 8;                                   // KS: chunks in a row
+    static constexpr int STEP = STEP_BYTES / ESIZE, PER_CHUNK = 16 / ESIZE;   // elements
+    static constexpr int PER_ROW = ROWS / PER_CHUNK;                           // KS: chunks in a row
     static_assert(CHUNKS % 64 == 0 && (CHUNKS >= THREADS ? CHUNKS % THREADS == 0 : THREADS % CHUNKS == 0), "whole waves copy");
 
     Operand op;
     unsigned voff[ROUNDS];
     unsigned lds[ROUNDS];      // wave-uniform
 
-    // rows: of the operand from the tile's first on, at least 1 (KS: columns, a multiple of 8)
+    // rows: of the operand from the tile's first on, at least 1 (KS: columns, whole chunks)
     __device__ void init(const Operand &o, int rows)
     {
         op = o;
@@ -90,43 +92,40 @@ struct Stager {
                 voff[r] = (unsigned)(row < rows ? row : rows - 1) * (unsigned)op.stride + (unsigned)chunk * 16u;
             } else {
                 const int k = c / PER_ROW, chunk = (c % PER_ROW) ^ twist(k);
-                voff[r] = (unsigned)k * (unsigned)op.stride + (unsigned)(chunk < rows / 8 ? chunk : 0) * 16u;
+                voff[r] = (unsigned)k * (unsigned)op.stride + (unsigned)(chunk < rows / PER_CHUNK ? chunk : 0) * 16u;
             }
         }
     }
-    __device__ static int twist(int k) { return (((k & 3) << 1) | (k & 8)) & (PER_ROW - 1); }
+    __device__ static int twist(int k) { return (ESIZE == 4 ? k & 12 : ((k & 3) << 1) | (k & 8)) & (PER_ROW - 1); }
 
-    template <int ESIZE>
     __device__ __forceinline__ const char *step_base(int k, int plane) const
     {
         return op.base + plane * op.plane + (LAYOUT == KC ? (long long)k * ESIZE : k * op.stride);
     }
     // Round r of the copy of the step at `k` (element index, a multiple of the step), whose base is `base`, into the buffer at `at`; k_end:
     // elements of K.
-    template <int ESIZE>
     __device__ __forceinline__ void copy_round(int r, const char *base, unsigned at, int k, int k_end) const
     {
-        if (k + STEP_BYTES / ESIZE <= k_end) {
+        if (k + STEP <= k_end) {
             copy_to_lds(base, voff[r], at + lds[r]);
         } else {
             const int c = (r * THREADS + (int)threadIdx.x) % CHUNKS;
-            const int mine = LAYOUT == KC ? k + ((c & 7) ^ ((c >> 4) & 7)) * (16 / ESIZE) : k + c / PER_ROW;
+            const int mine = LAYOUT == KC ? k + ((c & 7) ^ ((c >> 4) & 7)) * PER_CHUNK : k + c / PER_ROW;
             copy_to_lds(mine < k_end ? base + voff[r] : reinterpret_cast<const char *>(zero_line), at + lds[r]);
         }
     }
     __device__ __forceinline__ void copy_whole_round(int r, const char *base, unsigned at) const { copy_to_lds(base, voff[r], at + lds[r]); }
-    template <int ESIZE>
     __device__ __forceinline__ void copy(unsigned at, int k, int k_end, int plane) const
     {
-        const char *base = step_base<ESIZE>(k, plane);
+        const char *base = step_base(k, plane);
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) copy_round<ESIZE>(r, base, at, k, k_end);
+        for (int r = 0; r < ROUNDS; ++r) copy_round(r, base, at, k, k_end);
     }
 };
 
-// Reads fragments of an operand's LDS tile: 16 rows of m or n from `row0` (a multiple of 16) and half a step of 16-bit values, or a whole step
-// of 8-bit ones.  Lane l has row l % 16; of K it has, for 16 bits, the 8 values from 8 (l / 16) on in half h.
-template <int LAYOUT, int ROWS>
+// Reads fragments of an operand's LDS tile: 16 rows of m or n from `row0` (a multiple of 16) and half a step, or a whole step of 8-bit values.
+// Lane l has row l % 16; of K it has, for 16 bits, the 8 values from 8 (l / 16) on in half h, for fp32 the 4 from 4 (l / 16) on.
+template <int LAYOUT, int ROWS, int ESIZE>
 struct Reader {
     unsigned at[2];
     __device__ void init(int lane)
@@ -135,20 +134,36 @@ struct Reader {
         if (LAYOUT == KC) {
             at[0] = (unsigned)(row * STEP_BYTES + (((g) ^ (row >> 1)) & 7) * 16);
             at[1] = (unsigned)(row * STEP_BYTES + (((4 + g) ^ (row >> 1)) & 7) * 16);
-        } else {
+        } else if (ESIZE == 2) {
             const int k = 8 * g + (row >> 2);
             at[0] = (unsigned)(k * ROWS * 2 + (row & 1) * 8);
-            at[1] = (unsigned)((((row & 3) >> 1)) ^ Stager<KS, ROWS, 64>::twist(k));
+            at[1] = (unsigned)((((row & 3) >> 1)) ^ Stager<KS, ROWS, 64, 2>::twist(k));
+        } else {
+            at[0] = (unsigned)(4 * g * ROWS * 4 + (row & 3) * 4);
+            at[1] = (unsigned)((row >> 2) ^ Stager<KS, ROWS, 64, 4>::twist(4 * g));
         }
     }
-    __device__ __forceinline__ s16x8 half(const char *tile, int row0, int h) const
+    __device__ __forceinline__ void half(const char *tile, int row0, int h, s16x8 &f) const
     {
-        if (LAYOUT == KC) return *reinterpret_cast<const s16x8 *>(tile + at[h] + row0 * STEP_BYTES);
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const unsigned a = at[0] + (((unsigned)(row0 / 8)) ^ at[1]) * 16u;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + a + (32 * h) * ROWS * 2));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + a + (32 * h + 4) * ROWS * 2));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        if (LAYOUT == KC) {
+            f = *reinterpret_cast<const s16x8 *>(tile + at[h] + row0 * STEP_BYTES);
+        } else {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const unsigned a = at[0] + (((unsigned)(row0 / 8)) ^ at[1]) * 16u;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + a + (32 * h) * ROWS * 2));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + a + (32 * h + 4) * ROWS * 2));
+            f = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    __device__ __forceinline__ void half(const char *tile, int row0, int h, f32x4 &f) const
+    {
+        if (LAYOUT == KC) {
+            f = *reinterpret_cast<const f32x4 *>(tile + at[h] + row0 * STEP_BYTES);
+        } else {
+            const char *p = tile + at[0] + (((unsigned)(row0 / 4)) ^ at[1]) * 16u;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) f[q] = *reinterpret_cast<const float *>(p + (16 * h + q) * ROWS * 4);
+        }
     }
     __device__ __forceinline__ i32x8 whole(const char *tile, int row0) const
     {
@@ -158,16 +173,31 @@ struct Reader {
     }
 };
 
+// What the products are made of.
 struct Bf16 {
+    using Frag = s16x8;
+    static constexpr int SIZE = 2;
     __device__ static __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
 };
 struct F16 {
+    using Frag = s16x8;
+    static constexpr int SIZE = 2;
     __device__ static __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+struct F32 {
+    using Frag = f32x4;
+    static constexpr int SIZE = 4;
+    __device__ static __forceinline__ f32x4 mfma(f32x4 a, f32x4 b, f32x4 c)
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[q], b[q], c, 0, 0, 0);
+        return c;
     }
 };
 
@@ -178,25 +208,24 @@ struct TileShape {
     static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FM = WM / 16, FN = WN / 16;
     static constexpr int STAGE_BYTES = (BM + BN) * STEP_BYTES;
     static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
-    static constexpr int LDS_ALL = LDS_BYTES;
     static constexpr int WAVES_PER_EU = FM * FN > 32 ? 1 : 2;          // (registers for one wave, or two)
     static_assert(WM % 16 == 0 && WN % 16 == 0, "whole fragments");
 };
 
-// The loop over K of 16-bit operands.  TERMS = 1: one plane each.  TERMS = 3: two planes (high and low part) each, and the products
+// The loop over K.  TERMS = 1: one plane each.  TERMS = 3: two planes (high and low part) each, and the products
 // low x high, high x low and high x high, the small ones first.
 template <typename T, typename S, int LA, int LB, int TERMS>
-__device__ __forceinline__ void multiply16(const Operand &a, int a_rows, const Operand &b, int b_rows, int k0, int k_end, char *smem,
-                                           f32x4 (&acc)[S::FM][S::FN])
+__device__ __forceinline__ void multiply(const Operand &a, int a_rows, const Operand &b, int b_rows, int k0, int k_end, char *smem,
+                                         f32x4 (&acc)[S::FM][S::FN])
 {
-    Stager<LA, S::BM, S::THREADS> sa;
-    Stager<LB, S::BN, S::THREADS> sb;
+    Stager<LA, S::BM, S::THREADS, T::SIZE> sa;
+    Stager<LB, S::BN, S::THREADS, T::SIZE> sb;
     sa.init(a, a_rows);
     sb.init(b, b_rows);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
-    Reader<LA, S::BM> ra;
-    Reader<LB, S::BN> rb;
+    Reader<LA, S::BM, T::SIZE> ra;
+    Reader<LB, S::BN, T::SIZE> rb;
     ra.init(lane);
     rb.init(lane);
 #pragma unroll
@@ -204,7 +233,7 @@ __device__ __forceinline__ void multiply16(const Operand &a, int a_rows, const O
 #pragma unroll
         for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int STEP = STEP_BYTES / 2, COPIES = decltype(sa)::ROUNDS + decltype(sb)::ROUNDS;
+    constexpr int STEP = STEP_BYTES / T::SIZE, COPIES = decltype(sa)::ROUNDS + decltype(sb)::ROUNDS;
     const int per_term = (k_end - k0 + STEP - 1) / STEP, steps = TERMS * per_term;
     const unsigned lds0 = (unsigned)(uintptr_t)smem;
     // The copy of a step in COPIES parts.
@@ -217,8 +246,8 @@ __device__ __forceinline__ void multiply16(const Operand &a, int a_rows, const O
         const int term = TERMS == 1 ? 0 : s / per_term;
         next.k = k0 + (s - term * per_term) * STEP;
         next.at = lds0 + (unsigned)buffer * S::STAGE_BYTES;
-        next.a = sa.template step_base<2>(next.k, TERMS == 1 ? 0 : (term == 0));       // plane 0: high, 1: low
-        next.b = sb.template step_base<2>(next.k, TERMS == 1 ? 0 : (term == 1));
+        next.a = sa.step_base(next.k, TERMS == 1 ? 0 : (term == 0));       // plane 0: high, 1: low
+        next.b = sb.step_base(next.k, TERMS == 1 ? 0 : (term == 1));
     };
     auto copy_part = [&](int p, auto whole) {
         constexpr int A = decltype(sa)::ROUNDS;
@@ -229,9 +258,9 @@ __device__ __forceinline__ void multiply16(const Operand &a, int a_rows, const O
                 sb.copy_whole_round(p - A, next.b, next.at + S::BM * STEP_BYTES);
         } else {
             if (p < A)
-                sa.template copy_round<2>(p, next.a, next.at, next.k, k_end);
+                sa.copy_round(p, next.a, next.at, next.k, k_end);
             else
-                sb.template copy_round<2>(p - A, next.b, next.at + S::BM * STEP_BYTES, next.k, k_end);
+                sb.copy_round(p - A, next.b, next.at + S::BM * STEP_BYTES, next.k, k_end);
         }
     };
     auto copy = [&](int s, int buffer) {
@@ -245,12 +274,12 @@ __device__ __forceinline__ void multiply16(const Operand &a, int a_rows, const O
     // barrier comes LAG rows into the second half, which cover the last reads of it.  The copy that it allows is issued in parts, one or two
     // to a row: all at once they would fill the queue of the address unit (16 cycles each) and hold up the wave's products.
     constexpr int LAG = S::FM / 4;
-    s16x8 fa[S::FM], fb[2][S::FN];
+    typename T::Frag fa[S::FM], fb[2][S::FN];
     const char *tile = smem;
-    auto read_a = [&](int i, int h) { fa[i] = ra.half(tile, wm + 16 * i, h); };
+    auto read_a = [&](int i, int h) { ra.half(tile, wm + 16 * i, h, fa[i]); };
     auto read_b = [&](int h) {
 #pragma unroll
-        for (int j = 0; j < S::FN; ++j) fb[h][j] = rb.half(tile + S::BM * STEP_BYTES, wn + 16 * j, h);
+        for (int j = 0; j < S::FN; ++j) rb.half(tile + S::BM * STEP_BYTES, wn + 16 * j, h, fb[h][j]);
     };
     auto row = [&](int i, int h) {
 #pragma unroll

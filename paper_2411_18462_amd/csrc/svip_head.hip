@@ -53,21 +53,29 @@ using Large = TileShape<HEAD_LARGE>;
 using Middle = TileShape<128, 128, 2, 2, 3>;           // (fp32 logits of 8-bit matrices: the tile's bf16 fragments need the registers)
 using Small = TileShape<128, 64, 4, 1, 3>;
 
+// Up to 64 rows wait for the weight's bytes: a tile of all rows, small enough for two workgroups a CU.
+constexpr int FEW_ROWS = 64;
+
 // f with the shape for `rows` rows of hidden states (n of the tiles).
 template <typename F>
 static bool by_rows(int rows, F f)
 {
-    if (rows > 64) return f(Large{});
+    if (rows > FEW_ROWS) return f(Large{});
     return f(Small{});
 }
 
-// f with the products' type and terms of a dtype: fp32 values go as two fp16 parts.
+// f with what the products are made of, their terms and the dtype.  fp32 values of many rows go as two fp16 parts, at a third of the rate of 16-bit
+// values and three times that of fp32 products; of few rows as they are, since laying out a weight's parts would cost more than its products.
 template <typename F>
-static bool by_product(int dtype, F f)
+static bool by_product(int dtype, int rows, F f)
 {
-    if (dtype == SVIP_F32) return f(F16{}, std::integral_constant<int, 3>{}, std::integral_constant<int, SVIP_F32>{});
-    if (dtype == SVIP_BF16) return f(Bf16{}, std::integral_constant<int, 1>{}, std::integral_constant<int, SVIP_BF16>{});
-    return f(F16{}, std::integral_constant<int, 1>{}, std::integral_constant<int, SVIP_F16>{});
+    constexpr std::integral_constant<int, 1> one{};
+    if (dtype == SVIP_F32 && rows <= FEW_ROWS) return f(F32{}, Small{}, one, std::integral_constant<int, SVIP_F32>{});
+    if (dtype == SVIP_F32) return f(F16{}, Large{}, std::integral_constant<int, 3>{}, std::integral_constant<int, SVIP_F32>{});
+    return by_rows(rows, [&](auto shape) {
+        if (dtype == SVIP_BF16) return f(Bf16{}, shape, one, std::integral_constant<int, SVIP_BF16>{});
+        return f(F16{}, shape, one, std::integral_constant<int, SVIP_F16>{});
+    });
 }
 
 // ---- workspace ---------------------------------------------------------------------------------------------------------------------------------
@@ -78,7 +86,8 @@ constexpr size_t PIECE_BYTES = (size_t)256 << 20;      // of a piece's softmax: 
 constexpr int LEAST_PIECE = 2048;                      // tokens
 
 struct HeadPlan {
-    int planes, width;         // fp32: 2; channels of packed rows
+    bool parts;                // fp32 as two fp16 parts
+    int planes, size, width;   // planes and bytes of what the products are made of; channels of its rows
     int piece;                 // tokens of a piece of the vocabulary, a multiple of TILE_MAX
     int splits, per_split;     // of a piece's tokens in the gradient of the hidden states
     size_t part, target, rows, hidden, weighted, weight, grad, sum, bytes;     // offsets
@@ -88,14 +97,16 @@ struct HeadPlan {
 static HeadPlan plan(int call, int dtype, int N, int V, int D)
 {
     HeadPlan p = {};
-    const bool f32 = dtype == SVIP_F32, grad = call == SVIP_HEAD_LOSS_GRAD;
-    p.planes = f32 ? 2 : 1;
-    p.width = up(D, 8);
-    const int least = N > 64 ? Large::BM : Small::BM;
+    const bool grad = call == SVIP_HEAD_LOSS_GRAD;
+    p.parts = dtype == SVIP_F32 && N > FEW_ROWS;
+    p.planes = p.parts ? 2 : 1;
+    p.size = dtype == SVIP_F32 && !p.parts ? 4 : 2;
+    p.width = p.parts ? up(D, 8) : D;
+    const int least = N > FEW_ROWS ? Large::BM : Small::BM;
     // pieces: of the softmax in the gradient, of the weight's parts in fp32; equal, so that none is a sliver
     long long most = V;
-    if (grad) most = (long long)(PIECE_BYTES / ((size_t)N * 2 * p.planes));
-    if (f32) most = most < (long long)(PIECE_BYTES / ((size_t)p.width * 4)) ? most : (long long)(PIECE_BYTES / ((size_t)p.width * 4));
+    if (grad) most = (long long)(PIECE_BYTES / ((size_t)N * p.size * p.planes));
+    if (p.parts) most = most < (long long)(PIECE_BYTES / ((size_t)p.width * 4)) ? most : (long long)(PIECE_BYTES / ((size_t)p.width * 4));
     if (most < LEAST_PIECE) most = LEAST_PIECE;
     p.piece = up(ceil_div(V, ceil_div(V, most)), TILE_MAX);
     if (p.piece > up(V, TILE_MAX)) p.piece = up(V, TILE_MAX);
@@ -110,26 +121,26 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
         p.bytes = at;
         return p;
     }
-    const size_t packed = (size_t)p.planes * N * p.width * 2;
+    const size_t packed = (size_t)p.planes * N * up(p.width, 8) * p.size;
     // (a loss and its gradient may use one workspace of either's size or more, one after the other: nothing is kept between them)
     p.part = take((size_t)ceil_div(V, least) * N * sizeof(float2));
     p.target = take((size_t)N * sizeof(float));
-    if (f32) {
+    if (p.parts) {
         p.rows = take((size_t)N * sizeof(float));
         p.hidden = take(packed);
         p.weight = take((size_t)2 * p.piece * p.width * 2);
     }
     if (grad) {
         p.weighted = take(packed);
-        p.grad = take((size_t)p.planes * N * p.grad_stride * 2);
+        p.grad = take((size_t)p.planes * N * p.grad_stride * p.size);
         // enough workgroups to fill the chip twice over where the gradient of the hidden states has few tiles
-        const long long tiles = N > 64 ? (long long)ceil_div(p.width, Large::BM) * ceil_div(N, Large::BN)
+        const long long tiles = N > FEW_ROWS ? (long long)ceil_div(p.width, Large::BM) * ceil_div(N, Large::BN)
                                        : (long long)ceil_div(p.width, Small::BM) * ceil_div(N, Small::BN);
-        const int steps = p.piece / 64;
+        const int step = STEP_BYTES / p.size, steps = p.piece / step;
         long long splits = 512 / tiles;
         if (splits > steps / 8) splits = steps / 8;
         if (splits < 1) splits = 1;
-        p.per_split = ceil_div(steps, splits) * 64;
+        p.per_split = ceil_div(steps, splits) * step;
         p.splits = ceil_div(p.piece, p.per_split);
         p.sum = take((size_t)p.splits * N * p.width * sizeof(float));
     }
@@ -175,21 +186,20 @@ static HeadScalars *scalars(const LossCall &c) { return reinterpret_cast<HeadSca
 // The scalars that the tiles use, and in fp32 the parts of the hidden states.
 static bool prepare(const LossCall &c, const HeadPlan &p, const float *grad_loss, float grad_scale)
 {
-    const bool f32 = c.dtype == SVIP_F32;
+    if (!p.parts && !grad_loss) return true;
     HeadScalars *sc = scalars(c);
-    if (f32) {
+    if (p.parts) {
         if (!launch(k_head_clear, 1, 1, c.st, HeadClearArgs{sc})) return false;
         auto largest = [&](const void *x, long long stride, int rows, const int *targets, unsigned *out) {
             HeadMaxArgs m = {static_cast<const float *>(x), stride, rows, c.D, targets, c.V, out};
-            const long long groups = ceil_div((long long)rows * (c.D / 4), 256 * 8);
-            return launch(k_head_max, groups < 2048 ? groups : 2048, 256, c.st, m);
+            return launch(k_head_max, rows < 4 * 2048 ? ceil_div(rows, 4) : 2048, 256, c.st, m);
         };
         if (!largest(c.weight, c.weight_stride, c.V, nullptr, &sc->weight_max)) return false;
         if (grad_loss && !largest(c.hidden, c.hidden_stride, c.N, c.targets, &sc->hidden_max)) return false;
     }
-    HeadScalarsArgs a = {sc, f32, c.N, c.V, c.temperature, c.targets, grad_loss, grad_scale, reinterpret_cast<unsigned *>(c.ws)};
+    HeadScalarsArgs a = {sc, p.parts, c.N, c.V, c.temperature, c.targets, grad_loss, grad_scale, reinterpret_cast<unsigned *>(c.ws)};
     if (!launch(k_head_scalars, 1, SCALARS_WG, c.st, a)) return false;
-    if (!f32) return true;
+    if (!p.parts) return true;
     HeadPackArgs h = {};
     h.x = c.hidden;
     h.stride = c.hidden_stride;
@@ -208,7 +218,7 @@ static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, 
     HeadArgs a = {};
     const int size = size_of(c.dtype);
     const char *rows = static_cast<const char *>(c.weight) + (long long)v0 * c.weight_stride * size;
-    if (c.dtype == SVIP_F32) {
+    if (p.parts) {
         HeadPackArgs w = {};
         w.x = rows;
         w.stride = c.weight_stride;
@@ -231,6 +241,7 @@ static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, 
     a.D = p.width;
     a.v0 = v0;
     a.sc = scalars(c);
+    a.to_log2 = (float)(1.4426950408889634 / (double)c.temperature);
     a.targets = c.targets;
     a.part = reinterpret_cast<float2 *>(c.ws + p.part);
     a.target_logit = reinterpret_cast<float *>(c.ws + p.target);
@@ -243,19 +254,17 @@ static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, 
 static bool run_loss(const LossCall &c, const HeadPlan &p, float *loss, float *lse)
 {
     if (!prepare(c, p, nullptr, 1.f)) return false;
-    const int whole = c.dtype == SVIP_F32 ? p.piece : c.V;
+    const int whole = p.parts ? p.piece : c.V;
     int records = 0;
     for (int v0 = 0; v0 < c.V; v0 += whole) {
         const int count = c.V - v0 < whole ? c.V - v0 : whole;
         HeadArgs a;
         if (!piece_args(c, p, v0, count, &a)) return false;
-        const bool ok = by_product(c.dtype, [&](auto type, auto terms, auto) {
-            return by_rows(c.N, [&](auto shape) {
-                using S = decltype(shape);
-                a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
-                records = v0 / S::BM + a.tiles.m;
-                return launch(k_head_stats<decltype(type), S, decltype(terms)::value>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
-            });
+        const bool ok = by_product(c.dtype, c.N, [&](auto type, auto shape, auto terms, auto) {
+            using S = decltype(shape);
+            a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
+            records = v0 / S::BM + a.tiles.m;
+            return launch(k_head_stats<decltype(type), S, decltype(terms)::value>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
         });
         if (!ok) return false;
     }
@@ -271,17 +280,19 @@ struct GradOut {
 
 static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, const float *grad_loss, const GradOut &out)
 {
-    const float scale = c.dtype == SVIP_BF16 ? 1.f : GRAD_SCALE_F16;
+    const float scale = c.dtype == SVIP_F16 || p.parts ? GRAD_SCALE_F16 : 1.f;
     if (!prepare(c, p, grad_loss, scale)) return false;
     const int size = size_of(c.dtype);
-    const long long packed_plane = (long long)c.N * p.width * 2, grad_plane = (long long)c.N * p.grad_stride * 2;
+    const int wide = up(p.width, 8);                       // of the weighted hidden states' rows
+    const long long packed_plane = (long long)c.N * wide * p.size, grad_plane = (long long)c.N * p.grad_stride * p.size;
     if (out.weight) {
         HeadPackArgs h = {};
         h.x = c.hidden;
         h.stride = c.hidden_stride;
         h.rows = c.N;
         h.cols = c.D;
-        h.cols_p = p.width;
+        h.cols_p = wide;
+        h.whole = p.size == 4;
         h.out = c.ws + p.weighted;
         h.plane = packed_plane;
         h.sc = scalars(c);
@@ -289,7 +300,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         h.grad_loss = grad_loss;
         h.vocab = c.V;
         if (!by_dtype(c.dtype, [&](auto dt) {
-                return launch(k_head_pack<decltype(dt)::value>, ceil_div((long long)c.N * (p.width / 8), 256), 256, c.st, h);
+                return launch(k_head_pack<decltype(dt)::value>, ceil_div((long long)c.N * (wide / 8), 256), 256, c.st, h);
             }))
             return false;
     }
@@ -301,44 +312,42 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         a.grad = c.ws + p.grad;
         a.grad_stride = p.grad_stride;
         a.grad_plane = grad_plane;
-        const Operand grad = {c.ws + p.grad, p.grad_stride * 2, grad_plane};
-        const bool ok = by_product(c.dtype, [&](auto type, auto terms_, auto dt) {
+        const Operand grad = {c.ws + p.grad, p.grad_stride * p.size, grad_plane};
+        const bool ok = by_product(c.dtype, c.N, [&](auto type, auto shape, auto terms, auto dt) {
             using T = decltype(type);
-            constexpr int TERMS = decltype(terms_)::value, DT = decltype(dt)::value;
-            return by_rows(c.N, [&](auto shape) {
-                using S = decltype(shape);
-                a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
-                if (!launch(k_head_softmax<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a)) return false;
-                if (out.hidden) {
-                    HeadHiddenArgs g = {};
-                    g.weight = a.weight;
-                    g.grad = grad;
-                    g.N = c.N;
-                    g.D = p.width;
-                    g.V = count;
-                    g.tiles = {ceil_div(p.width, S::BM), ceil_div(c.N, S::BN)};
-                    g.splits = ceil_div(count, p.per_split);
-                    g.per_split = p.per_split;
-                    g.first = v0 == 0;
-                    g.sum = reinterpret_cast<float *>(c.ws + p.sum);
-                    if (!launch(k_head_grad_hidden<T, S, TERMS>, (long long)g.tiles.m * g.tiles.n * g.splits, S::THREADS, c.st, g)) return false;
-                }
-                if (out.weight) {
-                    HeadWeightArgs g = {};
-                    g.hidden = {c.ws + p.weighted, (long long)p.width * 2, packed_plane};
-                    g.grad = grad;
-                    g.N = c.N;
-                    g.D = c.D;
-                    g.Dp = p.width;
-                    g.V = count;
-                    g.tiles = {ceil_div(p.width, S::BM), ceil_div(count, S::BN)};
-                    g.sc = scalars(c);
-                    g.out = static_cast<char *>(out.weight) + (long long)v0 * out.weight_stride * size;
-                    g.out_stride = out.weight_stride;
-                    if (!launch(k_head_grad_weight<T, S, TERMS, DT>, (long long)g.tiles.m * g.tiles.n, S::THREADS, c.st, g)) return false;
-                }
-                return true;
-            });
+            using S = decltype(shape);
+            constexpr int TERMS = decltype(terms)::value, DT = decltype(dt)::value;
+            a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
+            if (!launch(k_head_softmax<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a)) return false;
+            if (out.hidden) {
+                HeadHiddenArgs g = {};
+                g.weight = a.weight;
+                g.grad = grad;
+                g.N = c.N;
+                g.D = p.width;
+                g.V = count;
+                g.tiles = {ceil_div(p.width, S::BM), ceil_div(c.N, S::BN)};
+                g.splits = ceil_div(count, p.per_split);
+                g.per_split = p.per_split;
+                g.first = v0 == 0;
+                g.sum = reinterpret_cast<float *>(c.ws + p.sum);
+                if (!launch(k_head_grad_hidden<T, S, TERMS>, (long long)g.tiles.m * g.tiles.n * g.splits, S::THREADS, c.st, g)) return false;
+            }
+            if (out.weight) {
+                HeadWeightArgs g = {};
+                g.hidden = {c.ws + p.weighted, (long long)wide * p.size, packed_plane};
+                g.grad = grad;
+                g.N = c.N;
+                g.D = c.D;
+                g.Dp = p.width;
+                g.V = count;
+                g.tiles = {ceil_div(p.width, S::BM), ceil_div(count, S::BN)};
+                g.sc = scalars(c);
+                g.out = static_cast<char *>(out.weight) + (long long)v0 * out.weight_stride * size;
+                g.out_stride = out.weight_stride;
+                if (!launch(k_head_grad_weight<T, S, TERMS, DT>, (long long)g.tiles.m * g.tiles.n, S::THREADS, c.st, g)) return false;
+            }
+            return true;
         });
         if (!ok) return false;
     }
