@@ -632,19 +632,40 @@ struct HeadHiddenFinishArgs {
     void *out;
     long long out_stride;
 };
+// The splits' sums, four slices of them side by side: a row's 64 columns of four a workgroup.
+constexpr int JOIN_COLUMNS = 64, JOIN_SLICES = 4, JOIN_BATCH = 8;
 template <int DT>
-__global__ __launch_bounds__(256) void k_head_hidden_finish(HeadHiddenFinishArgs a)
+__global__ __launch_bounds__(JOIN_COLUMNS * JOIN_SLICES) void k_head_hidden_finish(HeadHiddenFinishArgs a)
 {
-    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4, per_row = a.D;
-    const long long n = i / per_row;
-    const int d = (int)(i - n * per_row);
-    if (n >= a.N) return;
+    __shared__ f32x4 sums[JOIN_SLICES][JOIN_COLUMNS];
+    const int groups = (a.D + 4 * JOIN_COLUMNS - 1) / (4 * JOIN_COLUMNS), n = blockIdx.x / groups;
+    const int column = threadIdx.x % JOIN_COLUMNS, slice = threadIdx.x / JOIN_COLUMNS;
+    const int d = ((blockIdx.x - n * groups) * JOIN_COLUMNS + column) * 4;
+    const bool use = counts(a.targets[n], a.vocab);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    float m = 0.f;
-    if (counts(a.targets[n], a.vocab)) {
-        m = a.grad_loss[n] * a.sc->hidden_mult;
-        for (int k = 0; k < a.splits; ++k) s += *reinterpret_cast<const f32x4 *>(a.sum + ((long long)k * a.N + n) * a.Dp + d);
+    if (use && d < a.D) {
+        const float *p = a.sum + (long long)n * a.Dp + d;
+        const long long next = (long long)a.N * a.Dp;
+        for (int k = slice; k < a.splits; k += JOIN_SLICES * JOIN_BATCH) {
+            f32x4 v[JOIN_BATCH];
+#pragma unroll
+            for (int q = 0; q < JOIN_BATCH; ++q) {
+                const int at = k + q * JOIN_SLICES;
+                if (at < a.splits) v[q] = *reinterpret_cast<const f32x4 *>(p + at * next);
+            }
+#pragma unroll
+            for (int q = 0; q < JOIN_BATCH; ++q)
+                if (k + q * JOIN_SLICES < a.splits) s += v[q];
+        }
     }
+    if (a.splits > 1) {
+        sums[slice][column] = s;
+        __syncthreads();
+    }
+    if (slice || d >= a.D) return;
+    if (a.splits > 1)
+        for (int k = 1; k < JOIN_SLICES; ++k) s += sums[k][column];
+    const float m = use ? a.grad_loss[n] * a.sc->hidden_mult : 0.f;
     Stored<DT>::put4(static_cast<typename Stored<DT>::type *>(a.out) + n * a.out_stride + d, s * m);
 }
 

@@ -46,51 +46,80 @@ static bool by_dtype(int d, F f)
 
 // ---- shapes of the tiles -------------------------------------------------------------------------------------------------------------------
 
-#ifndef HEAD_LARGE
-#define HEAD_LARGE 256, 256, 2, 4, 2
-#endif
-using Large = TileShape<HEAD_LARGE>;
-using Middle = TileShape<128, 128, 2, 2, 3>;           // (fp32 logits of 8-bit matrices: the tile's bf16 fragments need the registers)
-using Small = TileShape<128, 64, 4, 1, 3>;
+// m x n of a workgroup's tile, its waves along either, buffers in LDS.
+using Large = TileShape<256, 256, 2, 4, 2>;            // one workgroup a CU
+using Middle = TileShape<128, 128, 2, 2, 2>;           // two
+using Small = TileShape<128, 64, 4, 1, 3>;             // two: up to 64 rows wait for the weight's bytes, and a tile has them all
+using Few = TileShape<128, 32, 4, 1, 4>;               // two: up to 32 rows
+using Middle8 = TileShape<128, 128, 2, 2, 3>;          // fp32 logits of 8-bit matrices (the tile's bf16 fragments need the registers)
+enum ShapeId { LARGE, MIDDLE, SMALL, FEW };
 
-// Up to 64 rows wait for the weight's bytes: a tile of all rows, small enough for two workgroups a CU.
-constexpr int FEW_ROWS = 64;
+constexpr int FEW_ROWS = 64, FEWER_ROWS = 32;
+constexpr int CUS = 256;
+constexpr int LEAST_TILE = 128, MOST_TILE = 256;       // tokens of a tile
 
-// f with the shape for `rows` rows of hidden states (n of the tiles).
-template <typename F>
-static bool by_rows(int rows, F f)
+// Time of a product of m x n over `steps` steps, in units of 1 us or so.  A large tile takes 1.4 us a step and 5 us besides, with one workgroup a CU; a
+// middle one, of a quarter of its size, 0.85 us and 5 us, with two.  So many tiles go faster as large ones (loss of 8192 x 151936 x 2048: 3690 us
+// against 4820), and where large ones would leave CUs without work as middle ones (129 x 32000 x 1024: 27 us against 23;
+// gradients of 1000 x 5000 x 1024: 125 us against 91).
+static double tiles_cost(ShapeId id, long long m, long long n, int splits, double steps)
 {
-    if (rows > FEW_ROWS) return f(Large{});
-    return f(Small{});
+    const long long size = id == LARGE ? 256 : 128, at_once = id == LARGE ? CUS : 2 * CUS;
+    const long long rounds = ((m + size - 1) / size * ((n + size - 1) / size) * splits + at_once - 1) / at_once;
+    return (double)rounds * (5.0 + (id == LARGE ? 1.4 : 0.85) * steps);
+}
+static ShapeId larger_or_middle(long long m, long long n, double steps)
+{
+    return tiles_cost(LARGE, m, n, 1, steps) <= tiles_cost(MIDDLE, m, n, 1, steps) ? LARGE : MIDDLE;
+}
+// of the tiles of logits
+static ShapeId shape_of(int rows, long long vocab, double steps)
+{
+    if (rows <= FEWER_ROWS) return FEW;
+    if (rows <= FEW_ROWS) return SMALL;
+    return larger_or_middle(vocab, rows, steps);
+}
+// f with the shape of that number, of those that the kernel comes in.
+template <typename F>
+static bool by_shape(ShapeId id, bool few, F f)
+{
+    if (id == LARGE) return f(Large{});
+    if (id == MIDDLE) return f(Middle{});
+    if (few && id == SMALL) return f(Small{});
+    return few && f(Few{});
 }
 
 // f with what the products are made of, their terms and the dtype.  fp32 values of many rows go as two fp16 parts, at a third of the rate of 16-bit
-// values and three times that of fp32 products; of few rows as they are, since laying out a weight's parts would cost more than its products.
+// values and three times that of fp32 products; of few rows as they are, since laying out a weight's parts would cost more than its
+// products (17 rows, 32000 x 512, loss and gradients: 387 us in parts, 131 us as they are).
 template <typename F>
-static bool by_product(int dtype, int rows, F f)
+static bool by_product(int dtype, bool parts, F f)
 {
     constexpr std::integral_constant<int, 1> one{};
-    if (dtype == SVIP_F32 && rows <= FEW_ROWS) return f(F32{}, Small{}, one, std::integral_constant<int, SVIP_F32>{});
-    if (dtype == SVIP_F32) return f(F16{}, Large{}, std::integral_constant<int, 3>{}, std::integral_constant<int, SVIP_F32>{});
-    return by_rows(rows, [&](auto shape) {
-        if (dtype == SVIP_BF16) return f(Bf16{}, shape, one, std::integral_constant<int, SVIP_BF16>{});
-        return f(F16{}, shape, one, std::integral_constant<int, SVIP_F16>{});
-    });
+    if (dtype == SVIP_BF16) return f(Bf16{}, one, std::integral_constant<int, SVIP_BF16>{});
+    if (dtype == SVIP_F16) return f(F16{}, one, std::integral_constant<int, SVIP_F16>{});
+    if (parts) return f(F16{}, std::integral_constant<int, 3>{}, std::integral_constant<int, SVIP_F32>{});
+    return f(F32{}, one, std::integral_constant<int, SVIP_F32>{});
 }
+// The shapes a kernel of these products comes in: fp32 as it is only for few rows, in parts only for many.
+template <typename T, int TERMS, typename S>
+constexpr bool made_of() { return TERMS == 3 ? S::BN >= 128 : (!std::is_same<T, F32>::value || S::BN <= 128); }
 
 // ---- workspace ---------------------------------------------------------------------------------------------------------------------------------
 
 constexpr size_t HEAD_HEADER = 512;                    // flag word (256 bytes), HeadScalars
-constexpr int TILE_MAX = 256;
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;      // of a piece's softmax: what the memory-side cache holds
 constexpr int LEAST_PIECE = 2048;                      // tokens
+constexpr int MOST_SPLITS = 128;
+constexpr size_t SPLIT_BYTES = (size_t)128 << 20;
 
 struct HeadPlan {
     bool parts;                // fp32 as two fp16 parts
     int planes, size, width;   // planes and bytes of what the products are made of; channels of its rows
-    int piece;                 // tokens of a piece of the vocabulary, a multiple of TILE_MAX
+    int piece;                 // tokens of a piece of the vocabulary, a multiple of MOST_TILE
+    ShapeId logits, hidden_grad, weight_grad;
     int splits, per_split;     // of a piece's tokens in the gradient of the hidden states
-    size_t part, target, rows, hidden, weighted, weight, grad, sum, bytes;     // offsets
+    size_t part, target, rows, hidden_parts, weighted, weight, grad, sum, bytes;     // offsets
     long long grad_stride;
 };
 
@@ -102,14 +131,14 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     p.planes = p.parts ? 2 : 1;
     p.size = dtype == SVIP_F32 && !p.parts ? 4 : 2;
     p.width = p.parts ? up(D, 8) : D;
-    const int least = N > FEW_ROWS ? Large::BM : Small::BM;
+    const double terms = p.parts ? 3.0 : 1.0;
     // pieces: of the softmax in the gradient, of the weight's parts in fp32; equal, so that none is a sliver
     long long most = V;
     if (grad) most = (long long)(PIECE_BYTES / ((size_t)N * p.size * p.planes));
     if (p.parts) most = most < (long long)(PIECE_BYTES / ((size_t)p.width * 4)) ? most : (long long)(PIECE_BYTES / ((size_t)p.width * 4));
     if (most < LEAST_PIECE) most = LEAST_PIECE;
-    p.piece = up(ceil_div(V, ceil_div(V, most)), TILE_MAX);
-    if (p.piece > up(V, TILE_MAX)) p.piece = up(V, TILE_MAX);
+    p.piece = up(ceil_div(V, ceil_div(V, most)), MOST_TILE);
+    if (p.piece > up(V, MOST_TILE)) p.piece = up(V, MOST_TILE);
     p.grad_stride = p.piece;
     size_t at = HEAD_HEADER;
     auto take = [&](size_t bytes) {
@@ -121,28 +150,42 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
         p.bytes = at;
         return p;
     }
+    const int step = STEP_BYTES / p.size;
+    p.logits = shape_of(N, grad || p.parts ? p.piece : V, terms * ceil_div(D, step));
     const size_t packed = (size_t)p.planes * N * up(p.width, 8) * p.size;
     // (a loss and its gradient may use one workspace of either's size or more, one after the other: nothing is kept between them)
-    p.part = take((size_t)ceil_div(V, least) * N * sizeof(float2));
+    p.part = take((size_t)ceil_div(V, LEAST_TILE) * N * sizeof(float2));
     p.target = take((size_t)N * sizeof(float));
     if (p.parts) {
         p.rows = take((size_t)N * sizeof(float));
-        p.hidden = take(packed);
+        p.hidden_parts = take(packed);
         p.weight = take((size_t)2 * p.piece * p.width * 2);
     }
     if (grad) {
         p.weighted = take(packed);
         p.grad = take((size_t)p.planes * N * p.grad_stride * p.size);
-        // enough workgroups to fill the chip twice over where the gradient of the hidden states has few tiles
-        const long long tiles = N > FEW_ROWS ? (long long)ceil_div(p.width, Large::BM) * ceil_div(N, Large::BN)
-                                       : (long long)ceil_div(p.width, Small::BM) * ceil_div(N, Small::BN);
-        const int step = STEP_BYTES / p.size, steps = p.piece / step;
-        long long splits = 512 / tiles;
-        if (splits > steps / 8) splits = steps / 8;
-        if (splits < 1) splits = 1;
-        p.per_split = ceil_div(steps, splits) * step;
+        p.weight_grad = N <= FEW_ROWS ? MIDDLE : larger_or_middle(D, p.piece, terms * ceil_div(N, step));
+        // The gradient of the hidden states has few tiles and many steps, which are split where that fills the chip better.
+        const int steps = p.piece / step;
+        double best = 0.0;
+        for (int splits = 1; splits <= MOST_SPLITS && (splits == 1 || steps / splits >= 8); ++splits) {
+            if (splits > 1 && (size_t)splits * N * p.width * sizeof(float) > SPLIT_BYTES) break;
+            for (ShapeId id : {LARGE, MIDDLE}) {
+                const bool few = N <= FEW_ROWS;
+                if (few && id == LARGE) continue;
+                // few rows: tiles of 128 x all rows, whatever the rows' number; the sums of the splits are read once more in the end
+                const double cost = tiles_cost(id, p.width, few ? 1 : N, splits, terms * ceil_div(steps, splits)) + 4.0 * N * p.width * splits / 3e6;
+                if (best == 0.0 || cost < best) {
+                    best = cost;
+                    p.hidden_grad = few ? p.logits : id;
+                    p.per_split = ceil_div(steps, splits) * step;
+                }
+            }
+        }
         p.splits = ceil_div(p.piece, p.per_split);
         p.sum = take((size_t)p.splits * N * p.width * sizeof(float));
+        const size_t loss = plan(SVIP_HEAD_LOSS, dtype, N, V, D).bytes;          // (one workspace serves both)
+        if (at < loss) at = loss;
     }
     p.bytes = at;
     return p;
@@ -206,7 +249,7 @@ static bool prepare(const LossCall &c, const HeadPlan &p, const float *grad_loss
     h.rows = c.N;
     h.cols = c.D;
     h.cols_p = p.width;
-    h.out = c.ws + p.hidden;
+    h.out = c.ws + p.hidden_parts;
     h.plane = (long long)c.N * p.width * 2;
     h.row_inv = reinterpret_cast<float *>(c.ws + p.rows);
     return launch(k_head_pack_rows, ceil_div(c.N, 4), 256, c.st, h);
@@ -230,7 +273,7 @@ static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, 
         w.sc = scalars(c);
         if (!launch(k_head_pack<SVIP_F32>, ceil_div((long long)count * (p.width / 8), 256), 256, c.st, w)) return false;
         a.weight = {w.out, (long long)p.width * 2, w.plane};
-        a.hidden = {c.ws + p.hidden, (long long)p.width * 2, (long long)c.N * p.width * 2};
+        a.hidden = {c.ws + p.hidden_parts, (long long)p.width * 2, (long long)c.N * p.width * 2};
         a.row_inv = reinterpret_cast<const float *>(c.ws + p.rows);
     } else {
         a.weight = {rows, c.weight_stride * size, 0};
@@ -260,11 +303,18 @@ static bool run_loss(const LossCall &c, const HeadPlan &p, float *loss, float *l
         const int count = c.V - v0 < whole ? c.V - v0 : whole;
         HeadArgs a;
         if (!piece_args(c, p, v0, count, &a)) return false;
-        const bool ok = by_product(c.dtype, c.N, [&](auto type, auto shape, auto terms, auto) {
-            using S = decltype(shape);
-            a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
-            records = v0 / S::BM + a.tiles.m;
-            return launch(k_head_stats<decltype(type), S, decltype(terms)::value>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
+        const bool ok = by_product(c.dtype, p.parts, [&](auto type, auto terms, auto) {
+            return by_shape(p.logits, true, [&](auto shape) {
+                using S = decltype(shape);
+                using T = decltype(type);
+                constexpr int TERMS = decltype(terms)::value;
+                a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
+                records = v0 / S::BM + a.tiles.m;
+                if constexpr (made_of<T, TERMS, S>())
+                    return launch(k_head_stats<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
+                else
+                    return false;
+            });
         });
         if (!ok) return false;
     }
@@ -313,13 +363,20 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         a.grad_stride = p.grad_stride;
         a.grad_plane = grad_plane;
         const Operand grad = {c.ws + p.grad, p.grad_stride * p.size, grad_plane};
-        const bool ok = by_product(c.dtype, c.N, [&](auto type, auto shape, auto terms, auto dt) {
+        const bool ok = by_product(c.dtype, p.parts, [&](auto type, auto terms, auto dt) {
             using T = decltype(type);
-            using S = decltype(shape);
             constexpr int TERMS = decltype(terms)::value, DT = decltype(dt)::value;
-            a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
-            if (!launch(k_head_softmax<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a)) return false;
-            if (out.hidden) {
+            // launches a kernel in a shape, `tiles` its tiles along m and n
+            const auto softmax = [&](auto shape) {
+                using S = decltype(shape);
+                a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
+                if constexpr (made_of<T, TERMS, S>())
+                    return launch(k_head_softmax<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
+                else
+                    return false;
+            };
+            const auto grad_hidden = [&](auto shape) {
+                using S = decltype(shape);
                 HeadHiddenArgs g = {};
                 g.weight = a.weight;
                 g.grad = grad;
@@ -331,9 +388,13 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
                 g.per_split = p.per_split;
                 g.first = v0 == 0;
                 g.sum = reinterpret_cast<float *>(c.ws + p.sum);
-                if (!launch(k_head_grad_hidden<T, S, TERMS>, (long long)g.tiles.m * g.tiles.n * g.splits, S::THREADS, c.st, g)) return false;
-            }
-            if (out.weight) {
+                if constexpr (made_of<T, TERMS, S>())
+                    return launch(k_head_grad_hidden<T, S, TERMS>, (long long)g.tiles.m * g.tiles.n * g.splits, S::THREADS, c.st, g);
+                else
+                    return false;
+            };
+            const auto grad_weight = [&](auto shape) {
+                using S = decltype(shape);
                 HeadWeightArgs g = {};
                 g.hidden = {c.ws + p.weighted, (long long)wide * p.size, packed_plane};
                 g.grad = grad;
@@ -345,9 +406,13 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
                 g.sc = scalars(c);
                 g.out = static_cast<char *>(out.weight) + (long long)v0 * out.weight_stride * size;
                 g.out_stride = out.weight_stride;
-                if (!launch(k_head_grad_weight<T, S, TERMS, DT>, (long long)g.tiles.m * g.tiles.n, S::THREADS, c.st, g)) return false;
-            }
-            return true;
+                if constexpr (made_of<T, TERMS, S>())
+                    return launch(k_head_grad_weight<T, S, TERMS, DT>, (long long)g.tiles.m * g.tiles.n, S::THREADS, c.st, g);
+                else
+                    return false;
+            };
+            return by_shape(p.logits, true, softmax) && (!out.hidden || by_shape(p.hidden_grad, true, grad_hidden)) &&
+                   (!out.weight || by_shape(p.weight_grad, false, grad_weight));
         });
         if (!ok) return false;
     }
@@ -356,7 +421,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
     HeadHiddenFinishArgs f = {reinterpret_cast<const float *>(c.ws + p.sum), splits, c.N, c.D, p.width, scalars(c), c.targets, grad_loss, c.V, out.hidden,
                               out.hidden_stride};
     return by_dtype(c.dtype, [&](auto dt) {
-        return launch(k_head_hidden_finish<decltype(dt)::value>, ceil_div((long long)c.N * c.D / 4, 256), 256, c.st, f);
+        return launch(k_head_hidden_finish<decltype(dt)::value>, (long long)c.N * ceil_div(c.D, 4 * JOIN_COLUMNS), JOIN_COLUMNS * JOIN_SLICES, c.st, f);
     });
 }
 
@@ -418,8 +483,8 @@ svip_status svip_head_logits(const void *hidden_q, const void *hidden_scale, con
     a.out = logits_out;
     a.out_stride = row_stride;
     const bool ok = by_dtype(dtype, [&](auto dt) {
-        return by_rows(N, [&](auto shape) {
-            using S = std::conditional_t<decltype(dt)::value == SVIP_F32 && std::is_same<decltype(shape), Large>::value, Middle, decltype(shape)>;
+        return by_shape(N <= FEW_ROWS ? SMALL : LARGE, true, [&](auto shape) {
+            using S = std::conditional_t<std::is_same<decltype(shape), Small>::value, Small, std::conditional_t<decltype(dt)::value == SVIP_F32, Middle8, Large>>;
             a.tiles = {ceil_div(V, S::BM), ceil_div(N, S::BN)};
             return launch(k_head_logits<S, decltype(dt)::value>, (long long)a.tiles.m * a.tiles.n, S::THREADS, static_cast<hipStream_t>(hip_stream), a);
         });
