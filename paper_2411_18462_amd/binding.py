@@ -126,7 +126,8 @@ def load():
     from . import _marshal
 
     _marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value
-                    for f in (lib.svip_draft_step, lib.svip_draft_step_greedy, lib.svip_verify, lib.svip_verify_greedy)))
+                    for f in (lib.svip_draft_step, lib.svip_draft_step_greedy, lib.svip_verify, lib.svip_verify_greedy,
+                            lib.svip_quantize_blocks, lib.svip_head_logits)))
     _lib, _native = lib, _marshal
     return lib
 
@@ -489,12 +490,15 @@ def _on_one_device(**tensors):
 def quantize_blocks(x, *, block_rows=1, q_out, scale_out, stream=None):
     """svip_quantize_blocks.  x [rows, cols] float32, bfloat16 or float16; q_out [rows, K] float8_e4m3fn, K = cols filled up to a
     multiple of 128; scale_out [ceil(rows / block_rows), K / 128] float8_e8m0fnu."""
+    status = (_native or _load_native()).quantize_blocks(x, block_rows, q_out, scale_out, None if stream is None else _stream(stream))
+    if status != _DECLINED:
+        return _check(status) if status else None
     if x.dtype not in _DTYPES:
         raise SvipError(3, "x must be float32, bfloat16 or float16")
     if block_rows not in (1, HEAD_BLOCK):
         raise SvipError(6, "block_rows must be 1 or 128")
-    px, sx = _rows(x, None, None, "x") if x.is_cuda else (None, 0)
     with _on_one_device(x=x, q_out=q_out, scale_out=scale_out):
+        px, sx = _rows(x, None, None, "x")
         rows, cols = x.shape
         kb = -(-cols // HEAD_BLOCK)
         pq, sq = _rows(q_out, (rows, kb * HEAD_BLOCK), torch.float8_e4m3fn, "q_out")
@@ -505,6 +509,10 @@ def quantize_blocks(x, *, block_rows=1, q_out, scale_out, stream=None):
 def head_logits(hidden_q, hidden_scale, weight_q, weight_scale, *, logits_out, workspace, stream=None):
     """svip_head_logits.  hidden_q [N, K], weight_q [V, K] float8_e4m3fn; hidden_scale [N, K / 128], weight_scale [ceil(V / 128), K / 128]
     float8_e8m0fnu; logits_out [N, V] float32, bfloat16 or float16."""
+    status = (_native or _load_native()).head_logits(hidden_q, hidden_scale, weight_q, weight_scale, logits_out, workspace,
+                                                     None if stream is None else _stream(stream))
+    if status != _DECLINED:
+        return _check(status) if status else None
     if logits_out.dtype not in _DTYPES:
         raise SvipError(3, "logits_out must be float32, bfloat16 or float16")
     with _on_one_device(hidden_q=hidden_q, hidden_scale=hidden_scale, weight_q=weight_q, weight_scale=weight_scale, logits_out=logits_out,

@@ -195,6 +195,46 @@ __device__ __forceinline__ void tile_of(unsigned block, Tiles t, int group, int 
     tn = (int)(g * (unsigned)group + j % width);
 }
 
+// Stores a tile of 16-bit results, `rows` rows (n) of `cols` values (m) of it, at `out`.  A lane's four neighbours in m are 8 bytes, which stored as they
+// are would reach memory 32 bytes to a row at a time; so the tile goes through LDS, and 16 bytes a lane fill whole lines.  Chunk c of
+// row n lies at chunk c ^ (n % 16): neither the 16 rows of a fragment nor the chunks of a row meet a bank twice.
+// value(i, j): results of fragment (i, j); called by all threads of the workgroup, when no copy into `smem` is under way.
+template <typename S, typename X, typename Value>
+__device__ __forceinline__ void store_rows(char *smem, int rows, int cols, X *out, long long stride, Value value)
+{
+    typedef X x4 __attribute__((ext_vector_type(4)));
+    typedef X x8 __attribute__((ext_vector_type(8)));
+    constexpr int CHUNKS = S::BM / 8, MASK = (CHUNKS < 16 ? CHUNKS : 16) - 1, ROUNDS = S::BN * CHUNKS / S::THREADS;
+    static_assert(S::BN * S::BM * 2 <= S::LDS_BYTES && S::BN * CHUNKS % S::THREADS == 0, "");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN, g = lane >> 4;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = wn + 16 * j + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int chunk = (wm / 8 + 2 * i + (g >> 1)) ^ (n & MASK);
+            *reinterpret_cast<x4 *>(smem + n * (S::BM * 2) + chunk * 16 + (g & 1) * 8) = __builtin_convertvector(value(i, j), x4);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const int c = k * S::THREADS + (int)threadIdx.x, n = c / CHUNKS, m = c % CHUNKS * 8;
+        if (n >= rows || m >= cols) continue;
+        const x8 v = *reinterpret_cast<const x8 *>(smem + n * (S::BM * 2) + ((c % CHUNKS) ^ (n & MASK)) * 16);
+        X *p = out + n * stride + m;
+        if (m + 8 <= cols) {
+            *reinterpret_cast<x8 *>(p) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (m + e < cols) p[e] = v[e];
+        }
+    }
+}
+
 // ---- logits from 8-bit matrices ------------------------------------------------------------------------------------------------------------
 
 struct HeadLogitsArgs {
@@ -208,7 +248,7 @@ struct HeadLogitsArgs {
 };
 
 constexpr int SCALE_STEPS = 64;                        // steps whose scales are in LDS at a time
-constexpr int SCALE_PITCH = SCALE_STEPS + 4;
+constexpr int SCALE_PITCH = SCALE_STEPS + 4, SCALE_WORDS = SCALE_STEPS / 4;
 
 // A step is 128 values of K: one block of each operand.
 // For 16-bit logits the matrix cores multiply the codes, and take the scales as they are (16x16x128, one scale per 32 values; here all
@@ -228,7 +268,8 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
 {
     constexpr int WEIGHT_BLOCKS = (S::BM + QBLOCK - 1) / QBLOCK;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
-    __shared__ unsigned char hs[S::BN * SCALE_PITCH], ws[WEIGHT_BLOCKS * SCALE_PITCH];
+    __shared__ __attribute__((aligned(4))) unsigned char scale_bytes[(S::BN + WEIGHT_BLOCKS) * SCALE_PITCH];
+    unsigned char *const hs = scale_bytes, *const ws = scale_bytes + S::BN * SCALE_PITCH;
     int tm, tn;
     tile_of(blockIdx.x, a.tiles, 4, tm, tn);
     const int v0 = tm * S::BM, n0 = tn * S::BN;
@@ -260,21 +301,33 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         sa.copy(at, s * QBLOCK, a.K, 0);
         sb.copy(at + S::BM * STEP_BYTES, s * QBLOCK, a.K, 0);
     };
+    // The scales of SCALE_STEPS steps into LDS, read four at a time, all under way before the first is needed.
     auto scales = [&](int s0) {
         const int count = steps - s0 < SCALE_STEPS ? steps - s0 : SCALE_STEPS;
-        for (int i = threadIdx.x; i < S::BN * count; i += S::THREADS) {
-            const int r = i / count, s = i - r * count, n = n0 + r < a.N ? n0 + r : a.N - 1;
-            hs[r * SCALE_PITCH + s] = a.hidden_scale[n * a.hidden_scale_stride + s0 + s];
+        constexpr int ROWS = S::BN + WEIGHT_BLOCKS, ROUNDS = (ROWS * SCALE_WORDS + S::THREADS - 1) / S::THREADS;
+        unsigned word[ROUNDS];
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) {
+            const int i = k * S::THREADS + (int)threadIdx.x, r = i / SCALE_WORDS, q = i % SCALE_WORDS;
+            const int n = n0 + r < a.N ? n0 + r : a.N - 1, block = v0 / QBLOCK + r - S::BN, last = (a.V - 1) / QBLOCK;
+            const unsigned char *p = r < S::BN ? a.hidden_scale + n * a.hidden_scale_stride
+                                               : a.weight_scale + (block < last ? block : last) * a.weight_scale_stride;
+            word[k] = 0u;
+            if (4 * q + 4 <= count)
+                __builtin_memcpy(&word[k], p + s0 + 4 * q, 4);
+            else
+                for (int e = 4 * q; e < count; ++e) word[k] |= (unsigned)p[s0 + e] << (8 * (e & 3));
         }
-        for (int i = threadIdx.x; i < WEIGHT_BLOCKS * count; i += S::THREADS) {
-            const int r = i / count, s = i - r * count, b = v0 / QBLOCK + r, last = (a.V - 1) / QBLOCK;
-            ws[r * SCALE_PITCH + s] = a.weight_scale[(b < last ? b : last) * a.weight_scale_stride + s0 + s];
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) {
+            const int i = k * S::THREADS + (int)threadIdx.x, r = i / SCALE_WORDS, q = i % SCALE_WORDS;
+            if (r < ROWS) *reinterpret_cast<unsigned *>(scale_bytes + r * SCALE_PITCH + 4 * q) = word[k];
         }
     };
+    const int w_row = (v0 % QBLOCK + wm) / QBLOCK;
 #pragma unroll
     for (int s = 0; s < S::STAGES - 1; ++s)
         if (s < steps) copy(s);
-    const int w_row = (v0 % QBLOCK + wm) / QBLOCK;
     for (int s = 0; s < steps; ++s) {
         if (s % SCALE_STEPS == 0) {
             if (s) __syncthreads();
@@ -321,15 +374,19 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         }
     }
     using X = typename Stored<DT>::type;
+    if constexpr (DT != SVIP_F32) {
+        store_rows<S, X>(smem, a.N - n0, a.V - v0, static_cast<X *>(a.out) + n0 * a.out_stride + v0, a.out_stride, [&](int i, int j) { return acc[i][j]; });
+    } else {
 #pragma unroll
-    for (int j = 0; j < S::FN; ++j) {
-        const int n = n0 + wn + 16 * j + (lane & 15);
-        if (n >= a.N) continue;
-        X *row = static_cast<X *>(a.out) + n * a.out_stride;
+        for (int j = 0; j < S::FN; ++j) {
+            const int n = n0 + wn + 16 * j + (lane & 15);
+            if (n >= a.N) continue;
+            X *row = static_cast<X *>(a.out) + n * a.out_stride;
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int v = v0 + wm + 16 * i + 4 * (lane >> 4);
-            if (v < a.V) put_up_to_4<DT>(row + v, acc[i][j], a.V - v);
+            for (int i = 0; i < S::FM; ++i) {
+                const int v = v0 + wm + 16 * i + 4 * (lane >> 4);
+                if (v < a.V) put_up_to_4<DT>(row + v, acc[i][j], a.V - v);
+            }
         }
     }
 }
@@ -552,33 +609,47 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     multiply<T, S, KC, KC, TERMS>(w, a.V - v0, h, a.N - n0, 0, a.D, smem, acc);
 
     using X = typename GradOf<T>::type;
-    typedef X x4 __attribute__((ext_vector_type(4)));
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN, first = v0 + wm + 4 * (lane >> 4);
+    const int cols = (int)a.grad_stride - v0;              // (columns behind the vocabulary are zeros)
+    float c[S::FN], base[S::FN], scale[S::FN];
+    int t[S::FN];                          // where a row's target is among this lane's tokens: 16 i + e
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
-        const int n = n0 + wn + 16 * j + (lane & 15);
-        if (n >= a.N) continue;
-        const float c = TERMS == 3 ? logits_scale<TERMS>(a) * a.row_inv[n] : logits_scale<TERMS>(a);
-        const int target = a.targets[n], first = v0 + wm + 4 * (lane >> 4), t = target - a.v0 - first;
-        const bool use = counts(target, a.vocab);
-        const float base = a.lse[n] * HEAD_LOG2E;
-        char *row = a.grad + T::SIZE * ((long long)n * a.grad_stride);
+        const int n = n0 + wn + 16 * j + (lane & 15), m = n < a.N ? n : a.N - 1, target = a.targets[m];
+        c[j] = TERMS == 3 ? logits_scale<TERMS>(a) * a.row_inv[m] : logits_scale<TERMS>(a);
+        t[j] = target - a.v0 - first;
+        base[j] = a.lse[m] * HEAD_LOG2E;
+        scale[j] = counts(target, a.vocab) ? GradOf<T>::SCALE : 0.f;
+    }
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int v = v0 + wm + 16 * i + 4 * (lane >> 4);
-            if (v >= a.grad_stride) continue;               // (a multiple of 64)
-            x4 g, low;
+    for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], c, -base));
-                if (t == 16 * i + e) p -= 1.f;
-                p = use && v + e < a.V ? p * GradOf<T>::SCALE : 0.f;
-                g[e] = (X)p;
-                if (TERMS == 3) low[e] = (X)(p - (float)g[e]);
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], c[j], -base[j]));
+                if (t[j] == 16 * i + e) p -= 1.f;
+                acc[i][j][e] = scale[j] != 0.f && first + 16 * i + e < a.V ? p * scale[j] : 0.f;
             }
-            *reinterpret_cast<x4 *>(row + T::SIZE * v) = g;
-            if (TERMS == 3) *reinterpret_cast<x4 *>(row + a.grad_plane + 2 * v) = low;
+    X *out = reinterpret_cast<X *>(a.grad) + n0 * a.grad_stride + v0;
+    if constexpr (sizeof(X) == 2) {
+        store_rows<S, X>(smem, a.N - n0, cols, out, a.grad_stride, [&](int i, int j) { return acc[i][j]; });
+        if (TERMS == 3)
+            store_rows<S, X>(smem, a.N - n0, cols, out + a.grad_plane / 2, a.grad_stride, [&](int i, int j) {
+                typedef X x4 __attribute__((ext_vector_type(4)));
+                return acc[i][j] - __builtin_convertvector(__builtin_convertvector(acc[i][j], x4), f32x4);
+            });
+    } else {
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            const int n = wn + 16 * j + (lane & 15);
+            if (n0 + n >= a.N) continue;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int m = wm + 16 * i + 4 * (lane >> 4);
+                if (m < cols) *reinterpret_cast<f32x4 *>(out + n * a.grad_stride + m) = acc[i][j];
+            }
         }
     }
 }
@@ -692,17 +763,21 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     multiply<T, S, KS, KS, TERMS>(h, a.Dp - d0, g, (int)(g.stride / T::SIZE) - v0, 0, a.N, smem, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN;
-    const float m = a.sc->weight_mult;
+    const float mult = a.sc->weight_mult;
     using X = typename Stored<DT>::type;
+    X *out = static_cast<X *>(a.out) + v0 * a.out_stride + d0;
+    if constexpr (sizeof(X) == 2) {
+        store_rows<S, X>(smem, a.V - v0, a.D - d0, out, a.out_stride, [&](int i, int j) { return acc[i][j] * mult; });
+    } else {
 #pragma unroll
-    for (int j = 0; j < S::FN; ++j) {
-        const int v = v0 + wn + 16 * j + (lane & 15);
-        if (v >= a.V) continue;
-        X *row = static_cast<X *>(a.out) + v * a.out_stride;
+        for (int j = 0; j < S::FN; ++j) {
+            const int v = wn + 16 * j + (lane & 15);
+            if (v0 + v >= a.V) continue;
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int d = d0 + wm + 16 * i + 4 * (lane >> 4);
-            if (d < a.D) Stored<DT>::put4(row + d, acc[i][j] * m);
+            for (int i = 0; i < S::FM; ++i) {
+                const int d = wm + 16 * i + 4 * (lane >> 4);
+                if (d0 + d < a.D) *reinterpret_cast<f32x4 *>(out + v * a.out_stride + d) = acc[i][j] * mult;
+            }
         }
     }
 }

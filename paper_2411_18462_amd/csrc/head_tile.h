@@ -300,7 +300,7 @@ __device__ __forceinline__ void multiply(const Operand &a, int a_rows, const Ope
     bool more = false;
     int s = 0;
     // MAIN: a step behind which a whole one is copied; what its first rows carry is the rest of the copy begun in the step before it, also whole.
-    auto step = [&](auto main) {
+    auto step = [&](auto main) __attribute__((always_inline)) {
         constexpr bool MAIN = decltype(main)::value;
         read_b(1);
 #pragma unroll

@@ -9,8 +9,11 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
 
 #include "../../include/svip.h"
 
@@ -21,6 +24,8 @@ decltype(&svip_draft_step) g_draft_step;
 decltype(&svip_draft_step_greedy) g_draft_step_greedy;
 decltype(&svip_verify) g_verify;
 decltype(&svip_verify_greedy) g_verify_greedy;
+decltype(&svip_quantize_blocks) g_quantize_blocks;
+decltype(&svip_head_logits) g_head_logits;
 
 // A plain dense device tensor, or nullptr: no subclass, nothing wrapped by a transform (those have no pointer to give).
 const at::Tensor *device_tensor(PyObject *o)
@@ -93,6 +98,18 @@ struct Args {
         }
         if (*stride < 0) *stride = B > 1 ? t->stride(0) : 1;
         return static_cast<T *>(t->data_ptr());
+    }
+    // A matrix with unit stride along its rows on the current device; *stride: between its rows.
+    const at::Tensor *matrix(at::ScalarType type, long long rows, long long cols, long long *stride)
+    {
+        const at::Tensor *t = device_tensor(v[i++]);
+        if (!t || t->dim() != 2 || (type != at::ScalarType::Undefined && t->scalar_type() != type) || (rows >= 0 && t->size(0) != rows) ||
+            (cols >= 0 && t->size(1) != cols) || t->stride(1) != 1 || t->device().index() != c10::hip::current_device()) {
+            ok = false;
+            return nullptr;
+        }
+        *stride = t->size(0) > 1 ? t->stride(0) : std::max<long long>(t->size(1), t->stride(0));
+        return t;
     }
     const at::Tensor *workspace()
     {
@@ -246,15 +263,71 @@ PyObject *verify_greedy(PyObject *, PyObject *const *argv, Py_ssize_t n)
     });
 }
 
-// bind(addresses of svip_draft_step, svip_draft_step_greedy, svip_verify, svip_verify_greedy)
+// quantize_blocks(x, block_rows, q_out, scale_out, stream)
+PyObject *quantize_blocks(PyObject *, PyObject *const *argv, Py_ssize_t n)
+{
+    return answer([&]() -> long {
+        if (n != 5) return DECLINED;
+        Args a{argv};
+        long long sx = 0, sq = 0, ss = 0;
+        const at::Tensor *x = a.matrix(at::ScalarType::Undefined, -1, -1, &sx);
+        if (!a.ok) return DECLINED;
+        const int dtype = dtype_of(*x), block_rows = a.whole(false);
+        const long long rows = x->size(0), cols = x->size(1), kb = (cols + 127) / 128;
+        if (dtype < 0 || (block_rows != 1 && block_rows != 128)) return DECLINED;
+        const at::Tensor *q = a.matrix(at::kFloat8_e4m3fn, rows, kb * 128, &sq);
+        const at::Tensor *s = a.matrix(at::kFloat8_e8m0fnu, (rows + block_rows - 1) / block_rows, kb, &ss);
+        void *stream = a.stream();
+        if (!a.ok || !fits(rows) || !fits(cols)) return DECLINED;
+        const void *xp = x->data_ptr();
+        void *qp = q->data_ptr(), *sp = s->data_ptr();
+        long status;
+        Py_BEGIN_ALLOW_THREADS
+        status = g_quantize_blocks(xp, dtype, (int)rows, (int)cols, sx, block_rows, qp, sq, sp, ss, stream);
+        Py_END_ALLOW_THREADS
+        return status;
+    });
+}
+
+// head_logits(hidden_q, hidden_scale, weight_q, weight_scale, logits_out, workspace, stream)
+PyObject *head_logits(PyObject *, PyObject *const *argv, Py_ssize_t n)
+{
+    return answer([&]() -> long {
+        if (n != 7) return DECLINED;
+        Args a{argv};
+        long long sh = 0, shs = 0, sw = 0, sws = 0, so = 0;
+        const at::Tensor *h = a.matrix(at::kFloat8_e4m3fn, -1, -1, &sh);
+        if (!a.ok) return DECLINED;
+        const long long N = h->size(0), K = h->size(1);
+        const at::Tensor *hs = a.matrix(at::kFloat8_e8m0fnu, N, K / 128, &shs), *w = a.matrix(at::kFloat8_e4m3fn, -1, K, &sw);
+        if (!a.ok) return DECLINED;
+        const long long V = w->size(0);
+        const at::Tensor *ws = a.matrix(at::kFloat8_e8m0fnu, (V + 127) / 128, K / 128, &sws), *out = a.matrix(at::ScalarType::Undefined, N, V, &so);
+        const at::Tensor *space = a.workspace();
+        void *stream = a.stream();
+        if (!a.ok || !fits(N) || !fits(V) || !fits(K) || space->device() != h->device()) return DECLINED;
+        const int dtype = dtype_of(*out);
+        if (dtype < 0) return DECLINED;
+        const void *hp = h->data_ptr(), *hsp = hs->data_ptr(), *wp = w->data_ptr(), *wsp = ws->data_ptr();
+        void *op = out->data_ptr(), *sp = space->data_ptr();
+        const size_t sn = (size_t)space->numel();
+        long status;
+        Py_BEGIN_ALLOW_THREADS
+        status = g_head_logits(hp, hsp, wp, wsp, (int)N, (int)V, (int)K, sh, shs, sw, sws, op, dtype, so, sp, sn, stream);
+        Py_END_ALLOW_THREADS
+        return status;
+    });
+}
+
+// bind(addresses of svip_draft_step, svip_draft_step_greedy, svip_verify, svip_verify_greedy, svip_quantize_blocks, svip_head_logits)
 PyObject *bind(PyObject *, PyObject *const *argv, Py_ssize_t n)
 {
-    void *f[4];
-    if (n != 4) {
-        PyErr_SetString(PyExc_TypeError, "bind takes four addresses");
+    void *f[6];
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "bind takes six addresses");
         return nullptr;
     }
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 6; ++i) {
         f[i] = PyLong_AsVoidPtr(argv[i]);
         if (!f[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: a null address");
@@ -265,6 +338,8 @@ PyObject *bind(PyObject *, PyObject *const *argv, Py_ssize_t n)
     g_draft_step_greedy = reinterpret_cast<decltype(g_draft_step_greedy)>(f[1]);
     g_verify = reinterpret_cast<decltype(g_verify)>(f[2]);
     g_verify_greedy = reinterpret_cast<decltype(g_verify_greedy)>(f[3]);
+    g_quantize_blocks = reinterpret_cast<decltype(g_quantize_blocks)>(f[4]);
+    g_head_logits = reinterpret_cast<decltype(g_head_logits)>(f[5]);
     Py_RETURN_NONE;
 }
 
@@ -273,6 +348,8 @@ PyMethodDef methods[] = {
     {"draft_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(draft_step)), METH_FASTCALL, nullptr},
     {"verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(verify)), METH_FASTCALL, nullptr},
     {"verify_greedy", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(verify_greedy)), METH_FASTCALL, nullptr},
+    {"quantize_blocks", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(quantize_blocks)), METH_FASTCALL, nullptr},
+    {"head_logits", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(head_logits)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "native argument marshalling of binding.py", -1, methods};
 

@@ -51,7 +51,9 @@ using Large = TileShape<256, 256, 2, 4, 2>;            // one workgroup a CU
 using Middle = TileShape<128, 128, 2, 2, 2>;           // two
 using Small = TileShape<128, 64, 4, 1, 3>;             // two: up to 64 rows wait for the weight's bytes, and a tile has them all
 using Few = TileShape<128, 32, 4, 1, 4>;               // two: up to 32 rows
-using Middle8 = TileShape<128, 128, 2, 2, 3>;          // fp32 logits of 8-bit matrices (the tile's bf16 fragments need the registers)
+// of 8-bit matrices (16-bit logits of many rows: Large)
+using Middle8 = TileShape<128, 128, 2, 2, 3>;          // fp32 logits (the tile's bf16 fragments need the registers)
+using Narrow8 = TileShape<64, 32, 4, 1, 4>;            // three: few rows and a vocabulary too small to fill the chip with tiles of 128
 enum ShapeId { LARGE, MIDDLE, SMALL, FEW };
 
 constexpr int FEW_ROWS = 64, FEWER_ROWS = 32;
@@ -483,11 +485,18 @@ svip_status svip_head_logits(const void *hidden_q, const void *hidden_scale, con
     a.out = logits_out;
     a.out_stride = row_stride;
     const bool ok = by_dtype(dtype, [&](auto dt) {
-        return by_shape(N <= FEW_ROWS ? SMALL : LARGE, true, [&](auto shape) {
-            using S = std::conditional_t<std::is_same<decltype(shape), Small>::value, Small, std::conditional_t<decltype(dt)::value == SVIP_F32, Middle8, Large>>;
+        constexpr int DT = decltype(dt)::value;
+        const auto in = [&](auto shape) {
+            using S = decltype(shape);
             a.tiles = {ceil_div(V, S::BM), ceil_div(N, S::BN)};
-            return launch(k_head_logits<S, decltype(dt)::value>, (long long)a.tiles.m * a.tiles.n, S::THREADS, static_cast<hipStream_t>(hip_stream), a);
-        });
+            return launch(k_head_logits<S, DT>, (long long)a.tiles.m * a.tiles.n, S::THREADS, static_cast<hipStream_t>(hip_stream), a);
+        };
+        if (N <= FEWER_ROWS && ceil_div(V, Small::BM) < 2 * CUS) return in(Narrow8{});
+        if (N <= FEW_ROWS) return in(Small{});
+        if constexpr (DT == SVIP_F32)
+            return in(Middle8{});
+        else
+            return in(Large{});
     });
     return ok ? SVIP_OK : SVIP_ERR_HIP;
 }
