@@ -153,12 +153,22 @@ __global__ __launch_bounds__(QUANT_WG) void k_quantize_blocks(QuantizeArgs a)
     const int c = kb * QBLOCK + (threadIdx.x % LANES) * VEC, r0 = rb * QBLOCK + threadIdx.x / LANES;
     float v[ROUNDS][VEC];
     unsigned m = 0u;
+    if ((kb + 1) * QBLOCK <= a.cols) {         // whole columns: rows behind the last are read as the last, all loads under way at once
+        using X = typename Stored<DT>::type;
+        typedef X vec __attribute__((ext_vector_type(VEC)));
+        vec w[ROUNDS];
 #pragma unroll
-    for (int i = 0; i < ROUNDS; ++i) {
-        if (r0 + i * ROWS < a.rows)
-            load_chunk<DT>(a, r0 + i * ROWS, c, v[i]);
-        else
-            for (int j = 0; j < VEC; ++j) v[i][j] = 0.f;
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int r = r0 + i * ROWS < a.rows ? r0 + i * ROWS : a.rows - 1;
+            w[i] = *reinterpret_cast<const vec *>(static_cast<const X *>(a.x) + r * a.row_stride + c);
+        }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i][j] = (float)w[i][j];
+    } else {
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) load_chunk<DT>(a, r0 + i * ROWS < a.rows ? r0 + i * ROWS : a.rows - 1, c, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i)
@@ -887,22 +897,36 @@ struct HeadPackArgs {
     int vocab;
     float *row_inv;            // hidden states for the logits: parts of their own scale for each row
     int whole;                 // fp32 as it is, no parts
+    int row_threads;           // of a workgroup, side by side in a row: a power of two
 };
 template <int DT>
 __device__ __forceinline__ void load_columns(const HeadPackArgs &a, long long r, int c, float (&v)[8])
 {
-    const auto *x = static_cast<const typename Stored<DT>::type *>(a.x) + r * a.stride + c;
+    using X = typename Stored<DT>::type;
+    constexpr int VEC = Stored<DT>::VEC;                   // 16 bytes
+    typedef X vec __attribute__((ext_vector_type(VEC)));
+    const X *x = static_cast<const X *>(a.x) + r * a.stride + c;
+    if (c + 8 <= a.cols) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c + e < a.cols ? (float)x[e] : 0.f;
+        for (int q = 0; q < 8; q += VEC) {
+            const vec w = *reinterpret_cast<const vec *>(x + q);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[q + e] = (float)w[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < a.cols ? (float)x[e] : 0.f;
+    }
 }
 // Eight columns a thread: a weight (fp32), or hidden states weighted for the gradient of the weight.
 template <int DT>
 __global__ __launch_bounds__(256) void k_head_pack(HeadPackArgs a)
 {
-    const int per_row = a.cols_p / 8;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, r = i / per_row;
-    if (r >= a.rows) return;
-    const int c = (int)(i - r * per_row) * 8;
+    const unsigned blocks = (unsigned)(a.cols_p + 8 * a.row_threads - 1) / (unsigned)(8 * a.row_threads), group = blockIdx.x / blocks;
+    const unsigned in_row = threadIdx.x & (unsigned)(a.row_threads - 1);
+    const long long r = (long long)group * (256 / a.row_threads) + threadIdx.x / (unsigned)a.row_threads;
+    const int c = (int)((blockIdx.x - group * blocks) * (unsigned)a.row_threads + in_row) * 8;
+    if (r >= a.rows || c >= a.cols_p) return;
     float v[8];
     load_columns<DT>(a, r, c, v);
     if (a.targets) {

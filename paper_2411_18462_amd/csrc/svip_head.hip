@@ -74,12 +74,12 @@ static ShapeId larger_or_middle(long long m, long long n, double steps)
 {
     return tiles_cost(LARGE, m, n, 1, steps) <= tiles_cost(MIDDLE, m, n, 1, steps) ? LARGE : MIDDLE;
 }
-// of the tiles of logits
-static ShapeId shape_of(int rows, long long vocab, double steps)
+// of the tiles of logits; fp32 as it is comes in no large ones
+static ShapeId shape_of(int rows, long long vocab, double steps, bool large)
 {
     if (rows <= FEWER_ROWS) return FEW;
     if (rows <= FEW_ROWS) return SMALL;
-    return larger_or_middle(vocab, rows, steps);
+    return large ? larger_or_middle(vocab, rows, steps) : MIDDLE;
 }
 // f with the shape of that number, of those that the kernel comes in.
 template <typename F>
@@ -91,9 +91,14 @@ static bool by_shape(ShapeId id, bool few, F f)
     return few && f(Few{});
 }
 
-// f with what the products are made of, their terms and the dtype.  fp32 values of many rows go as two fp16 parts, at a third of the rate of 16-bit
-// values and three times that of fp32 products; of few rows as they are, since laying out a weight's parts would cost more than its
-// products (17 rows, 32000 x 512, loss and gradients: 387 us in parts, 131 us as they are).
+// fp32 values of many rows go as two fp16 parts, at a third of the rate of 16-bit values and three times that of fp32 products; of few rows as they
+// are, since laying out a weight's parts costs more than it saves (us in parts / as they are, 32000 x 1024: loss of 128 rows 203 / 70,
+// 300 rows 235 / 186, 512 rows 239 / 244; loss and gradients of 128 rows 541 / 305, 200 rows 629 / 513, 300 rows 693 / 737; 128256 x 2048: loss of
+// 200 rows 1065 / 944, 300 rows 1261 / 1405, loss and gradients of 128 rows 2896 / 2086, 200 rows 3226 / 3768).
+constexpr int PARTS_LOSS = 256, PARTS_GRAD = 160;
+static bool in_parts(int dtype, int call, int rows) { return dtype == SVIP_F32 && rows > (call == SVIP_HEAD_LOSS_GRAD ? PARTS_GRAD : PARTS_LOSS); }
+
+// f with what the products are made of, their terms and the dtype.
 template <typename F>
 static bool by_product(int dtype, bool parts, F f)
 {
@@ -129,7 +134,7 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
 {
     HeadPlan p = {};
     const bool grad = call == SVIP_HEAD_LOSS_GRAD;
-    p.parts = dtype == SVIP_F32 && N > FEW_ROWS;
+    p.parts = in_parts(dtype, call, N);
     p.planes = p.parts ? 2 : 1;
     p.size = dtype == SVIP_F32 && !p.parts ? 4 : 2;
     p.width = p.parts ? up(D, 8) : D;
@@ -153,7 +158,8 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
         return p;
     }
     const int step = STEP_BYTES / p.size;
-    p.logits = shape_of(N, grad || p.parts ? p.piece : V, terms * ceil_div(D, step));
+    const bool large = p.size == 2;
+    p.logits = shape_of(N, grad || p.parts ? p.piece : V, terms * ceil_div(D, step), large);
     const size_t packed = (size_t)p.planes * N * up(p.width, 8) * p.size;
     // (a loss and its gradient may use one workspace of either's size or more, one after the other: nothing is kept between them)
     p.part = take((size_t)ceil_div(V, LEAST_TILE) * N * sizeof(float2));
@@ -166,7 +172,7 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     if (grad) {
         p.weighted = take(packed);
         p.grad = take((size_t)p.planes * N * p.grad_stride * p.size);
-        p.weight_grad = N <= FEW_ROWS ? MIDDLE : larger_or_middle(D, p.piece, terms * ceil_div(N, step));
+        p.weight_grad = N <= FEW_ROWS || !large ? MIDDLE : larger_or_middle(D, p.piece, terms * ceil_div(N, step));
         // The gradient of the hidden states has few tiles and many steps, which are split where that fills the chip better.
         const int steps = p.piece / step;
         double best = 0.0;
@@ -174,7 +180,7 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
             if (splits > 1 && (size_t)splits * N * p.width * sizeof(float) > SPLIT_BYTES) break;
             for (ShapeId id : {LARGE, MIDDLE}) {
                 const bool few = N <= FEW_ROWS;
-                if (few && id == LARGE) continue;
+                if ((few || !large) && id == LARGE) continue;
                 // few rows: tiles of 128 x all rows, whatever the rows' number; the sums of the splits are read once more in the end
                 const double cost = tiles_cost(id, p.width, few ? 1 : N, splits, terms * ceil_div(steps, splits)) + 4.0 * N * p.width * splits / 3e6;
                 if (best == 0.0 || cost < best) {
@@ -226,6 +232,14 @@ static svip_status check_loss(const LossCall &c, const void *out, int call, size
     return check_workspace(c.ws, ws_bytes, plan(call, c.dtype, c.N, c.V, c.D).bytes);
 }
 
+// Workgroups of k_head_pack; sets the threads to a row.
+static long long pack_grid(HeadPackArgs &a)
+{
+    a.row_threads = 1;
+    while (a.row_threads < 256 && a.row_threads * 8 < a.cols_p) a.row_threads *= 2;
+    return (long long)ceil_div(a.rows, 256 / a.row_threads) * ceil_div(a.cols_p, 8 * a.row_threads);
+}
+
 static HeadScalars *scalars(const LossCall &c) { return reinterpret_cast<HeadScalars *>(c.ws + 256); }
 
 // The scalars that the tiles use, and in fp32 the parts of the hidden states.
@@ -273,7 +287,7 @@ static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, 
         w.out = c.ws + p.weight;
         w.plane = (long long)p.piece * p.width * 2;
         w.sc = scalars(c);
-        if (!launch(k_head_pack<SVIP_F32>, ceil_div((long long)count * (p.width / 8), 256), 256, c.st, w)) return false;
+        if (!launch(k_head_pack<SVIP_F32>, pack_grid(w), 256, c.st, w)) return false;
         a.weight = {w.out, (long long)p.width * 2, w.plane};
         a.hidden = {c.ws + p.hidden_parts, (long long)p.width * 2, (long long)c.N * p.width * 2};
         a.row_inv = reinterpret_cast<const float *>(c.ws + p.rows);
@@ -352,7 +366,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         h.grad_loss = grad_loss;
         h.vocab = c.V;
         if (!by_dtype(c.dtype, [&](auto dt) {
-                return launch(k_head_pack<decltype(dt)::value>, ceil_div((long long)c.N * (wide / 8), 256), 256, c.st, h);
+                return launch(k_head_pack<decltype(dt)::value>, pack_grid(h), 256, c.st, h);
             }))
             return false;
     }
