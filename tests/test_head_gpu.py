@@ -227,3 +227,287 @@ def test_loss_and_gradients(svip, N, V, D, dtype):
     svip.head_loss_grad(h, w, y, temperature=T, lse=lse, grad_loss=r, grad_weight_out=dw2[:V, :D], workspace=ws)
     assert torch.equal(dh2[:N, :D], dh[:N, :D]) and torch.equal(dw2[:V, :D], dw[:V, :D])
     assert svip.workspace_flags(ws) == 0
+
+
+@pytest.mark.parametrize("N,V,D,dtype", [(8192, 40000, 64, "bf16"), (4096, 40000, 64, "f32"), (300, 20000, 4096, "f32"), (2500, 70001, 72, "f16")])
+def test_vocabulary_in_several_pieces(svip, N, V, D, dtype):
+    """Sizes whose softmax (256 MiB a piece) or whose weight's parts do not fit one piece, the last piece shorter than the others."""
+    test_loss_and_gradients(svip, N, V, D, dtype)
+
+
+def run_loss(svip, h, w, y, T=1.0, r=None, ws=None, stream=None):
+    N, D = h.shape
+    ws = svip.new_head_workspace(svip.HEAD_LOSS_GRAD, h.dtype, N, w.shape[0], D) if ws is None else ws
+    out = dict(loss=torch.full((N,), 9.0, device="cuda"), lse=torch.full((N,), 9.0, device="cuda"))
+    svip.head_loss(h, w, y, temperature=T, loss_out=out["loss"], lse_out=out["lse"], workspace=ws, stream=stream)
+    if r is not None:
+        out |= dict(dh=torch.full_like(h, 9.0), dw=torch.full_like(w, 9.0))
+        svip.head_loss_grad(h, w, y, temperature=T, lse=out["lse"], grad_loss=r, grad_hidden_out=out["dh"], grad_weight_out=out["dw"], workspace=ws,
+                            stream=stream)
+    return out
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [20, 200])
+def test_rows_without_a_target_may_hold_anything(svip, dtype, N):
+    V, D = 700, 64
+    h, w, y, r = (t.contiguous() for t in inputs(N, V, D, dtype, 5))
+    none = y < 0
+    assert none.any()
+    want = run_loss(svip, torch.where(none[:, None], torch.zeros_like(h), h), w, y, 1.0, torch.where(none, 0.0, r))
+    big = torch.finfo(h.dtype).max
+    for fill, weight in ((float("nan"), float("nan")), (float("inf"), float("-inf")), (big, 3e38)):
+        got = run_loss(svip, torch.where(none[:, None], torch.full_like(h, fill), h), w, y, 1.0, torch.where(none, torch.full_like(r, weight), r))
+        assert torch.equal(got["loss"], want["loss"]) and torch.equal(got["lse"][~none], want["lse"][~none])
+        assert torch.equal(got["dh"], want["dh"]) and torch.equal(got["dw"], want["dw"])
+    assert (want["loss"][none] == 0).all() and (want["dh"][none] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [3, 100])
+def test_no_row_has_a_target(svip, dtype, N):
+    h, w, y, r = (t.contiguous() for t in inputs(N, 400, 72, dtype, 6))
+    got = run_loss(svip, h, w, torch.full_like(y, -1), 1.0, r)
+    assert (got["loss"] == 0).all() and (got["dh"] == 0).all() and (got["dw"] == 0).all()
+    want = ByDefinition(h, w, torch.zeros_like(y), 1.0, dtype)           # (every row counts there)
+    within(got["lse"], want.lse, want.lse_off, "lse")
+
+
+def test_targets_behind_the_vocabulary_are_flagged_and_count_as_none(svip):
+    h, w, y, r = (t.contiguous() for t in inputs(30, 300, 64, "bf16", 7))
+    bad = y.clone()
+    bad[3], bad[11] = 300, 2 ** 31 - 1
+    y[3] = y[11] = -5
+    ws = svip.new_head_workspace(svip.HEAD_LOSS_GRAD, h.dtype, 30, 300, 64)
+    want, got = run_loss(svip, h, w, y, 1.0, r), run_loss(svip, h, w, bad, 1.0, r, ws)
+    assert all(torch.equal(want[k], got[k]) for k in want)
+    assert svip.workspace_flags(ws) == svip.FLAG_BAD_TOKEN
+    ws2 = svip.new_head_workspace(svip.HEAD_LOSS_GRAD, h.dtype, 30, 300, 64)
+    svip.head_loss_grad(h, w, bad, lse=got["lse"], grad_loss=r, grad_hidden_out=got["dh"], workspace=ws2)
+    assert svip.workspace_flags(ws2) == svip.FLAG_BAD_TOKEN
+
+
+def test_uncounted_gradients_are_zero_and_infinite_weights_of_a_row_reach_everything_it_does(svip):
+    """grad_loss of zero everywhere; and a row of hidden states that is not finite makes its own loss and every gradient of the weight NaN."""
+    h, w, y, r = (t.contiguous() for t in inputs(9, 300, 64, "bf16", 8))
+    y[0] = 5
+    got = run_loss(svip, h, w, y, 1.0, torch.zeros_like(r))
+    assert (got["dh"] == 0).all() and (got["dw"] == 0).all()
+    h[0, 3] = float("nan")
+    got = run_loss(svip, h, w, y, 1.0, r)
+    assert got["loss"][0].isnan() and got["loss"][1:].isfinite().all() and got["dh"][1:].isfinite().all() and got["dw"].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [7, 300])
+def test_gradients_against_differences(svip, dtype, N):
+    """Central differences of the summed loss along random directions, in the fp32 kernels on values that the type holds exactly: the third
+    derivative of a logsumexp along a direction is at most 2 (2 max |change of a logit|)^3."""
+    V, D = 400, 64
+    h, w, y, r = (t.contiguous() for t in inputs(N, V, D, dtype, 9))
+    g = run_loss(svip, h, w, y, 1.0, r)
+    h, w = h.float(), w.float()
+    r = torch.where(y >= 0, r, 0.0)
+    for i, at in enumerate(("dh", "dw")):
+        d = torch.randn(h.shape if at == "dh" else w.shape, device="cuda", generator=gen(i))
+        change = d.double() @ w.double().T if at == "dh" else h.double() @ d.double().T
+        eps = 0.05 / float(change.abs().max())
+        sides = []
+        for s in (eps, -eps):
+            H, W = (h + s * d, w) if at == "dh" else (h, w + s * d)
+            sides.append((ByDefinition(H, W, y, 1.0, "f32"), run_loss(svip, H, W, y)["loss"].double()))
+        got = float(((sides[0][1] - sides[1][1]) * r).sum()) / (2 * eps)
+        want = ByDefinition(h, w, y, 1.0, dtype, r)
+        grad, off = (want.dH, want.dH_off) if at == "dh" else (want.dW, want.dW_off)
+        # the differences' own error: third order, the losses' and the rounding of h + s d
+        third = float(r.abs().sum()) * 2 * (2 * 0.05) ** 3 / 6 / eps
+        losses = float(sum((s[0].loss_off * r.abs()).sum() for s in sides)) / (2 * eps)
+        moved = 2 * U32 * float((grad.abs() * (h if at == "dh" else w).abs()).sum()) / eps
+        analytic = float((g[at].double() * d).sum())
+        assert abs(analytic - got) <= third + losses + moved + float((off * d.abs()).sum()), (at, analytic, got)
+
+
+def test_same_bits_again_in_any_workspace_and_on_any_stream(svip):
+    """Twice, in a larger workspace full of NaN, and two calls at once on streams of their own."""
+    cases = [(*(t.contiguous() for t in inputs(N, V, D, dtype, N)), T) for N, V, D, dtype, T in
+             ((300, 5000, 256, "bf16", 1.0), (40, 3000, 136, "f32", 0.7), (170, 2000, 512, "f32", 1.0), (31, 9000, 64, "f16", 2.0))]
+    want = [run_loss(svip, h, w, y, T, r) for h, w, y, r, T in cases]
+    torch.cuda.synchronize()
+    spaces = []
+    for h, w, y, r, T in cases:
+        n = svip.head_workspace_bytes(svip.HEAD_LOSS_GRAD, h.dtype, h.shape[0], w.shape[0], h.shape[1])
+        ws = torch.full((n + 4096,), 0xff, dtype=torch.uint8, device="cuda")
+        ws[:256] = 0
+        spaces.append(ws)
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = []
+    torch.cuda.synchronize()
+    for (h, w, y, r, T), ws, s in zip(cases, spaces, streams):
+        with torch.cuda.stream(s):
+            got.append(run_loss(svip, h, w, y, T, r, ws))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for k in a:
+            assert torch.equal(a[k], b[k]), k
+    # the stream as an argument
+    h, w, y, r, T = cases[0]
+    s = streams[0]
+    s.wait_stream(torch.cuda.current_stream())
+    out = run_loss(svip, h, w, y, T, r, spaces[0], stream=s)
+    s.synchronize()
+    assert all(torch.equal(out[k], want[0][k]) for k in out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [33, 300])
+def test_replayed_graph(svip, dtype, N):
+    """A drafter's step with the head in 8 bits besides, captured once and replayed over new inputs between eager work: every replay's results
+    are those of eager calls."""
+    V, D = 3000, 256
+    h, w, y, r = (t.contiguous() for t in inputs(N, V, D, dtype, 11))
+    ws, ws8 = svip.new_head_workspace(svip.HEAD_LOSS_GRAD, h.dtype, N, V, D), svip.new_head_workspace(svip.HEAD_LOGITS, h.dtype, N, V, D)
+    out = dict(loss=torch.zeros(N, device="cuda"), lse=torch.zeros(N, device="cuda"), dh=torch.zeros_like(h), dw=torch.zeros_like(w),
+               z=torch.zeros(N, V, dtype=h.dtype, device="cuda"), hq=torch.zeros(N, D, dtype=torch.float8_e4m3fn, device="cuda"),
+               wq=torch.zeros(V, D, dtype=torch.float8_e4m3fn, device="cuda"), hs=torch.zeros(N, D // 128, dtype=torch.uint8, device="cuda"),
+               ws=torch.zeros(-(-V // 128), D // 128, dtype=torch.uint8, device="cuda"))
+
+    def step():
+        svip.head_loss(h, w, y, loss_out=out["loss"], lse_out=out["lse"], workspace=ws)
+        svip.head_loss_grad(h, w, y, lse=out["lse"], grad_loss=r, grad_hidden_out=out["dh"], grad_weight_out=out["dw"], workspace=ws)
+        hs, s = out["hs"].view(torch.float8_e8m0fnu), out["ws"].view(torch.float8_e8m0fnu)
+        svip.quantize_blocks(h, q_out=out["hq"], scale_out=hs)
+        svip.quantize_blocks(w, block_rows=128, q_out=out["wq"], scale_out=s)
+        svip.head_logits(out["hq"], hs, out["wq"], s, logits_out=out["z"], workspace=ws8)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        g = gen(100 + i)
+        h.copy_(torch.randn(N, D, device="cuda", generator=g))
+        w.copy_(torch.randn(V, D, device="cuda", generator=g) * 0.1)
+        y.copy_(torch.randint(-1, V, (N,), device="cuda", generator=g))
+        step()
+        torch.cuda.synchronize()
+        want = {k: v.clone() for k, v in out.items()}
+        for v in out.values():
+            v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in out:
+            assert torch.equal(out[k].view(torch.uint8), want[k].view(torch.uint8)), (i, k)
+
+
+def test_rows_further_apart_than_32_bits_reach(svip):
+    """Rows 2^23 elements (8 bits: 2^24) apart, which puts the last ones past 4 GiB, in inputs and outputs."""
+    N, V, D, far = 40, 300, 128, 1 << 23
+    g = gen(12)
+    space = torch.zeros(V * far, dtype=torch.bfloat16, device="cuda")
+    h, w, y, r = (t.contiguous() for t in inputs(N, V, D, "bf16", 12))
+    want = run_loss(svip, h, w, y, 1.0, r)
+    fw = space.as_strided((V, D), (far, 1))
+    fw.copy_(w)
+    fh = space.as_strided((N, D), (far, 1), 1024)
+    fh.copy_(h)
+    gw, gh = space.as_strided((V, D), (far, 1), 2048), space.as_strided((N, D), (far, 1), 4096)
+    ws = svip.new_head_workspace(svip.HEAD_LOSS_GRAD, h.dtype, N, V, D)
+    loss, lse = torch.zeros(N, device="cuda"), torch.zeros(N, device="cuda")
+    svip.head_loss(fh, fw, y, loss_out=loss, lse_out=lse, workspace=ws)
+    svip.head_loss_grad(fh, fw, y, lse=lse, grad_loss=r, grad_hidden_out=gh, grad_weight_out=gw, workspace=ws)
+    assert torch.equal(loss, want["loss"]) and torch.equal(gh, want["dh"]) and torch.equal(gw, want["dw"])
+    q, s = quantize(svip, w, 128)
+    bytes_ = space.view(torch.uint8)
+    fq = bytes_.as_strided((V, D), (2 * far, 1), 8192)
+    fs = bytes_.as_strided((-(-V // 128), 1), (2 * far, 1), 16384 + 3)
+    svip.quantize_blocks(fw, block_rows=128, q_out=fq.view(torch.float8_e4m3fn), scale_out=fs.view(torch.float8_e8m0fnu))
+    assert torch.equal(fq, q) and torch.equal(fs, s)
+    hq, hs = quantize(svip, h, 1)
+    z = torch.zeros(N, 304, dtype=torch.bfloat16, device="cuda")
+    space8 = svip.new_head_workspace(svip.HEAD_LOGITS, z.dtype, N, V, D)
+    args = (hq.view(torch.float8_e4m3fn), hs.view(torch.float8_e8m0fnu))
+    svip.head_logits(*args, q.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu), logits_out=z[:, :V], workspace=space8)
+    fz = space.as_strided((N, V), (far * 7, 1), 16384)
+    svip.head_logits(*args, fq.view(torch.float8_e4m3fn), fs.view(torch.float8_e8m0fnu), logits_out=fz, workspace=space8)
+    assert torch.equal(fz, z[:, :V])
+    del g
+
+
+# ---- together --------------------------------------------------------------------------------------------------------------------------
+
+def test_a_round_from_the_head_in_8_bits(svip):
+    """Hidden states and weight in 8 bits -> logits -> drafting and verification, as a serving loop chains them; and the training loss of the
+    very numbers that the 8 bits stand for agrees with the logsumexp that the draft step writes."""
+    B, k, V, D = 6, 3, 2051, 384
+    g = gen(13)
+    weight = {m: torch.randn(V, D, device="cuda", generator=g).mul_(1.5 / math.sqrt(D)).bfloat16() for m in ("draft", "target")}
+    hidden = {m: torch.randn(n, D, device="cuda", generator=g).bfloat16() for m, n in (("draft", B * k), ("target", B * (k + 1)))}
+    row = -(-V // 8) * 8
+    logits, value = {}, {}
+    for m in weight:
+        (wq, wsc), (hq, hsc) = quantize(svip, weight[m], 128), quantize(svip, hidden[m], 1)
+        n = hidden[m].shape[0]
+        logits[m] = torch.zeros(n, row, device="cuda")
+        views = (hq.view(torch.float8_e4m3fn), hsc.view(torch.float8_e8m0fnu), wq.view(torch.float8_e4m3fn), wsc.view(torch.float8_e8m0fnu))
+        svip.head_logits(*views, logits_out=logits[m][:, :V], workspace=svip.new_head_workspace(svip.HEAD_LOGITS, torch.float32, n, V, D))
+        value[m] = values(*views[:2], 1)[:, :D], values(*views[2:], 128)[:, :D]
+    draft, target = logits["draft"].view(B, k, row)[..., :V], logits["target"].view(B, k + 1, row)[..., :V]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    u = torch.rand(3, B, k, device="cuda", generator=g)
+    tok, dl = torch.zeros(B, k, **i32), torch.zeros(B, **i32)
+    lse, stop = torch.zeros(B, k, dtype=torch.float64, device="cuda"), torch.zeros(B, dtype=torch.uint8, device="cuda")
+    ws = svip.new_workspace(B, k, V)
+    for j in range(k):
+        svip.draft_step(draft[:, j], temperature=1.0, h=9.0, step_j=j, k_max=k, u_sample=u[0][:, j], stop_in=stop, token_out=tok[:, j],
+                        lse_out=lse[:, j], stop_out=stop, draft_len_out=dl, workspace=ws)
+    nacc, nxt = torch.zeros(B, **i32), torch.zeros(B, **i32)
+    svip.verify(target, draft, temperature=1.0, draft_tokens=tok, draft_len=dl, draft_lse=lse, u_accept=u[1], u_resample=u[2][:, 0].contiguous(),
+                n_accepted_out=nacc, next_token_out=nxt, workspace=ws)
+    assert (dl == k).all() and (tok >= 0).all() and (tok < V).all() and (nxt >= 0).all() and (nxt < V).all() and (nacc <= k).all()
+    h, w = (t.bfloat16() for t in value["draft"])                        # exact: three mantissa bits and a power of two
+    assert torch.equal(h.double(), value["draft"][0]) and torch.equal(w.double(), value["draft"][1])
+    flat = tok.reshape(-1)
+    got = run_loss(svip, h, w, flat, 1.0, torch.full((B * k,), 1.0 / (B * k), device="cuda"))
+    want = ByDefinition(h, w, flat, 1.0, "bf16", torch.full((B * k,), 1.0 / (B * k), device="cuda"))
+    assert ((got["lse"].double() - lse.reshape(-1)).abs() <= 2 * want.lse_off).all()
+    within(got["loss"], want.loss, want.loss_off, "loss")
+    within(got["dh"], want.dH, want.dH_off, "gradient of hidden")
+    within(got["dw"], want.dW, want.dW_off, "gradient of weight")
+
+
+def test_native_and_python_marshalling_agree(svip, monkeypatch):
+    from paper_2411_18462_amd import binding
+
+    h, w, _, _ = inputs(20, 300, 256, "bf16", 14)
+    taken = []
+    real = binding._load_native()
+
+    class Counts:
+        def __getattr__(self, name):
+            def call(*a):
+                status = getattr(real, name)(*a)
+                taken.append((name, status))
+                return status
+            return call
+
+    class Declines:
+        def __getattr__(self, name):
+            return lambda *a: -1
+
+    results = []
+    for native in (Counts(), Declines()):
+        monkeypatch.setattr(binding, "_native", native)
+        (hq, hs), (wq, s) = quantize(svip, h, 1, 16, 2), quantize(svip, w, 128, 32, 1)
+        z = torch.zeros(20, 304, device="cuda")
+        svip.head_logits(hq.view(torch.float8_e4m3fn), hs.view(torch.float8_e8m0fnu), wq.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu),
+                         logits_out=z[:, :300], workspace=svip.new_head_workspace(svip.HEAD_LOGITS, torch.float32, 20, 300, 256))
+        results.append((hq, hs, wq, s, z))
+        with pytest.raises(ValueError):
+            svip.quantize_blocks(h, q_out=hq.view(torch.float8_e4m3fn)[:, :128], scale_out=hs.view(torch.float8_e8m0fnu))
+        with pytest.raises(svip.SvipError):
+            svip.quantize_blocks(h.double(), q_out=hq.view(torch.float8_e4m3fn), scale_out=hs.view(torch.float8_e8m0fnu))
+        with pytest.raises(svip.SvipError, match="ALIGN"):
+            svip.quantize_blocks(h[:, 1:], q_out=hq.view(torch.float8_e4m3fn), scale_out=hs.view(torch.float8_e8m0fnu))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert [t for t in taken if t[1] == 0] == [("quantize_blocks", 0)] * 2 + [("head_logits", 0)]
