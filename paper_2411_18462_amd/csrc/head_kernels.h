@@ -705,7 +705,8 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
 
 struct HeadHiddenFinishArgs {
     const float *sum;
-    int splits, N, D, Dp;      // D of the output, Dp of the sums (both multiples of 4)
+    int splits, slices;        // slices: JOIN_SLICES or 1
+    int N, D, Dp;              // D of the output, Dp of the sums (both multiples of 4)
     const HeadScalars *sc;
     const int *targets;
     const float *grad_loss;
@@ -713,38 +714,39 @@ struct HeadHiddenFinishArgs {
     void *out;
     long long out_stride;
 };
-// The splits' sums, four slices of them side by side: a row's 64 columns of four a workgroup.
+// A workgroup takes 64 columns of four: of one row with four slices of its splits side by side, or, where there are few splits, of four rows.
 constexpr int JOIN_COLUMNS = 64, JOIN_SLICES = 4, JOIN_BATCH = 8;
 template <int DT>
 __global__ __launch_bounds__(JOIN_COLUMNS * JOIN_SLICES) void k_head_hidden_finish(HeadHiddenFinishArgs a)
 {
     __shared__ f32x4 sums[JOIN_SLICES][JOIN_COLUMNS];
-    const int groups = (a.D + 4 * JOIN_COLUMNS - 1) / (4 * JOIN_COLUMNS), n = blockIdx.x / groups;
-    const int column = threadIdx.x % JOIN_COLUMNS, slice = threadIdx.x / JOIN_COLUMNS;
-    const int d = ((blockIdx.x - n * groups) * JOIN_COLUMNS + column) * 4;
-    const bool use = counts(a.targets[n], a.vocab);
+    const int groups = (a.D + 4 * JOIN_COLUMNS - 1) / (4 * JOIN_COLUMNS), group = blockIdx.x / groups;
+    const int column = threadIdx.x % JOIN_COLUMNS, part = threadIdx.x / JOIN_COLUMNS, slice = a.slices == 1 ? 0 : part;
+    const int n = a.slices == 1 ? group * JOIN_SLICES + part : group;
+    const int d = ((blockIdx.x - group * groups) * JOIN_COLUMNS + column) * 4;
+    const bool use = n < a.N && counts(a.targets[n], a.vocab);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (use && d < a.D) {
         const float *p = a.sum + (long long)n * a.Dp + d;
         const long long next = (long long)a.N * a.Dp;
-        for (int k = slice; k < a.splits; k += JOIN_SLICES * JOIN_BATCH) {
+        for (int k = slice; k < a.splits; k += a.slices * JOIN_BATCH) {
             f32x4 v[JOIN_BATCH];
 #pragma unroll
             for (int q = 0; q < JOIN_BATCH; ++q) {
-                const int at = k + q * JOIN_SLICES;
+                const int at = k + q * a.slices;
                 if (at < a.splits) v[q] = *reinterpret_cast<const f32x4 *>(p + at * next);
             }
 #pragma unroll
             for (int q = 0; q < JOIN_BATCH; ++q)
-                if (k + q * JOIN_SLICES < a.splits) s += v[q];
+                if (k + q * a.slices < a.splits) s += v[q];
         }
     }
-    if (a.splits > 1) {
+    if (a.slices > 1) {
         sums[slice][column] = s;
         __syncthreads();
     }
-    if (slice || d >= a.D) return;
-    if (a.splits > 1)
+    if (slice || n >= a.N || d >= a.D) return;
+    if (a.slices > 1)
         for (int k = 1; k < JOIN_SLICES; ++k) s += sums[k][column];
     const float m = use ? a.grad_loss[n] * a.sc->hidden_mult : 0.f;
     Stored<DT>::put4(static_cast<typename Stored<DT>::type *>(a.out) + n * a.out_stride + d, s * m);

@@ -51,7 +51,7 @@ using Large = TileShape<256, 256, 2, 4, 2>;            // one workgroup a CU
 using Middle = TileShape<128, 128, 2, 2, 2>;           // two
 using Small = TileShape<128, 64, 4, 1, 3>;             // two: up to 64 rows wait for the weight's bytes, and a tile has them all
 using Few = TileShape<128, 32, 4, 1, 4>;               // two: up to 32 rows
-// of 8-bit matrices (16-bit logits of many rows: Large)
+// of 8-bit matrices (16-bit logits of many rows: Large and Middle)
 using Middle8 = TileShape<128, 128, 2, 2, 3>;          // fp32 logits (the tile's bf16 fragments need the registers)
 using Narrow8 = TileShape<64, 32, 4, 1, 4>;            // three: few rows and a vocabulary too small to fill the chip with tiles of 128
 enum ShapeId { LARGE, MIDDLE, SMALL, FEW };
@@ -63,16 +63,20 @@ constexpr int LEAST_TILE = 128, MOST_TILE = 256;       // tokens of a tile
 // Time of a product of m x n over `steps` steps, in units of 1 us or so.  A large tile takes 1.4 us a step and 5 us besides, with one workgroup a CU; a
 // middle one, of a quarter of its size, 0.85 us and 5 us, with two.  So many tiles go faster as large ones (loss of 8192 x 151936 x 2048: 3690 us
 // against 4820), and where large ones would leave CUs without work as middle ones (129 x 32000 x 1024: 27 us against 23;
-// gradients of 1000 x 5000 x 1024: 125 us against 91).
-static double tiles_cost(ShapeId id, long long m, long long n, int splits, double steps)
+// gradients of 1000 x 5000 x 1024: 125 us against 91).  8-bit tiles, whose steps are twice as many values, take 1.65 us and 8 us, middle
+// ones 1.08 us and 3.8 us (logits of 1088 x 128256 x 4096: 610 us against 691; 325 x 50257 x 5120: 149 against 135; 100 x 32000 x 1024:
+// 20 against 13).
+static double tiles_cost(ShapeId id, long long m, long long n, int splits, double steps, bool codes = false)
 {
-    const long long size = id == LARGE ? 256 : 128, at_once = id == LARGE ? CUS : 2 * CUS;
+    const bool large = id == LARGE;
+    const long long size = large ? 256 : 128, at_once = large ? CUS : 2 * CUS;
     const long long rounds = ((m + size - 1) / size * ((n + size - 1) / size) * splits + at_once - 1) / at_once;
-    return (double)rounds * (5.0 + (id == LARGE ? 1.4 : 0.85) * steps);
+    const double a_step = codes ? (large ? 1.65 : 1.08) : (large ? 1.4 : 0.85), besides = codes ? (large ? 8.0 : 3.8) : 5.0;
+    return (double)rounds * (besides + a_step * steps);
 }
-static ShapeId larger_or_middle(long long m, long long n, double steps)
+static ShapeId larger_or_middle(long long m, long long n, double steps, bool codes = false)
 {
-    return tiles_cost(LARGE, m, n, 1, steps) <= tiles_cost(MIDDLE, m, n, 1, steps) ? LARGE : MIDDLE;
+    return tiles_cost(LARGE, m, n, 1, steps, codes) <= tiles_cost(MIDDLE, m, n, 1, steps, codes) ? LARGE : MIDDLE;
 }
 // of the tiles of logits; fp32 as it is comes in no large ones
 static ShapeId shape_of(int rows, long long vocab, double steps, bool large)
@@ -434,10 +438,11 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
     }
     if (!out.hidden) return true;
     const int splits = ceil_div(c.V < p.piece ? c.V : p.piece, p.per_split);           // (of the first piece: those that were written)
-    HeadHiddenFinishArgs f = {reinterpret_cast<const float *>(c.ws + p.sum), splits, c.N, c.D, p.width, scalars(c), c.targets, grad_loss, c.V, out.hidden,
+    const int slices = splits < JOIN_SLICES ? 1 : JOIN_SLICES;
+    HeadHiddenFinishArgs f = {reinterpret_cast<const float *>(c.ws + p.sum), splits, slices, c.N, c.D, p.width, scalars(c), c.targets, grad_loss, c.V, out.hidden,
                               out.hidden_stride};
     return by_dtype(c.dtype, [&](auto dt) {
-        return launch(k_head_hidden_finish<decltype(dt)::value>, (long long)c.N * ceil_div(c.D, 4 * JOIN_COLUMNS), JOIN_COLUMNS * JOIN_SLICES, c.st, f);
+        return launch(k_head_hidden_finish<decltype(dt)::value>, (long long)ceil_div(c.N, JOIN_SLICES / slices) * ceil_div(c.D, 4 * JOIN_COLUMNS), JOIN_COLUMNS * JOIN_SLICES, c.st, f);
     });
 }
 
@@ -510,7 +515,7 @@ svip_status svip_head_logits(const void *hidden_q, const void *hidden_scale, con
         if constexpr (DT == SVIP_F32)
             return in(Middle8{});
         else
-            return in(Large{});
+            return larger_or_middle(V, N, K / QBLOCK, true) == LARGE ? in(Large{}) : in(Middle{});
     });
     return ok ? SVIP_OK : SVIP_ERR_HIP;
 }
