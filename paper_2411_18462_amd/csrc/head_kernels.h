@@ -255,6 +255,9 @@ struct HeadLogitsArgs {
     Tiles tiles;
     void *out;
     long long out_stride;      // elements
+    int per_split;             // of K, a multiple of the step
+    float *part;               // [splits][N][part_stride] where there are several, null: one
+    long long part_stride;
 };
 
 constexpr int SCALE_STEPS = 64;                        // steps whose scales are in LDS at a time
@@ -280,9 +283,10 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
     __shared__ __attribute__((aligned(4))) unsigned char scale_bytes[(S::BN + WEIGHT_BLOCKS) * SCALE_PITCH];
     unsigned char *const hs = scale_bytes, *const ws = scale_bytes + S::BN * SCALE_PITCH;
+    const unsigned tiles = (unsigned)a.tiles.m * (unsigned)a.tiles.n, split = blockIdx.x / tiles;
     int tm, tn;
-    tile_of(blockIdx.x, a.tiles, 4, tm, tn);
-    const int v0 = tm * S::BM, n0 = tn * S::BN;
+    tile_of(blockIdx.x - split * tiles, a.tiles, 4, tm, tn);
+    const int v0 = tm * S::BM, n0 = tn * S::BN, k0 = (int)split * a.per_split, k_end = min(a.K, k0 + a.per_split);
     Operand w = a.weight, h = a.hidden;
     w.base += (long long)v0 * w.stride;
     h.base += (long long)n0 * h.stride;
@@ -304,12 +308,12 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     constexpr int COPIES = decltype(sa)::ROUNDS + decltype(sb)::ROUNDS;
-    const int steps = a.K / QBLOCK;
+    const int steps = (k_end - k0) / QBLOCK;
     const unsigned lds0 = (unsigned)(uintptr_t)smem;
     auto copy = [&](int s) {
         const unsigned at = lds0 + (unsigned)(s % S::STAGES) * S::STAGE_BYTES;
-        sa.copy(at, s * QBLOCK, a.K, 0);
-        sb.copy(at + S::BM * STEP_BYTES, s * QBLOCK, a.K, 0);
+        sa.copy(at, k0 + s * QBLOCK, k_end, 0);
+        sb.copy(at + S::BM * STEP_BYTES, k0 + s * QBLOCK, k_end, 0);
     };
     // The scales of SCALE_STEPS steps into LDS, read four at a time, all under way before the first is needed.
     auto scales = [&](int s0) {
@@ -320,8 +324,8 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         for (int k = 0; k < ROUNDS; ++k) {
             const int i = k * S::THREADS + (int)threadIdx.x, r = i / SCALE_WORDS, q = i % SCALE_WORDS;
             const int n = n0 + r < a.N ? n0 + r : a.N - 1, block = v0 / QBLOCK + r - S::BN, last = (a.V - 1) / QBLOCK;
-            const unsigned char *p = r < S::BN ? a.hidden_scale + n * a.hidden_scale_stride
-                                               : a.weight_scale + (block < last ? block : last) * a.weight_scale_stride;
+            const unsigned char *p = (r < S::BN ? a.hidden_scale + n * a.hidden_scale_stride
+                                                : a.weight_scale + (block < last ? block : last) * a.weight_scale_stride) + k0 / QBLOCK;
             word[k] = 0u;
             if (4 * q + 4 <= count)
                 __builtin_memcpy(&word[k], p + s0 + 4 * q, 4);
@@ -384,7 +388,19 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         }
     }
     using X = typename Stored<DT>::type;
-    if constexpr (DT != SVIP_F32) {
+    if (a.part) {
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            const int n = n0 + wn + 16 * j + (lane & 15);
+            if (n >= a.N) continue;
+            float *row = a.part + ((long long)split * a.N + n) * a.part_stride;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int v = v0 + wm + 16 * i + 4 * (lane >> 4);
+                if (v < a.part_stride) *reinterpret_cast<f32x4 *>(row + v) = acc[i][j];       // (V filled up to fours)
+            }
+        }
+    } else if constexpr (DT != SVIP_F32) {
         store_rows<S, X>(smem, a.N - n0, a.V - v0, static_cast<X *>(a.out) + n0 * a.out_stride + v0, a.out_stride, [&](int i, int j) { return acc[i][j]; });
     } else {
 #pragma unroll
@@ -399,6 +415,26 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
             }
         }
     }
+}
+
+struct HeadLogitsJoinArgs {
+    const float *part;
+    long long part_stride;
+    int splits, N, V;
+    void *out;
+    long long out_stride;
+};
+// The sums of the splits of K, four logits a thread.
+template <int DT>
+__global__ __launch_bounds__(256) void k_head_logits_join(HeadLogitsJoinArgs a)
+{
+    const int groups = (int)((a.part_stride + 1023) / 1024), n = blockIdx.x / groups;
+    const int v = ((blockIdx.x - n * groups) * 256 + (int)threadIdx.x) * 4;
+    if (v >= a.V) return;
+    const float *p = a.part + n * a.part_stride + v;
+    f32x4 s = *reinterpret_cast<const f32x4 *>(p);
+    for (int k = 1; k < a.splits; ++k) s += *reinterpret_cast<const f32x4 *>(p + (long long)k * a.N * a.part_stride);
+    put_up_to_4<DT>(static_cast<typename Stored<DT>::type *>(a.out) + n * a.out_stride + v, s, a.V - v);
 }
 
 // ---- cross entropy -------------------------------------------------------------------------------------------------------------------------

@@ -126,7 +126,7 @@ __device__ __forceinline__ double add_halves(double v)
 // Wave-uniform fp64 sum of all 64 lanes' values by the DPP butterfly and two row exchanges (about 24 vector-ALU
 // slots).  The same sum as two v_mfma_f64_16x16x4 against a matrix of ones is exact too and needs 6 slots, but its
 // long dependent latency made every kernel that used it slower (a draft step of 64 rows 12.7 us against 12.2 us,
-// the residual pass 13.45 us against 13.1 us), so the matrix cores stay unused in this library.
+// the residual pass 13.45 us against 13.1 us), so no sum here goes through the matrix cores.
 __device__ __forceinline__ double wave_sum(double v)
 {
     v = row_reduce(v, OpSum{});

@@ -122,7 +122,7 @@ def values(q, s, block_rows):
 
 @pytest.mark.parametrize("N,V,K,out", [(1, 1, 128, "f32"), (1, 1000, 5120, "bf16"), (7, 129, 256, "f16"), (16, 32000, 384, "f32"), (33, 515, 8320, "f32"),
                                        (64, 1283, 1024, "bf16"), (65, 257, 640, "f16"), (130, 2051, 128, "f32"), (257, 1000, 16640, "bf16"),
-                                       (300, 4099, 896, "f16"), (1088, 1500, 512, "bf16")])
+                                       (300, 4099, 896, "f16"), (1088, 1500, 512, "bf16"), (3, 301, 4096, "bf16"), (40, 1999, 2304, "f16"), (20, 777, 16640, "f32")])
 def test_logits(svip, N, V, K, out):
     g, t = gen(N + V + K), TYPES[out]
     hq, hs = eight_bits(N, K, 1, g, 16)
