@@ -416,7 +416,7 @@ size_t svip_head_workspace_bytes(int call, int dtype, int N, int V, int D);
  * scale_out past column K / 128 are not written.  No workspace.
  */
 svip_status svip_quantize_blocks(
-    const void *x, int dtype,        /* device, row r at element offset r * row_stride; 16-byte aligned rows */
+    const void *x, int dtype,        /* device, row r at element offset r * row_stride (any; x on its type's alignment) */
     int rows, int cols, long long row_stride,
     int block_rows,                  /* 1 or 128, else SVIP_ERR_PARAM */
     void *q_out, long long q_stride, /* device [rows, K], bytes; 16-byte aligned rows */

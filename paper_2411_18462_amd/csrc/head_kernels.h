@@ -92,7 +92,8 @@ struct QuantizeArgs {
     long long scale_stride;
 };
 
-// 16 bytes of x from column c of row r on, as floats, zeros past the last column.
+// 16 bytes of x from column c of row r on, as floats, zeros past the last column.  Rows begin wherever their type may: the memory takes a load of
+// 16 bytes at any address.
 template <int DT>
 __device__ __forceinline__ void load_chunk(const QuantizeArgs &a, long long r, int c, float (&v)[Stored<DT>::VEC])
 {
@@ -100,7 +101,7 @@ __device__ __forceinline__ void load_chunk(const QuantizeArgs &a, long long r, i
     using X = typename Stored<DT>::type;
     const X *p = static_cast<const X *>(a.x) + r * a.row_stride + c;
     if (c + VEC <= a.cols) {
-        typedef X vec __attribute__((ext_vector_type(VEC)));
+        typedef X vec __attribute__((ext_vector_type(VEC), aligned(sizeof(X))));
         const vec w = *reinterpret_cast<const vec *>(p);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) v[i] = (float)w[i];
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(QUANT_WG) void k_quantize_blocks(QuantizeArgs a)
     unsigned m = 0u;
     if ((kb + 1) * QBLOCK <= a.cols) {         // whole columns: rows behind the last are read as the last, all loads under way at once
         using X = typename Stored<DT>::type;
-        typedef X vec __attribute__((ext_vector_type(VEC)));
+        typedef X vec __attribute__((ext_vector_type(VEC), aligned(sizeof(X))));
         vec w[ROUNDS];
 #pragma unroll
         for (int i = 0; i < ROUNDS; ++i) {

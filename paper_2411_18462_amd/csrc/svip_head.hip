@@ -95,12 +95,18 @@ static bool by_shape(ShapeId id, bool few, F f)
     return few && f(Few{});
 }
 
-// fp32 values of many rows go as two fp16 parts, at a third of the rate of 16-bit values and three times that of fp32 products; of few rows as they
-// are, since laying out a weight's parts costs more than it saves (us in parts / as they are, 32000 x 1024: loss of 128 rows 203 / 70,
-// 300 rows 235 / 186, 512 rows 239 / 244; loss and gradients of 128 rows 541 / 305, 200 rows 629 / 513, 300 rows 693 / 737; 128256 x 2048: loss of
-// 200 rows 1065 / 944, 300 rows 1261 / 1405, loss and gradients of 128 rows 2896 / 2086, 200 rows 3226 / 3768).
-constexpr int PARTS_LOSS = 256, PARTS_GRAD = 160;
-static bool in_parts(int dtype, int call, int rows) { return dtype == SVIP_F32 && rows > (call == SVIP_HEAD_LOSS_GRAD ? PARTS_GRAD : PARTS_LOSS); }
+// fp32 values go as two fp16 parts, at a third of the rate of 16-bit values and nearly three times that of fp32 products, where that gains more than
+// laying out the parts costs: in us, a few launches and 12 bytes (gradients: 16) for each value of the weight.  Measured, in parts / as they are,
+// 32000 x 1024: loss of 128 rows 203 / 70, 300 rows 235 / 186, 512 rows 239 / 244; loss and gradients of 128 rows 541 / 305, 200 rows 629 / 513,
+// 300 rows 693 / 737; 128256 x 2048: loss of 200 rows 1065 / 944, 300 rows 1261 / 1405, loss and gradients of 128 rows 2896 / 2086, 200 rows
+// 3226 / 3768.
+static bool in_parts(int dtype, int call, int rows, int vocab, int width)
+{
+    const double weight = (double)vocab * width, product = 2.0 * rows * weight;
+    if (dtype != SVIP_F32 || rows <= FEW_ROWS) return false;
+    return call == SVIP_HEAD_LOSS_GRAD ? 100.0 + weight * 16 / 4.2e6 + 9.0 * product / 0.9e9 < 3.0 * product / 115e6
+                                       : 60.0 + weight * 12 / 4.2e6 + 3.0 * product / 1e9 < product / 115e6;
+}
 
 // f with what the products are made of, their terms and the dtype.
 template <typename F>
@@ -152,7 +158,7 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
 {
     HeadPlan p = {};
     const bool grad = call == SVIP_HEAD_LOSS_GRAD;
-    p.parts = in_parts(dtype, call, N);
+    p.parts = in_parts(dtype, call, N, V, D);
     p.planes = p.parts ? 2 : 1;
     p.size = dtype == SVIP_F32 && !p.parts ? 4 : 2;
     p.width = p.parts ? up(D, 8) : D;
@@ -482,7 +488,7 @@ svip_status svip_quantize_blocks(const void *x, int dtype, int rows, int cols, l
     if (rows <= 0 || rows > HEAD_MAX_VOCAB || cols <= 0 || cols > HEAD_MAX_WIDTH || row_stride < cols) return SVIP_ERR_SHAPE;
     const int kb = ceil_div(cols, QBLOCK);
     if (q_stride < (long long)kb * QBLOCK || scale_stride < kb) return SVIP_ERR_SHAPE;
-    if (!aligned16(x) || row_stride * size_of(dtype) % 16 != 0 || !aligned16(q_out) || q_stride % 16 != 0) return SVIP_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(x) % size_of(dtype) != 0 || !aligned16(q_out) || q_stride % 16 != 0) return SVIP_ERR_ALIGN;
     if (block_rows != 1 && block_rows != QBLOCK) return SVIP_ERR_PARAM;
     QuantizeArgs a = {x, row_stride, rows, cols, kb, static_cast<unsigned char *>(q_out), q_stride, static_cast<unsigned char *>(scale_out), scale_stride};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
