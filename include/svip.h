@@ -413,7 +413,7 @@ size_t svip_head_workspace_bytes(int call, int dtype, int N, int V, int D);
  *   q_out[r, c] = x[r, c] / 2^e rounded to e4m3 (OCP: 4 exponent bits, 3 mantissa bits, no infinity), ties to even
  *   scale_out[r / block_rows, c / 128] = e + 127              (e8m0: a power of two)
  * so that the value kept is q * 2^e.  A value that is not finite becomes the code 0x7f (NaN).  Bytes of q_out past column K and of
- * scale_out past column K / 128 are not written.  No workspace.
+ * scale_out past column K / 128 are not written.  No workspace.  rows <= 2^22, cols <= 2^17, fewer than 2^27 runs of 128 columns in all.
  */
 svip_status svip_quantize_blocks(
     const void *x, int dtype,        /* device, row r at element offset r * row_stride (any; x on its type's alignment) */

@@ -467,7 +467,7 @@ def _rows(t, shape, dtype, name):
         raise ValueError(f"{name} must be a matrix" + (f" {list(shape)}" if shape is not None else ""))
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} needs unit stride along its rows")
-    return _ptr(t, dtype, name), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return _ptr(t, dtype, name), t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16      # (of one row there is none: any that is aligned)
 
 
 def _vector(t, n, dtype, name):

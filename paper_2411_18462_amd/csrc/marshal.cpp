@@ -13,8 +13,6 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include <algorithm>
-
 #include "../../include/svip.h"
 
 namespace {
@@ -108,7 +106,7 @@ struct Args {
             ok = false;
             return nullptr;
         }
-        *stride = t->size(0) > 1 ? t->stride(0) : std::max<long long>(t->size(1), t->stride(0));
+        *stride = t->size(0) > 1 ? t->stride(0) : (t->size(1) + 15) / 16 * 16;       // (of one row there is none: any that is aligned)
         return t;
     }
     const at::Tensor *workspace()

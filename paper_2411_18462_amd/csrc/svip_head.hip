@@ -31,6 +31,7 @@ static svip_status check_matrix(const void *p, int dtype, int cols, long long st
 template <typename A>
 static bool launch(void (*kernel)(A), long long grid, unsigned block, hipStream_t st, const A &args)
 {
+    if (grid <= 0 || grid * block > 0xffffffffLL) return false;          // (threads of a launch)
     A copy = args;
     void *argv[] = {&copy};
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)grid), dim3(block), argv, 0, st) == hipSuccess;
@@ -487,7 +488,7 @@ svip_status svip_quantize_blocks(const void *x, int dtype, int rows, int cols, l
     if (!dtype_ok(dtype)) return SVIP_ERR_DTYPE;
     if (rows <= 0 || rows > HEAD_MAX_VOCAB || cols <= 0 || cols > HEAD_MAX_WIDTH || row_stride < cols) return SVIP_ERR_SHAPE;
     const int kb = ceil_div(cols, QBLOCK);
-    if (q_stride < (long long)kb * QBLOCK || scale_stride < kb) return SVIP_ERR_SHAPE;
+    if (q_stride < (long long)kb * QBLOCK || scale_stride < kb || (long long)rows * kb >= 1LL << 27) return SVIP_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(x) % size_of(dtype) != 0 || !aligned16(q_out) || q_stride % 16 != 0) return SVIP_ERR_ALIGN;
     if (block_rows != 1 && block_rows != QBLOCK) return SVIP_ERR_PARAM;
     QuantizeArgs a = {x, row_stride, rows, cols, kb, static_cast<unsigned char *>(q_out), q_stride, static_cast<unsigned char *>(scale_out), scale_stride};

@@ -44,6 +44,7 @@ def test_host_checks_of_the_head():
     assert quantize(dtype=3) == 3 and quantize(dtype=-1) == 3
     assert quantize(rows=0) == 2 and quantize(cols=0) == 2 and quantize(stride=192) == 2 and quantize(qs=240) == 2 and quantize(ss=1) == 2
     assert quantize(rows=(1 << 22) + 1) == 2 and quantize(cols=(1 << 17) + 1, stride=1 << 18, qs=1 << 18, ss=1 << 12) == 2
+    assert quantize(rows=1 << 22, cols=4096, stride=4096, qs=4096, ss=32) == 2
     assert quantize(x=p + 1) == 4 and quantize(x=p + 2, dtype=0) == 4 and quantize(q=p + 8) == 4 and quantize(qs=264) == 4
     assert quantize(block=0) == 6 and quantize(block=64) == 6
 

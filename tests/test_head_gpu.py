@@ -139,6 +139,19 @@ def test_logits(svip, N, V, K, out):
     assert (z[N] == 7).all() and (z[:, V:] == 7).all()                  # nothing behind the last row or between the rows
 
 
+def test_one_row_of_an_odd_vocabulary_needs_no_stride(svip):
+    """[1, V] as torch makes it, V no multiple of 8: there is no second row for a stride to lead to."""
+    g, V, K = gen(2), 1283, 256
+    hq, hs = eight_bits(1, K, 1, g, 0)
+    wq, ws = eight_bits(V, K, 128, g, 0)
+    z, rows = torch.zeros(1, V, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 1288, dtype=torch.bfloat16, device="cuda")
+    workspace = svip.new_head_workspace(svip.HEAD_LOGITS, z.dtype, 2, V, K)
+    svip.head_logits(hq, hs, wq, ws, logits_out=z, workspace=workspace)
+    svip.head_logits(hq.expand(2, K).contiguous(), hs.view(torch.uint8).expand(2, 2).contiguous().view(torch.float8_e8m0fnu), wq, ws,
+                     logits_out=rows[:, :V], workspace=workspace)
+    assert torch.equal(z[0], rows[0, :V]) and torch.equal(z[0], rows[1, :V])
+
+
 def test_logits_nan_code_reaches_its_row_alone(svip):
     g = gen(3)
     hq, hs = eight_bits(5, 256, 1, g, 0)
