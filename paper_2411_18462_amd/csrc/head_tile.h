@@ -212,8 +212,8 @@ struct TileShape {
     static_assert(WM % 16 == 0 && WN % 16 == 0, "whole fragments");
 };
 
-// The loop over K.  TERMS = 1: one plane each.  TERMS = 3: two planes (high and low part) each, and the products
-// low x high, high x low and high x high, the small ones first.
+// The loop over K.  TERMS = 1: one plane each.  TERMS = 2: two planes (high and low part) of B, and the products with low and with high.
+// TERMS = 3: two planes each, and the products low x high, high x low and high x high, the small ones first.
 template <typename T, typename S, int LA, int LB, int TERMS>
 __device__ __forceinline__ void multiply(const Operand &a, int a_rows, const Operand &b, int b_rows, int k0, int k_end, char *smem,
                                          f32x4 (&acc)[S::FM][S::FN])
@@ -246,8 +246,8 @@ __device__ __forceinline__ void multiply(const Operand &a, int a_rows, const Ope
         const int term = TERMS == 1 ? 0 : s / per_term;
         next.k = k0 + (s - term * per_term) * STEP;
         next.at = lds0 + (unsigned)buffer * S::STAGE_BYTES;
-        next.a = sa.step_base(next.k, TERMS == 1 ? 0 : (term == 0));       // plane 0: high, 1: low
-        next.b = sb.step_base(next.k, TERMS == 1 ? 0 : (term == 1));
+        next.a = sa.step_base(next.k, TERMS == 3 && term == 0);       // plane 0: high, 1: low
+        next.b = sb.step_base(next.k, TERMS != 1 && term == TERMS - 2);
     };
     auto copy_part = [&](int p, auto whole) {
         constexpr int A = decltype(sa)::ROUNDS;

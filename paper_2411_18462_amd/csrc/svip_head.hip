@@ -133,6 +133,7 @@ constexpr size_t SPLIT_BYTES = (size_t)128 << 20;
 
 struct HeadPlan {
     bool parts;                // fp32 as two fp16 parts
+    bool fine;                 // 16-bit G' in two parts for the gradient of the weight
     int planes, size, width;   // planes and bytes of what the products are made of; channels of its rows
     int piece;                 // tokens of a piece of the vocabulary, a multiple of MOST_TILE
     ShapeId logits, hidden_grad, weight_grad;
@@ -163,10 +164,12 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     p.planes = p.parts ? 2 : 1;
     p.size = dtype == SVIP_F32 && !p.parts ? 4 : 2;
     p.width = p.parts ? up(D, 8) : D;
+    p.fine = grad && p.size == 2 && !p.parts && N <= FEW_ROWS;
+    const int grad_planes = p.parts || p.fine ? 2 : 1;
     const double terms = p.parts ? 3.0 : 1.0;
     // pieces: of the softmax in the gradient, of the weight's parts in fp32; equal, so that none is a sliver
     long long most = V;
-    if (grad) most = (long long)(PIECE_BYTES / ((size_t)N * p.size * p.planes));
+    if (grad) most = (long long)(PIECE_BYTES / ((size_t)N * p.size * grad_planes));
     if (p.parts) most = most < (long long)(PIECE_BYTES / ((size_t)p.width * 4)) ? most : (long long)(PIECE_BYTES / ((size_t)p.width * 4));
     if (most < LEAST_PIECE) most = LEAST_PIECE;
     p.piece = up(ceil_div(V, ceil_div(V, most)), MOST_TILE);
@@ -198,7 +201,7 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     }
     if (grad) {
         p.weighted = take(packed);
-        p.grad = take((size_t)p.planes * N * p.grad_stride * p.size);
+        p.grad = take((size_t)grad_planes * N * p.grad_stride * p.size);
         p.weight_grad = N <= FEW_ROWS || !large ? MIDDLE : larger_or_middle(D, p.piece, terms * ceil_div(N, step));
         // The gradient of the hidden states has few tiles and many steps, which are split where that fills the chip better.
         const int steps = p.piece / step;
@@ -404,7 +407,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         a.lse = lse;
         a.grad = c.ws + p.grad;
         a.grad_stride = p.grad_stride;
-        a.grad_plane = grad_plane;
+        a.grad_plane = p.parts || (p.fine && out.weight) ? grad_plane : 0;
         const Operand grad = {c.ws + p.grad, p.grad_stride * p.size, grad_plane};
         const bool ok = by_product(c.dtype, p.parts, [&](auto type, auto terms, auto dt) {
             using T = decltype(type);
@@ -449,8 +452,11 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
                 g.sc = scalars(c);
                 g.out = static_cast<char *>(out.weight) + (long long)v0 * out.weight_stride * size;
                 g.out_stride = out.weight_stride;
+                const long long grid = (long long)g.tiles.m * g.tiles.n;
+                if constexpr (DT != SVIP_F32 && std::is_same<S, Middle>::value)
+                    if (p.fine) return launch(k_head_grad_weight<T, S, 2, DT>, grid, S::THREADS, c.st, g);
                 if constexpr (made_of<T, TERMS, S>())
-                    return launch(k_head_grad_weight<T, S, TERMS, DT>, (long long)g.tiles.m * g.tiles.n, S::THREADS, c.st, g);
+                    return launch(k_head_grad_weight<T, S, TERMS, DT>, grid, S::THREADS, c.st, g);
                 else
                     return false;
             };

@@ -242,6 +242,25 @@ def test_loss_and_gradients(svip, N, V, D, dtype):
     assert svip.workspace_flags(ws) == 0
 
 
+@pytest.mark.parametrize("dtype,two_parts", [("bf16", 2.0 ** -16), ("f16", 2.0 ** -22)])
+@pytest.mark.parametrize("N,V,D", [(1, 1000, 64), (2, 4099, 136), (8, 515, 1032), (33, 2051, 72), (64, 300, 520)])
+def test_weight_gradient_of_few_rows_is_rounded_once(svip, N, V, D, dtype, two_parts):
+    """Rows of one weight, whose hidden states need no rounding: G' in two parts is off by u^2 of an entry (fp16: down to 2^-40, half the step of a low
+    part behind its scale), and what remains is the sums' and the result's rounding."""
+    h, w, y, _ = inputs(N, V, D, dtype, N + V)
+    y[0] = V - 1
+    r = torch.full((N,), 0.25, device="cuda")
+    want, got = ByDefinition(h, w, y, 1.0, dtype, r), run_loss(svip, h, w, y, 1.0, r)
+    H, W = torch.where(want.valid[:, None], h.double(), 0.0), w.double()
+    z, f = H @ W.T, torch.where(want.valid, 0.25, 0.0).double()[:, None]
+    p = torch.softmax(z, 1)
+    d = (H.abs() @ W.abs().T).amax(1) * (D + 4) * U32
+    G = p - torch.zeros_like(p).scatter_(1, y.clamp(0, V - 1).long()[:, None], 1.0)
+    off = (torch.expm1(2 * (d + want.lse_off))[:, None] + 4 * U32) * p + two_parts * G.abs() + 2.0 ** -40
+    t = TYPES[dtype]
+    within(got["dw"], want.dW, (off * f).T @ H.abs() + (N + 2) * U32 * ((G.abs() * f).T @ H.abs()) + u(t) * want.dW.abs() + tiny(t), "gradient of weight")
+
+
 @pytest.mark.parametrize("N,V,D,dtype", [(8192, 40000, 64, "bf16"), (4096, 40000, 64, "f32"), (300, 20000, 4096, "f32"), (2500, 70001, 72, "f16")])
 def test_vocabulary_in_several_pieces(svip, N, V, D, dtype):
     """Sizes whose softmax (256 MiB a piece) or whose weight's parts do not fit one piece, the last piece shorter than the others."""
