@@ -51,7 +51,7 @@ static bool by_dtype(int d, F f)
 using Large = TileShape<256, 256, 2, 4, 2>;            // one workgroup a CU
 using Middle = TileShape<128, 128, 2, 2, 2>;           // two
 using Small = TileShape<128, 64, 4, 1, 3>;             // two: up to 64 rows wait for the weight's bytes, and a tile has them all
-using Few = TileShape<128, 32, 4, 1, 4>;               // two: up to 32 rows
+using Few = TileShape<128, 32, 4, 1, 4>;               // two: up to 32 rows; both also for more rows of a small vocabulary
 // of 8-bit matrices (16-bit logits of many rows: Large and Middle)
 using Middle8 = TileShape<128, 128, 2, 2, 3>;          // fp32 logits (the tile's bf16 fragments need the registers)
 using Narrow8 = TileShape<64, 32, 4, 1, 4>;            // three: few rows and a vocabulary too small to fill the chip with tiles of 128
@@ -61,45 +61,53 @@ constexpr int FEW_ROWS = 64, FEWER_ROWS = 32;
 constexpr int CUS = 256;
 constexpr int LEAST_TILE = 128, MOST_TILE = 256;       // tokens of a tile
 
-// Time of a product of m x n over `steps` steps, in units of 1 us or so.  A large tile takes 1.4 us a step and 5 us besides, with one workgroup a CU; a
-// middle one, of a quarter of its size, 0.85 us and 5 us, with two.  So many tiles go faster as large ones (loss of 8192 x 151936 x 2048: 3690 us
-// against 4820), and where large ones would leave CUs without work as middle ones (129 x 32000 x 1024: 27 us against 23;
-// gradients of 1000 x 5000 x 1024: 125 us against 91).  8-bit tiles, whose steps are twice as many values, take 1.65 us and 8 us, middle
+// What the products are made of.
+enum Kind { HALVES, SINGLES, CODES };                  // 16-bit values, fp32 as it is, 8-bit codes
+
+// Time of a product of m x n over `steps` steps, in units of 1 us or so: 5 us, and for each step of a round of tiles what one takes alone on a
+// CU or next to a second one.  16-bit values in large tiles, of which a CU holds one: 1.4 us a step; in smaller ones less for the tile, but more for
+// the product.  So many tiles go faster as large ones (loss of 8192 x 151936 x 2048: 3690 us against 4820), and where large ones would leave CUs
+// without work as smaller ones.  Measured, large / middle / small / few: loss of 129 x 32000 x 1024: 27 / 23 us; 300 x 32000 x 1024: 32.7 / 33.7 / 41.2 /
+// 44.7; 128 x 32000 x 4096: 88 / 65 / 59 / 72; 200 x 8000 x 2048: 44.7 / 28.2 / 18.5 / 21.7; 360 x 1533 x 4064: 82 / 54 / 31 / 27; gradients of 1000 x 5000 x
+// 1024: 125 / 91.  The fp32 instruction keeps a CU busy with one tile, two take twice as long: loss of 128 x 32000 x 1024: middle 70, small 69, few 73 us;
+// 200 x 20000 x 1024: 124 / 99 / 89; 337 x 1164 x 3504: 211 / 115 / 66.  8-bit tiles, whose steps are twice as many values, take 1.65 us and 8 us, middle
 // ones 1.08 us and 3.8 us (logits of 1088 x 128256 x 4096: 610 us against 691; 325 x 50257 x 5120: 149 against 135; 100 x 32000 x 1024:
 // 20 against 13).
-static double tiles_cost(ShapeId id, long long m, long long n, int splits, double steps, bool codes = false)
+static double tiles_cost(Kind kind, ShapeId id, long long m, long long n, int splits, double steps)
 {
-    const bool large = id == LARGE;
-    const long long size = large ? 256 : 128, at_once = large ? CUS : 2 * CUS;
-    const long long rounds = ((m + size - 1) / size * ((n + size - 1) / size) * splits + at_once - 1) / at_once;
-    const double a_step = codes ? (large ? 1.65 : 1.08) : (large ? 1.4 : 0.85), besides = codes ? (large ? 8.0 : 3.8) : 5.0;
-    return (double)rounds * (besides + a_step * steps);
+    static constexpr int BM[] = {Large::BM, Middle::BM, Small::BM, Few::BM}, BN[] = {Large::BN, Middle::BN, Small::BN, Few::BN};
+    static constexpr double ALONE[] = {1.4, 0.7, 0.35, 0.25}, PAIR[] = {1.4, 0.85, 0.5, 0.4}, SINGLE[] = {0.0, 1.85, 0.97, 0.53};
+    const long long tiles = ((m + BM[id] - 1) / BM[id]) * ((n + BN[id] - 1) / BN[id]) * splits, at_once = id == LARGE ? CUS : 2 * CUS;
+    const double rounds = (double)((tiles + at_once - 1) / at_once);
+    if (kind == SINGLES) return 5.0 + (double)((tiles + CUS - 1) / CUS) * SINGLE[id] * steps;
+    if (kind == CODES) return rounds * (id == LARGE ? 8.0 + 1.65 * steps : 3.8 + 1.08 * steps);
+    return rounds * (5.0 + (tiles <= CUS ? ALONE : PAIR)[id] * steps);
 }
-static ShapeId larger_or_middle(long long m, long long n, double steps, bool codes = false)
+static ShapeId fastest(Kind kind, ShapeId first, ShapeId last, long long m, long long n, double steps)
 {
-    return tiles_cost(LARGE, m, n, 1, steps, codes) <= tiles_cost(MIDDLE, m, n, 1, steps, codes) ? LARGE : MIDDLE;
+    ShapeId best = first;
+    for (int id = first + 1; id <= last; ++id)
+        if (tiles_cost(kind, (ShapeId)id, m, n, 1, steps) < tiles_cost(kind, best, m, n, 1, steps)) best = (ShapeId)id;
+    return best;
 }
-// of the tiles of logits; fp32 as it is comes in no large ones
-static ShapeId shape_of(int rows, long long vocab, double steps, bool large)
+// f with the shape of that number, of those from FIRST to LAST.
+template <ShapeId FIRST, ShapeId LAST, typename F>
+static bool by_shape(ShapeId id, F f)
 {
-    if (rows <= FEWER_ROWS) return FEW;
-    if (rows <= FEW_ROWS) return SMALL;
-    return large ? larger_or_middle(vocab, rows, steps) : MIDDLE;
-}
-// f with the shape of that number, of those that the kernel comes in.
-template <typename F>
-static bool by_shape(ShapeId id, bool few, F f)
-{
-    if (id == LARGE) return f(Large{});
+    if constexpr (FIRST <= LARGE)
+        if (id == LARGE) return f(Large{});
     if (id == MIDDLE) return f(Middle{});
-    if (few && id == SMALL) return f(Small{});
-    return few && f(Few{});
+    if constexpr (LAST >= SMALL)
+        if (id == SMALL) return f(Small{});
+    if constexpr (LAST >= FEW)
+        if (id == FEW) return f(Few{});
+    return false;
 }
 
 // fp32 values go as two fp16 parts, at a third of the rate of 16-bit values and nearly three times that of fp32 products, where that gains more than
 // laying out the parts costs: in us, a few launches and 12 bytes (gradients: 16) for each value of the weight.  Measured, in parts / as they are,
-// 32000 x 1024: loss of 128 rows 203 / 70, 300 rows 235 / 186, 512 rows 239 / 244; loss and gradients of 128 rows 541 / 305, 200 rows 629 / 513,
-// 300 rows 693 / 737; 128256 x 2048: loss of 200 rows 1065 / 944, 300 rows 1261 / 1405, loss and gradients of 128 rows 2896 / 2086, 200 rows
+// 32000 x 1024: loss of 128 rows 203 / 70, 300 rows 235 / 159, 512 rows 239 / 244; loss and gradients of 128 rows 541 / 300, 200 rows 629 / 513,
+// 300 rows 693 / 737 (604 with the loss as it is and the gradients in parts); 128256 x 2048: loss of 200 rows 1065 / 944, 300 rows 1261 / 1405, loss and gradients of 128 rows 2896 / 2086, 200 rows
 // 3226 / 3768.
 static bool in_parts(int dtype, int call, int rows, int vocab, int width)
 {
@@ -119,9 +127,11 @@ static bool by_product(int dtype, bool parts, F f)
     if (parts) return f(F16{}, std::integral_constant<int, 3>{}, std::integral_constant<int, SVIP_F32>{});
     return f(F32{}, one, std::integral_constant<int, SVIP_F32>{});
 }
-// The shapes a kernel of these products comes in: fp32 as it is only for few rows, in parts only for many.
-template <typename T, int TERMS, typename S>
-constexpr bool made_of() { return TERMS == 3 ? S::BN >= 128 : (!std::is_same<T, F32>::value || S::BN <= 128); }
+// The shapes that products of these come in: fp32 as it is in no large ones, in parts in no small ones.
+template <typename T, int TERMS>
+constexpr ShapeId first_shape() { return std::is_same<T, F32>::value ? MIDDLE : LARGE; }
+template <typename T, int TERMS>
+constexpr ShapeId last_shape() { return TERMS == 3 ? MIDDLE : FEW; }
 
 // ---- workspace ---------------------------------------------------------------------------------------------------------------------------------
 
@@ -188,8 +198,10 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
         return p;
     }
     const int step = STEP_BYTES / p.size;
-    const bool large = p.size == 2;
-    p.logits = shape_of(N, grad || p.parts ? p.piece : V, terms * ceil_div(D, step), large);
+    const bool few = N <= FEW_ROWS;
+    const Kind kind = p.size == 2 ? HALVES : SINGLES;
+    const ShapeId first = kind == HALVES ? LARGE : MIDDLE, last = p.parts ? MIDDLE : FEW;
+    p.logits = N <= FEWER_ROWS ? FEW : few ? SMALL : fastest(kind, first, last, grad || p.parts ? p.piece : V, N, terms * ceil_div(D, step));
     const size_t packed = (size_t)p.planes * N * up(p.width, 8) * p.size;
     // (a loss and its gradient may use one workspace of either's size or more, one after the other: nothing is kept between them)
     p.part = take((size_t)ceil_div(V, LEAST_TILE) * N * sizeof(float2));
@@ -202,17 +214,17 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     if (grad) {
         p.weighted = take(packed);
         p.grad = take((size_t)grad_planes * N * p.grad_stride * p.size);
-        p.weight_grad = N <= FEW_ROWS || !large ? MIDDLE : larger_or_middle(D, p.piece, terms * ceil_div(N, step));
+        p.weight_grad = few ? MIDDLE : fastest(kind, first, kind == HALVES ? MIDDLE : FEW, D, p.piece, terms * ceil_div(N, step));
         // The gradient of the hidden states has few tiles and many steps, which are split where that fills the chip better.
         const int steps = p.piece / step;
         double best = 0.0;
         for (int splits = 1; splits <= MOST_SPLITS && (splits == 1 || steps / splits >= 8); ++splits) {
             if (splits > 1 && (size_t)splits * N * p.width * sizeof(float) > SPLIT_BYTES) break;
             for (ShapeId id : {LARGE, MIDDLE}) {
-                const bool few = N <= FEW_ROWS;
-                if ((few || !large) && id == LARGE) continue;
-                // few rows: tiles of 128 x all rows, whatever the rows' number; the sums of the splits are read once more in the end
-                const double cost = tiles_cost(id, p.width, few ? 1 : N, splits, terms * ceil_div(steps, splits)) + 4.0 * N * p.width * splits / 3e6;
+                if (id < (few ? MIDDLE : first)) continue;
+                // few rows: tiles of 128 x all rows, whatever the rows' number and type, which wait for the weight's bytes; the sums of the splits are
+                // read once more in the end
+                const double cost = tiles_cost(few ? HALVES : kind, id, p.width, few ? 1 : N, splits, terms * ceil_div(steps, splits)) + 4.0 * N * p.width * splits / 3e6;
                 if (best == 0.0 || cost < best) {
                     best = cost;
                     p.hidden_grad = few ? p.logits : id;
@@ -350,16 +362,13 @@ static bool run_loss(const LossCall &c, const HeadPlan &p, float *loss, float *l
         HeadArgs a;
         if (!piece_args(c, p, v0, count, &a)) return false;
         const bool ok = by_product(c.dtype, p.parts, [&](auto type, auto terms, auto) {
-            return by_shape(p.logits, true, [&](auto shape) {
+            using T = decltype(type);
+            constexpr int TERMS = decltype(terms)::value;
+            return by_shape<first_shape<T, TERMS>(), last_shape<T, TERMS>()>(p.logits, [&](auto shape) {
                 using S = decltype(shape);
-                using T = decltype(type);
-                constexpr int TERMS = decltype(terms)::value;
                 a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
                 records = v0 / S::BM + a.tiles.m;
-                if constexpr (made_of<T, TERMS, S>())
-                    return launch(k_head_stats<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
-                else
-                    return false;
+                return launch(k_head_stats<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
             });
         });
         if (!ok) return false;
@@ -412,14 +421,12 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         const bool ok = by_product(c.dtype, p.parts, [&](auto type, auto terms, auto dt) {
             using T = decltype(type);
             constexpr int TERMS = decltype(terms)::value, DT = decltype(dt)::value;
+            constexpr ShapeId FIRST = first_shape<T, TERMS>(), LAST = last_shape<T, TERMS>();
             // launches a kernel in a shape, `tiles` its tiles along m and n
             const auto softmax = [&](auto shape) {
                 using S = decltype(shape);
                 a.tiles = {ceil_div(count, S::BM), ceil_div(c.N, S::BN)};
-                if constexpr (made_of<T, TERMS, S>())
-                    return launch(k_head_softmax<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
-                else
-                    return false;
+                return launch(k_head_softmax<T, S, TERMS>, (long long)a.tiles.m * a.tiles.n, S::THREADS, c.st, a);
             };
             const auto grad_hidden = [&](auto shape) {
                 using S = decltype(shape);
@@ -434,10 +441,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
                 g.per_split = p.per_split;
                 g.first = v0 == 0;
                 g.sum = reinterpret_cast<float *>(c.ws + p.sum);
-                if constexpr (made_of<T, TERMS, S>())
-                    return launch(k_head_grad_hidden<T, S, TERMS>, (long long)g.tiles.m * g.tiles.n * g.splits, S::THREADS, c.st, g);
-                else
-                    return false;
+                return launch(k_head_grad_hidden<T, S, TERMS>, (long long)g.tiles.m * g.tiles.n * g.splits, S::THREADS, c.st, g);
             };
             const auto grad_weight = [&](auto shape) {
                 using S = decltype(shape);
@@ -455,13 +459,10 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
                 const long long grid = (long long)g.tiles.m * g.tiles.n;
                 if constexpr (DT != SVIP_F32 && std::is_same<S, Middle>::value)
                     if (p.fine) return launch(k_head_grad_weight<T, S, 2, DT>, grid, S::THREADS, c.st, g);
-                if constexpr (made_of<T, TERMS, S>())
-                    return launch(k_head_grad_weight<T, S, TERMS, DT>, grid, S::THREADS, c.st, g);
-                else
-                    return false;
+                return launch(k_head_grad_weight<T, S, TERMS, DT>, grid, S::THREADS, c.st, g);
             };
-            return by_shape(p.logits, true, softmax) && (!out.hidden || by_shape(p.hidden_grad, true, grad_hidden)) &&
-                   (!out.weight || by_shape(p.weight_grad, false, grad_weight));
+            return by_shape<FIRST, LAST>(p.logits, softmax) && (!out.hidden || by_shape<FIRST, LAST>(p.hidden_grad, grad_hidden)) &&
+                   (!out.weight || by_shape<FIRST, std::is_same<T, F32>::value ? FEW : MIDDLE>(p.weight_grad, grad_weight));
         });
         if (!ok) return false;
     }
@@ -549,7 +550,7 @@ svip_status svip_head_logits(const void *hidden_q, const void *hidden_scale, con
         if constexpr (DT == SVIP_F32)
             return in(Middle8{});
         else
-            return larger_or_middle(V, N, K / QBLOCK, true) == LARGE ? in(Large{}) : in(Middle{});
+            return fastest(CODES, LARGE, MIDDLE, V, N, K / QBLOCK) == LARGE ? in(Large{}) : in(Middle{});
     });
     if (!ok) return SVIP_ERR_HIP;
     if (p.splits == 1) return SVIP_OK;

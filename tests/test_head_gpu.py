@@ -280,6 +280,13 @@ def run_loss(svip, h, w, y, T=1.0, r=None, ws=None, stream=None):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,D", [(66, 130, 2056), (129, 1000, 1032), (337, 1164, 3504), (700, 1200, 328), (200, 20000, 520)])
+def test_many_rows_of_a_small_vocabulary(svip, N, V, D, dtype):
+    """Sizes whose logits come in narrow tiles, several along the rows, the last of them short."""
+    test_loss_and_gradients(svip, N, V, D, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N", [20, 200])
 def test_rows_without_a_target_may_hold_anything(svip, dtype, N):
     V, D = 700, 64
