@@ -52,32 +52,35 @@ using Large = TileShape<256, 256, 2, 4, 2>;            // one workgroup a CU
 using Middle = TileShape<128, 128, 2, 2, 2>;           // two
 using Small = TileShape<128, 64, 4, 1, 3>;             // two: up to 64 rows wait for the weight's bytes, and a tile has them all
 using Few = TileShape<128, 32, 4, 1, 4>;               // two: up to 32 rows; both also for more rows of a small vocabulary
+using Narrow = TileShape<64, 32, 4, 1, 4>;             // three: 8-bit and fp32 logits of a vocabulary too small to fill the chip with tiles of 128
 // of 8-bit matrices (16-bit logits of many rows: Large and Middle)
 using Middle8 = TileShape<128, 128, 2, 2, 3>;          // fp32 logits (the tile's bf16 fragments need the registers)
-using Narrow8 = TileShape<64, 32, 4, 1, 4>;            // three: few rows and a vocabulary too small to fill the chip with tiles of 128
-enum ShapeId { LARGE, MIDDLE, SMALL, FEW };
+enum ShapeId { LARGE, MIDDLE, SMALL, FEW, NARROW };
 
 constexpr int FEW_ROWS = 64, FEWER_ROWS = 32;
 constexpr int CUS = 256;
-constexpr int LEAST_TILE = 128, MOST_TILE = 256;       // tokens of a tile
+constexpr int MOST_TILE = 256;                         // tokens of a tile
 
 // What the products are made of.
 enum Kind { HALVES, SINGLES, CODES };                  // 16-bit values, fp32 as it is, 8-bit codes
 
+static int tile_rows(ShapeId id) { return id == LARGE ? Large::BM : id == NARROW ? Narrow::BM : Middle::BM; }
 // Time of a product of m x n over `steps` steps, in units of 1 us or so: 5 us, and for each step of a round of tiles what one takes alone on a
 // CU or next to a second one.  16-bit values in large tiles, of which a CU holds one: 1.4 us a step; in smaller ones less for the tile, but more for
 // the product.  So many tiles go faster as large ones (loss of 8192 x 151936 x 2048: 3690 us against 4820), and where large ones would leave CUs
 // without work as smaller ones.  Measured, large / middle / small / few: loss of 129 x 32000 x 1024: 27 / 23 us; 300 x 32000 x 1024: 32.7 / 33.7 / 41.2 /
 // 44.7; 128 x 32000 x 4096: 88 / 65 / 59 / 72; 200 x 8000 x 2048: 44.7 / 28.2 / 18.5 / 21.7; 360 x 1533 x 4064: 82 / 54 / 31 / 27; gradients of 1000 x 5000 x
 // 1024: 125 / 91.  The fp32 instruction keeps a CU busy with one tile, two take twice as long: loss of 128 x 32000 x 1024: middle 70, small 69, few 73 us;
-// 200 x 20000 x 1024: 124 / 99 / 89; 337 x 1164 x 3504: 211 / 115 / 66.  8-bit tiles, whose steps are twice as many values, take 1.65 us and 8 us, middle
+// 200 x 20000 x 1024: 124 / 99 / 89; 337 x 1164 x 3504: 211 / 115 / 66, narrow 41; loss and gradients of 700 x 1200 x 1024 with the weight's in middle / small /
+// few: 130 / 108 / 106, of 128 x 32000 x 1024: 299 / 304 / 319.  8-bit tiles, whose steps are twice as many values, take 1.65 us and 8 us, middle
 // ones 1.08 us and 3.8 us (logits of 1088 x 128256 x 4096: 610 us against 691; 325 x 50257 x 5120: 149 against 135; 100 x 32000 x 1024:
 // 20 against 13).
 static double tiles_cost(Kind kind, ShapeId id, long long m, long long n, int splits, double steps)
 {
-    static constexpr int BM[] = {Large::BM, Middle::BM, Small::BM, Few::BM}, BN[] = {Large::BN, Middle::BN, Small::BN, Few::BN};
-    static constexpr double ALONE[] = {1.4, 0.7, 0.35, 0.25}, PAIR[] = {1.4, 0.85, 0.5, 0.4}, SINGLE[] = {0.0, 1.85, 0.97, 0.53};
-    const long long tiles = ((m + BM[id] - 1) / BM[id]) * ((n + BN[id] - 1) / BN[id]) * splits, at_once = id == LARGE ? CUS : 2 * CUS;
+    static constexpr int BN[] = {Large::BN, Middle::BN, Small::BN, Few::BN, Narrow::BN};
+    static constexpr double ALONE[] = {1.4, 0.7, 0.35, 0.25}, PAIR[] = {1.4, 0.85, 0.5, 0.4}, SINGLE[] = {0.0, 1.85, 0.97, 0.53, 0.29};
+    const int rows = tile_rows(id);
+    const long long tiles = ((m + rows - 1) / rows) * ((n + BN[id] - 1) / BN[id]) * splits, at_once = id == LARGE ? CUS : 2 * CUS;
     const double rounds = (double)((tiles + at_once - 1) / at_once);
     if (kind == SINGLES) return 5.0 + (double)((tiles + CUS - 1) / CUS) * SINGLE[id] * steps;
     if (kind == CODES) return rounds * (id == LARGE ? 8.0 + 1.65 * steps : 3.8 + 1.08 * steps);
@@ -101,6 +104,8 @@ static bool by_shape(ShapeId id, F f)
         if (id == SMALL) return f(Small{});
     if constexpr (LAST >= FEW)
         if (id == FEW) return f(Few{});
+    if constexpr (LAST >= NARROW)
+        if (id == NARROW) return f(Narrow{});
     return false;
 }
 
@@ -131,7 +136,7 @@ static bool by_product(int dtype, bool parts, F f)
 template <typename T, int TERMS>
 constexpr ShapeId first_shape() { return std::is_same<T, F32>::value ? MIDDLE : LARGE; }
 template <typename T, int TERMS>
-constexpr ShapeId last_shape() { return TERMS == 3 ? MIDDLE : FEW; }
+constexpr ShapeId last_shape() { return TERMS == 3 ? MIDDLE : std::is_same<T, F32>::value ? NARROW : FEW; }
 
 // ---- workspace ---------------------------------------------------------------------------------------------------------------------------------
 
@@ -158,7 +163,7 @@ static bool narrow_logits(int N, int V) { return N <= FEWER_ROWS && ceil_div(V, 
 static int logits_splits(int N, int V, int K, int *per_split)
 {
     const int steps = ceil_div(K, QBLOCK);
-    const long long tiles = narrow_logits(N, V) ? ceil_div(V, Narrow8::BM) : ceil_div(V, Small::BM), places = narrow_logits(N, V) ? 3 * CUS : 2 * CUS;
+    const long long tiles = narrow_logits(N, V) ? ceil_div(V, Narrow::BM) : ceil_div(V, Small::BM), places = narrow_logits(N, V) ? 3 * CUS : 2 * CUS;
     long long splits = N <= FEW_ROWS ? places / tiles : 1;
     if (splits > steps / 8) splits = steps / 8;
     if (splits < 1) splits = 1;
@@ -200,11 +205,11 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     const int step = STEP_BYTES / p.size;
     const bool few = N <= FEW_ROWS;
     const Kind kind = p.size == 2 ? HALVES : SINGLES;
-    const ShapeId first = kind == HALVES ? LARGE : MIDDLE, last = p.parts ? MIDDLE : FEW;
+    const ShapeId first = kind == HALVES ? LARGE : MIDDLE, last = p.parts ? MIDDLE : kind == HALVES ? FEW : NARROW;
     p.logits = N <= FEWER_ROWS ? FEW : few ? SMALL : fastest(kind, first, last, grad || p.parts ? p.piece : V, N, terms * ceil_div(D, step));
     const size_t packed = (size_t)p.planes * N * up(p.width, 8) * p.size;
     // (a loss and its gradient may use one workspace of either's size or more, one after the other: nothing is kept between them)
-    p.part = take((size_t)ceil_div(V, LEAST_TILE) * N * sizeof(float2));
+    p.part = take((size_t)ceil_div(V, tile_rows(p.logits)) * N * sizeof(float2));
     p.target = take((size_t)N * sizeof(float));
     if (p.parts) {
         p.rows = take((size_t)N * sizeof(float));
@@ -461,7 +466,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
                     if (p.fine) return launch(k_head_grad_weight<T, S, 2, DT>, grid, S::THREADS, c.st, g);
                 return launch(k_head_grad_weight<T, S, TERMS, DT>, grid, S::THREADS, c.st, g);
             };
-            return by_shape<FIRST, LAST>(p.logits, softmax) && (!out.hidden || by_shape<FIRST, LAST>(p.hidden_grad, grad_hidden)) &&
+            return by_shape<FIRST, LAST>(p.logits, softmax) && (!out.hidden || by_shape<FIRST, LAST == NARROW ? FEW : LAST>(p.hidden_grad, grad_hidden)) &&
                    (!out.weight || by_shape<FIRST, std::is_same<T, F32>::value ? FEW : MIDDLE>(p.weight_grad, grad_weight));
         });
         if (!ok) return false;
@@ -545,7 +550,7 @@ svip_status svip_head_logits(const void *hidden_q, const void *hidden_scale, con
             a.tiles = {ceil_div(V, S::BM), ceil_div(N, S::BN)};
             return launch(k_head_logits<S, DT>, (long long)a.tiles.m * a.tiles.n * p.splits, S::THREADS, st, a);
         };
-        if (narrow_logits(N, V)) return in(Narrow8{});
+        if (narrow_logits(N, V)) return in(Narrow{});
         if (N <= FEW_ROWS) return in(Small{});
         if constexpr (DT == SVIP_F32)
             return in(Middle8{});
