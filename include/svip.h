@@ -463,7 +463,8 @@ svip_status svip_head_loss(
  *   grad_hidden_out = G weight        grad_weight_out = G^T hidden
  * Either output may be NULL and is then not computed (a frozen head).  lse is svip_head_loss's; the logits are computed again, in pieces of the vocabulary, and the
  * difference of softmax and one-hot is held for one piece, in bf16 (bf16 inputs), in fp16 times 2^15 (fp16) or in two such
- * parts (fp32); for the weight's gradient of up to 64 rows, where its rounding would not even out, 16-bit types hold it in two parts too.  Rows without a target get gradients of zero and add none, whatever they and their grad_loss hold.
+ * parts (fp32); for the weight's gradient of up to 64 rows, where its rounding would not even out, 16-bit types hold it in
+ * two parts too.  Rows without a target get gradients of zero and add none, whatever they and their grad_loss hold.
  * The outputs must not overlap the inputs.
  */
 svip_status svip_head_loss_grad(
