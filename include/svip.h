@@ -463,8 +463,11 @@ svip_status svip_head_loss(
  *   grad_hidden_out = G weight        grad_weight_out = G^T hidden
  * Either output may be NULL and is then not computed (a frozen head).  lse is svip_head_loss's; the logits are computed again, in pieces of the vocabulary, and the
  * difference of softmax and one-hot is held for one piece, in bf16 (bf16 inputs), in fp16 times 2^15 (fp16) or in two such
- * parts (fp32); for the weight's gradient of up to 64 rows, where its rounding would not even out, 16-bit types hold it in
- * two parts too.  Rows without a target get gradients of zero and add none, whatever they and their grad_loss hold.
+ * parts (fp32).  The hidden states that the weight's gradient sums are multiplied by grad_loss relative to the largest and rounded to their type
+ * (fp32: in parts as above), which changes nothing where all rows have one grad_loss.  For up to 64 rows, where such roundings would not
+ * even out, 16-bit types hold the difference in two parts, times the mantissa of grad_loss, and the hidden states are multiplied by its power of two
+ * alone.  In fp16 and in parts of fp32 the weighted hidden states keep, besides their type's precision, 2^-38 of the largest |grad_loss x hidden|.
+ * Rows without a target get gradients of zero and add none, whatever they and their grad_loss hold.
  * The outputs must not overlap the inputs.
  */
 svip_status svip_head_loss_grad(

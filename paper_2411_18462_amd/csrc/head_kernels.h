@@ -444,12 +444,27 @@ __global__ __launch_bounds__(256) void k_head_logits_join(HeadLogitsJoinArgs a)
 // What the calls of a loss and its gradient compute once for all tiles, in the workspace.
 struct HeadScalars {
     float to_log2;             // accumulated products -> logits / T in units of log 2
-    float grad_top;            // largest |grad_loss| of a row that counts
+    float grad_top;            // largest finite |grad_loss| of a row that counts
     float hidden_mult;         // accumulated G' W -> gradient of the hidden states per grad_loss
-    float weight_mult;         // accumulated G'^T (H grad_loss / grad_top) -> gradient of the weight
-    float hidden_parts, weight_parts;      // fp32: what the parts of the weighted hidden states and of the weight are multiplied by
-    unsigned hidden_max, weight_max;       // fp32: largest finite magnitudes (bits), of hidden states in rows that count
+    float weight_mult;         // accumulated G'^T (weighted H) -> gradient of the weight
+    float weight_parts;        // fp32: what the parts of the weight are multiplied by
+    int weighted_shift;        // of the weighted hidden states: k_head_pack
 };
+
+// A row's weight in the loss, grad_loss, as m 2^e with 1/2 < |m| <= 1.
+constexpr int NO_EXPONENT = -(1 << 20);                // of zero and of what is not finite: below all others
+__device__ __forceinline__ bool is_finite(float g) { return (__float_as_uint(g) & 0x7f800000u) != 0x7f800000u; }
+__device__ __forceinline__ int weight_exponent(float g)
+{
+    if (g == 0.f || !is_finite(g)) return NO_EXPONENT;
+    const int e = __builtin_amdgcn_frexp_expf(g) - (fabsf(__builtin_amdgcn_frexp_mantf(g)) == 0.5f);
+    return e < 127 ? e : 127;                          // (|m| < 2 where 2^128 would be no fp32 number)
+}
+__device__ __forceinline__ float weight_mantissa(float g)
+{
+    const int e = weight_exponent(g);
+    return e == NO_EXPONENT ? (g == 0.f ? 0.f : 1.f) : __builtin_amdgcn_ldexpf(g, -e);
+}
 
 struct HeadArgs {
     Operand weight, hidden;    // of the tile kernels: m = vocabulary of the piece, n = rows
@@ -463,9 +478,12 @@ struct HeadArgs {
     float2 *part;              // [tiles of the vocabulary][N] (largest, sum of exp2 relative to it), base 2
     float *target_logit;       // [N] logits / T of the targets, base 2
     const float *lse;          // [N]
-    char *grad;                // [planes][N][grad_stride]: softmax - one-hot of the piece
+    const float *grad_loss;    // [N]
+    char *grad;                // [planes][N][grad_stride]: softmax - one-hot of the piece; null: not wanted
+    char *weighted;            // up to 64 rows in 16 bits: [2][N][grad_stride], the same times m of the rows' weights in two parts; null: not wanted
     long long grad_stride;     // elements
     long long grad_plane;      // bytes
+    int low_plane;             // whether `grad` has a second plane, of low parts
     int vocab;                 // tokens in all
     unsigned *flags;
 };
@@ -630,8 +648,11 @@ __global__ __launch_bounds__(FINISH_WG) static void k_head_finish(HeadFinishArgs
 // G' = softmax - one-hot of a tile of recomputed logits, rows without a target zero, in the products' type.  Its entries reach from 1 down to
 // nothing: fp16 (and the two parts of an fp32 value) carry them times 2^15, which keeps 11 bits down to 2^-29.  bf16 keeps its 8 bits
 // at any magnitude: its rounding, at most 2^-8 of a value, is of the size of the rounding of the gradients themselves.  In a sum over many rows these roundings
-// even out; the weight's gradient of few rows takes a 16-bit G' in two parts, high and low, and is off by its own rounding alone: of 1
-// to 8 rows it was up to 1.8 times as far off with one part (17 rows x 128256 x 2048 in bf16: 494 us with one, 509 with two).
+// even out; the weight's gradient of few rows takes a 16-bit G' in two parts, high and low: of 1 to 8 rows it was up to 1.8 times as far off with one part
+// (17 rows x 128256 x 2048 in bf16: 494 us with one, 509 with two).  These parts are of m G', m 2^e the rows' weights, and the hidden states are multiplied by 2^e
+// alone, which rounds nothing, so that the gradient is off by its own rounding, whatever the weights (with the weights in the hidden
+// states it was up to 1.43 times as far off).  The gradient of the hidden states, and many rows' of the weight, read G' as it is: its -1 at the target is
+// exact, and m would make it a number that is rounded (1000 rows of one weight: 1.60 times as far off as an fp32 result rounded once, now 1.03).
 constexpr float GRAD_SCALE_F16 = 32768.f;
 
 template <typename T> struct GradOf;
@@ -688,12 +709,28 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
             }
     X *out = reinterpret_cast<X *>(a.grad) + n0 * a.grad_stride + v0;
     if constexpr (sizeof(X) == 2) {
-        store_rows<S, X>(smem, a.N - n0, cols, out, a.grad_stride, [&](int i, int j) { return acc[i][j]; });
-        if (a.grad_plane)
-            store_rows<S, X>(smem, a.N - n0, cols, out + a.grad_plane / 2, a.grad_stride, [&](int i, int j) {
-                typedef X x4 __attribute__((ext_vector_type(4)));
-                return acc[i][j] - __builtin_convertvector(__builtin_convertvector(acc[i][j], x4), f32x4);
-            });
+        const auto high = [&](int i, int j) { return acc[i][j]; };
+        const auto low = [&](int i, int j) {
+            typedef X x4 __attribute__((ext_vector_type(4)));
+            return acc[i][j] - __builtin_convertvector(__builtin_convertvector(acc[i][j], x4), f32x4);
+        };
+        if (a.grad) store_rows<S, X>(smem, a.N - n0, cols, out, a.grad_stride, high);
+        if (a.low_plane) store_rows<S, X>(smem, a.N - n0, cols, out + a.grad_plane / 2, a.grad_stride, low);
+        if constexpr (TERMS == 1 && S::BN <= 64)
+            if (a.weighted) {
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j) {
+                    const int n = n0 + wn + 16 * j + (lane & 15);
+                    const float m = weight_mantissa(a.grad_loss[n < a.N ? n : a.N - 1]);
+#pragma unroll
+                    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = scale[j] != 0.f ? acc[i][j][e] * m : 0.f;
+                }
+                out = reinterpret_cast<X *>(a.weighted) + n0 * a.grad_stride + v0;
+                store_rows<S, X>(smem, a.N - n0, cols, out, a.grad_stride, high);
+                store_rows<S, X>(smem, a.N - n0, cols, out + a.grad_plane / 2, a.grad_stride, low);
+            }
     } else {
 #pragma unroll
         for (int j = 0; j < S::FN; ++j) {
@@ -805,7 +842,7 @@ struct HeadWeightArgs {
     void *out;                 // row 0: the piece's first token
     long long out_stride;
 };
-// Gradient of the weight: G'^T (H grad_loss / grad_top), both operands k strided: twice the LDS reads of 16 bytes a row, as the transposing read gives 8.
+// Gradient of the weight: G'^T (weighted H), both operands k strided: twice the LDS reads of 16 bytes a row, as the transposing read gives 8.
 // 4096 rows x 32256 tokens x 4096 in bf16: 0.82 to 0.85 ms, 1.27 to 1.32 PFLOP/s.
 template <typename T, typename S, int TERMS, int DT>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_grad_weight(HeadWeightArgs a)
@@ -843,13 +880,12 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
 // ---- what goes before the products -----------------------------------------------------------------------------------------------------------
 
 // fp32 values as two fp16 parts: x 2^s = high + low, with 2^s bringing the largest magnitude of the row (hidden states in the logits) or of the matrix
-// (where rows are summed over) to [2^14, 2^15).  Together they keep 22 bits of a value down to 2^-17 of that largest one, and 2^-40 of it
+// (the weight) to [2^14, 2^15), of the weighted hidden states, which are summed over, to [2^13, 2^15).  Together they keep 22 bits of a value down to 2^-17 of that largest one, and 2^-40 of it
 // below; of a product all but low x low is taken.  Products of three bf16 parts would need no scale, but six products for 24 bits.
-__device__ __forceinline__ float part_scale(unsigned max_bits)
+__device__ __forceinline__ float part_scale(int exponent)
 {
-    if (max_bits == 0u) return 1.f;
-    const int e = 127 + 14 - ((int)(max_bits >> 23) - 127);
-    return __uint_as_float((unsigned)min(max(e, 1), 253) << 23);
+    if (exponent == NO_EXPONENT) return 1.f;
+    return __uint_as_float((unsigned)min(max(127 + 14 - exponent, 1), 253) << 23);
 }
 __device__ __forceinline__ void store_parts(char *out, long long plane, const float (&v)[8], float s)
 {
@@ -864,39 +900,60 @@ __device__ __forceinline__ void store_parts(char *out, long long plane, const fl
 }
 
 struct HeadMaxArgs {
-    const float *x;
-    long long stride;
-    int rows, cols;            // cols: a multiple of 4
-    const int *targets;        // null, or rows without a target do not count
+    const void *x;
+    long long stride;          // elements
+    int rows, cols;            // cols: whole 16 bytes
+    const int *targets;        // null, or hidden states: rows without a target do not count, the others are multiplied by their weight
+    const float *grad_loss;
     int vocab;
-    unsigned *out;             // starts at 0
+    int *out;                  // [workgroups]: exponents of the largest magnitudes (2^e <= x < 2^(e + 1)), NO_EXPONENT: all zeros
 };
-// Largest finite magnitude of a matrix (bits), joined by an integer maximum, whose order does not matter.  A wave takes rows.
-__global__ __launch_bounds__(256) static void k_head_max(HeadMaxArgs a)
+// Exponent of the largest finite magnitude of a matrix, one for each workgroup, so that nothing has to be cleared or joined in memory.  A wave takes rows.
+constexpr int MAX_GROUPS = 2048;
+template <int DT>
+__global__ __launch_bounds__(256) void k_head_max(HeadMaxArgs a)
 {
+    constexpr int VEC = Stored<DT>::VEC;
+    using X = typename Stored<DT>::type;
+    typedef X vec __attribute__((ext_vector_type(VEC)));
+    __shared__ int tops[4];
     const int lane = threadIdx.x & 63;
-    unsigned m = 0u;
+    int top = NO_EXPONENT;
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += gridDim.x * 4) {
-        if (a.targets && !counts(a.targets[r], a.vocab)) continue;
-        const float *x = a.x + r * a.stride;
-        for (int c = lane * 4; c < a.cols; c += 256) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(x + c);
+        int e = 0;
+        float m = 1.f;
+        if (a.targets) {
+            if (!counts(a.targets[r], a.vocab)) continue;
+            const float g = a.grad_loss[r];
+            e = weight_exponent(g);
+            m = fabsf(weight_mantissa(g));
+            if (e == NO_EXPONENT) continue;
+        }
+        const X *x = static_cast<const X *>(a.x) + r * a.stride;
+        unsigned most = 0u;
+#pragma unroll 4
+        for (int c = lane * VEC; c < a.cols; c += 64 * VEC) {
+            const vec v = *reinterpret_cast<const vec *>(x + c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) m = max(m, finite_magnitude(v[e]));
+            for (int q = 0; q < VEC; ++q) most = max(most, finite_magnitude((float)v[q]));
+        }
+        if (most) {
+            const float in_1_2 = most < 0x800000u ? 1.f : __uint_as_float((most & 0x7fffffu) | 0x3f800000u);       // (below 2^-126: as that)
+            top = max(top, e + max((int)(most >> 23), 1) - 127 - (in_1_2 * m < 1.f) + (in_1_2 * m >= 2.f));
         }
     }
 #pragma unroll
-    for (int o = 32; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
-    if (lane == 0 && m) atomicMax(a.out, m);
+    for (int o = 32; o; o /= 2) top = max(top, __shfl_xor(top, o));
+    if (lane == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) a.out[blockIdx.x] = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
 }
-struct HeadClearArgs {
-    HeadScalars *sc;
-};
-__global__ static void k_head_clear(HeadClearArgs a) { a.sc->hidden_max = a.sc->weight_max = 0u; }
 
 struct HeadScalarsArgs {
     HeadScalars *sc;
-    int fp32;
+    const int *weight_max, *hidden_max;    // null, or what k_head_max wrote
+    int weight_groups, hidden_groups;
+    int fine;                  // the weights' mantissas are in G'
     int N, vocab;
     float temperature;
     const int *targets;
@@ -908,29 +965,50 @@ constexpr int SCALARS_WG = 1024;
 __global__ __launch_bounds__(SCALARS_WG) static void k_head_scalars(HeadScalarsArgs a)
 {
     __shared__ float tops[SCALARS_WG / 64];
+    __shared__ int most[2][SCALARS_WG / 64];
     float top = 0.f;
+    int m[2] = {NO_EXPONENT, NO_EXPONENT};                 // of the weight, of the weighted hidden states
     bool bad = false;
+    for (int i = threadIdx.x; i < a.weight_groups; i += SCALARS_WG) m[0] = max(m[0], a.weight_max[i]);
+    for (int i = threadIdx.x; i < a.hidden_groups; i += SCALARS_WG) m[1] = max(m[1], a.hidden_max[i]);
     if (a.grad_loss)
         for (int n = threadIdx.x; n < a.N; n += SCALARS_WG) {
             const int t = a.targets[n];
+            const float g = a.grad_loss[n];
             bad |= t >= a.vocab;
-            if (counts(t, a.vocab)) top = fmaxf(top, fabsf(a.grad_loss[n]));
+            if (counts(t, a.vocab) && is_finite(g)) top = fmaxf(top, fabsf(g));
         }
     top = wave_reduce(top, OpMax{});
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int o = 32; o; o /= 2) m[q] = max(m[q], __shfl_xor(m[q], o));
+    if ((threadIdx.x & 63) == 0) {
+        tops[threadIdx.x >> 6] = top;
+        most[0][threadIdx.x >> 6] = m[0];
+        most[1][threadIdx.x >> 6] = m[1];
+    }
     if (bad) atomicOr(a.flags, (unsigned)SVIP_FLAG_BAD_TOKEN);
     __syncthreads();
     if (threadIdx.x) return;
-    for (int i = 1; i < SCALARS_WG / 64; ++i) top = fmaxf(top, tops[i]);
-    // grad_loss / grad_top is at most 1 in magnitude, so the largest weighted hidden state is at most the largest hidden state
-    const float hs = a.fp32 ? part_scale(a.sc->hidden_max) : 1.f, ws = a.fp32 ? part_scale(a.sc->weight_max) : 1.f;
+    for (int i = 1; i < SCALARS_WG / 64; ++i) {
+        top = fmaxf(top, tops[i]);
+        m[0] = max(m[0], most[0][i]);
+        m[1] = max(m[1], most[1][i]);
+    }
+    // The weighted hidden states are H (grad_loss / grad_top) 2^(shift + e), e of grad_top, or H 2^(shift + e), e of the row's own weight where its mantissa
+    // is in G'.  fp16 and parts: the largest |H grad_loss| is at least 2^m1, so that either is below 2^15 and the largest above 2^13.  Other
+    // types hold any that is no larger than the hidden states.  (No further up than leaves the result's multiplier a normal number.)
+    const int e = top > 0.f ? weight_exponent(top) : 0;
+    const int shift = min(!a.hidden_max ? -e : m[1] == NO_EXPONENT ? 0 : 13 - m[1], 111);
+    const float ws = a.weight_max ? part_scale(m[0]) : 1.f;
     const double t = 1.0 / (double)a.temperature;
-    a.sc->hidden_parts = hs;
     a.sc->weight_parts = ws;
     a.sc->to_log2 = (float)(1.4426950408889634 * t / (double)ws);
     a.sc->grad_top = top;
     a.sc->hidden_mult = (float)(t / ((double)a.grad_scale * (double)ws));
-    a.sc->weight_mult = (float)((double)top * t / ((double)a.grad_scale * (double)hs));
+    a.sc->weight_mult = (float)(t / (double)a.grad_scale * ldexp(a.fine ? 1.0 : (double)top, a.fine ? -shift : -shift - e));
+    a.sc->weighted_shift = a.fine ? shift : shift + e;
 }
 
 struct HeadPackArgs {
@@ -940,8 +1018,9 @@ struct HeadPackArgs {
     char *out;                 // [planes][rows][cols_p] 16-bit
     long long plane;           // bytes
     const HeadScalars *sc;
-    const int *targets;        // hidden states for the gradient of the weight: rows weighted by grad_loss / grad_top, 0 where they do not count
+    const int *targets;        // hidden states for the gradient of the weight: weighted rows (k_head_scalars), 0 where they do not count
     const float *grad_loss;
+    int fine;
     int vocab;
     float *row_inv;            // hidden states for the logits: parts of their own scale for each row
     int whole;                 // fp32 as it is, no parts
@@ -979,9 +1058,11 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadPackArgs a)
     load_columns<DT>(a, r, c, v);
     if (a.targets) {
         const bool use = counts(a.targets[r], a.vocab);
-        const float top = a.sc->grad_top, w = top > 0.f ? a.grad_loss[r] / top : a.grad_loss[r];       // (else 0 or NaN)
+        const float g = a.grad_loss[r], top = a.sc->grad_top;
+        const float w = !is_finite(g) ? NAN : a.fine ? 1.f : top > 0.f ? g / top : 0.f;
+        const int shift = a.sc->weighted_shift + (a.fine && is_finite(g) ? weight_exponent(g) : 0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = use ? v[e] * w : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = use ? __builtin_amdgcn_ldexpf(v[e] * w, shift) : 0.f;
     }
     char *out = a.out + (r * a.cols_p + c) * 2;
     if (DT == SVIP_F32 && a.whole) {
@@ -989,7 +1070,7 @@ __global__ __launch_bounds__(256) void k_head_pack(HeadPackArgs a)
         *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
         *reinterpret_cast<f32x4 *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
     } else if constexpr (DT == SVIP_F32) {
-        store_parts(out, a.plane, v, a.targets ? a.sc->hidden_parts : a.sc->weight_parts);
+        store_parts(out, a.plane, v, a.targets ? 1.f : a.sc->weight_parts);
     } else {
         using X = typename Stored<DT>::type;
         typedef X x8 __attribute__((ext_vector_type(8)));
@@ -1013,7 +1094,7 @@ __global__ __launch_bounds__(256) static void k_head_pack_rows(HeadPackArgs a)
     }
 #pragma unroll
     for (int o = 32; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
-    const float s = part_scale(m);
+    const float s = part_scale(m ? (int)(m >> 23) - 127 : NO_EXPONENT);
     for (int c = lane * 8; c < a.cols_p; c += 512) {
         load_columns<SVIP_F32>(a, r, c, v);
         store_parts(a.out + ((long long)r * a.cols_p + c) * 2, a.plane, v, s);

@@ -148,12 +148,12 @@ constexpr size_t SPLIT_BYTES = (size_t)128 << 20;
 
 struct HeadPlan {
     bool parts;                // fp32 as two fp16 parts
-    bool fine;                 // 16-bit G' in two parts for the gradient of the weight
+    bool fine;                 // 16-bit G' in two parts, with the rows' weights, for the gradient of the weight
     int planes, size, width;   // planes and bytes of what the products are made of; channels of its rows
     int piece;                 // tokens of a piece of the vocabulary, a multiple of MOST_TILE
     ShapeId logits, hidden_grad, weight_grad;
     int splits, per_split;     // of a piece's tokens in the gradient of the hidden states
-    size_t part, target, rows, hidden_parts, weighted, weight, grad, sum, bytes;     // offsets
+    size_t part, target, rows, maxima, hidden_parts, weighted, weight, grad, sum, bytes;     // offsets
     long long grad_stride;
 };
 
@@ -180,7 +180,7 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     p.size = dtype == SVIP_F32 && !p.parts ? 4 : 2;
     p.width = p.parts ? up(D, 8) : D;
     p.fine = grad && p.size == 2 && !p.parts && N <= FEW_ROWS;
-    const int grad_planes = p.parts || p.fine ? 2 : 1;
+    const int grad_planes = p.fine ? 3 : p.parts ? 2 : 1;      // (fine: G', high and low parts of the weighted one)
     const double terms = p.parts ? 3.0 : 1.0;
     // pieces: of the softmax in the gradient, of the weight's parts in fp32; equal, so that none is a sliver
     long long most = V;
@@ -239,6 +239,9 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
         }
         p.splits = ceil_div(p.piece, p.per_split);
         p.sum = take((size_t)p.splits * N * p.width * sizeof(float));
+    }
+    if (p.parts || (grad && dtype == SVIP_F16)) p.maxima = take((size_t)2 * MAX_GROUPS * sizeof(int));
+    if (grad) {
         const size_t loss = plan(SVIP_HEAD_LOSS, dtype, N, V, D).bytes;          // (one workspace serves both)
         if (at < loss) at = loss;
     }
@@ -289,21 +292,34 @@ static long long pack_grid(HeadPackArgs &a)
 
 static HeadScalars *scalars(const LossCall &c) { return reinterpret_cast<HeadScalars *>(c.ws + 256); }
 
-// The scalars that the tiles use, and in fp32 the parts of the hidden states.
-static bool prepare(const LossCall &c, const HeadPlan &p, const float *grad_loss, float grad_scale)
+// The scalars that the tiles use, and in fp32 the parts of the hidden states.  weight_grad: the gradient of the weight is asked for.
+static bool prepare(const LossCall &c, const HeadPlan &p, const float *grad_loss, float grad_scale, bool weight_grad)
 {
     if (!p.parts && !grad_loss) return true;
-    HeadScalars *sc = scalars(c);
+    HeadScalarsArgs a = {};
+    a.sc = scalars(c);
+    a.fine = p.fine;
+    a.N = c.N;
+    a.vocab = c.V;
+    a.temperature = c.temperature;
+    a.targets = c.targets;
+    a.grad_loss = grad_loss;
+    a.grad_scale = grad_scale;
+    a.flags = reinterpret_cast<unsigned *>(c.ws);
+    int *const maxima = reinterpret_cast<int *>(c.ws + p.maxima);
+    auto largest = [&](const void *x, long long stride, int rows, const int *targets, int *out, int *groups) {
+        *groups = rows < 4 * MAX_GROUPS ? ceil_div(rows, 4) : MAX_GROUPS;
+        const HeadMaxArgs m = {x, stride, rows, c.D, targets, grad_loss, c.V, out};
+        return c.dtype == SVIP_F16 ? launch(k_head_max<SVIP_F16>, *groups, 256, c.st, m) : launch(k_head_max<SVIP_F32>, *groups, 256, c.st, m);
+    };
     if (p.parts) {
-        if (!launch(k_head_clear, 1, 1, c.st, HeadClearArgs{sc})) return false;
-        auto largest = [&](const void *x, long long stride, int rows, const int *targets, unsigned *out) {
-            HeadMaxArgs m = {static_cast<const float *>(x), stride, rows, c.D, targets, c.V, out};
-            return launch(k_head_max, rows < 4 * 2048 ? ceil_div(rows, 4) : 2048, 256, c.st, m);
-        };
-        if (!largest(c.weight, c.weight_stride, c.V, nullptr, &sc->weight_max)) return false;
-        if (grad_loss && !largest(c.hidden, c.hidden_stride, c.N, c.targets, &sc->hidden_max)) return false;
+        a.weight_max = maxima;
+        if (!largest(c.weight, c.weight_stride, c.V, nullptr, maxima, &a.weight_groups)) return false;
     }
-    HeadScalarsArgs a = {sc, p.parts, c.N, c.V, c.temperature, c.targets, grad_loss, grad_scale, reinterpret_cast<unsigned *>(c.ws)};
+    if (weight_grad && (p.parts || c.dtype == SVIP_F16)) {
+        a.hidden_max = maxima + MAX_GROUPS;
+        if (!largest(c.hidden, c.hidden_stride, c.N, c.targets, maxima + MAX_GROUPS, &a.hidden_groups)) return false;
+    }
     if (!launch(k_head_scalars, 1, SCALARS_WG, c.st, a)) return false;
     if (!p.parts) return true;
     HeadPackArgs h = {};
@@ -359,7 +375,7 @@ static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, 
 
 static bool run_loss(const LossCall &c, const HeadPlan &p, float *loss, float *lse)
 {
-    if (!prepare(c, p, nullptr, 1.f)) return false;
+    if (!prepare(c, p, nullptr, 1.f, false)) return false;
     const int whole = p.parts ? p.piece : c.V;
     int records = 0;
     for (int v0 = 0; v0 < c.V; v0 += whole) {
@@ -391,7 +407,7 @@ struct GradOut {
 static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, const float *grad_loss, const GradOut &out)
 {
     const float scale = c.dtype == SVIP_F16 || p.parts ? GRAD_SCALE_F16 : 1.f;
-    if (!prepare(c, p, grad_loss, scale)) return false;
+    if (!prepare(c, p, grad_loss, scale, out.weight != nullptr)) return false;
     const int size = size_of(c.dtype);
     const int wide = up(p.width, 8);                       // of the weighted hidden states' rows
     const long long packed_plane = (long long)c.N * wide * p.size, grad_plane = (long long)c.N * p.grad_stride * p.size;
@@ -408,6 +424,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         h.sc = scalars(c);
         h.targets = c.targets;
         h.grad_loss = grad_loss;
+        h.fine = p.fine;
         h.vocab = c.V;
         if (!by_dtype(c.dtype, [&](auto dt) {
                 return launch(k_head_pack<decltype(dt)::value>, pack_grid(h), 256, c.st, h);
@@ -419,9 +436,12 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
         HeadArgs a;
         if (!piece_args(c, p, v0, count, &a)) return false;
         a.lse = lse;
-        a.grad = c.ws + p.grad;
+        a.grad_loss = grad_loss;
+        a.grad = p.fine && !out.hidden ? nullptr : c.ws + p.grad;
+        a.weighted = p.fine && out.weight ? c.ws + p.grad + grad_plane : nullptr;
         a.grad_stride = p.grad_stride;
-        a.grad_plane = p.parts || (p.fine && out.weight) ? grad_plane : 0;
+        a.grad_plane = grad_plane;
+        a.low_plane = p.parts;
         const Operand grad = {c.ws + p.grad, p.grad_stride * p.size, grad_plane};
         const bool ok = by_product(c.dtype, p.parts, [&](auto type, auto terms, auto dt) {
             using T = decltype(type);
@@ -453,6 +473,7 @@ static bool run_grad(const LossCall &c, const HeadPlan &p, const float *lse, con
                 HeadWeightArgs g = {};
                 g.hidden = {c.ws + p.weighted, (long long)wide * p.size, packed_plane};
                 g.grad = grad;
+                if (p.fine) g.grad.base = a.weighted;
                 g.N = c.N;
                 g.D = c.D;
                 g.Dp = p.width;
