@@ -427,7 +427,7 @@ svip_status svip_quantize_blocks(
  * Logits of hidden states and weight in 8 bits:
  *   logits_out[n, v] = sum over blocks b of 2^(s_n,b + s_v,b) * sum over k in block b of hidden_q[n, k] * weight_q[v, k]
  * with the scales of hidden_scale[n, b] (blocks of 1 x 128) and weight_scale[v / 128, b] (blocks of 128 x 128), as
- * svip_quantize_blocks writes them.  K is a multiple of 128.  Sums in fp32, rounded once to dtype.  logits_out has the layout
+ * svip_quantize_blocks writes them (255, the NaN of e8m0: its rows' or tokens' logits are NaN).  K is a multiple of 128.  Sums in fp32, rounded once to dtype.  logits_out has the layout
  * that the calls above take: rows of V values, 16-byte aligned, row n at element offset n * row_stride.
  */
 svip_status svip_head_logits(

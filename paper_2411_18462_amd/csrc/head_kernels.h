@@ -56,6 +56,7 @@ __device__ __forceinline__ void put_up_to_4(typename Stored<DT>::type *p, f32x4 
 // of two costs is up to one bit at the small end of 2^15 : 1.)  Values that are not finite do not count for e and become the code of NaN.
 
 constexpr int QBLOCK = 128;
+constexpr int SCALE_NAN = 255;                         // as a scale's byte; never written here
 
 __device__ __forceinline__ unsigned finite_magnitude(float x)
 {
@@ -375,12 +376,13 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         } else {
 #pragma unroll
             for (int j = 0; j < S::FN; ++j) {
+                const float start = sca == SCALE_NAN || scb[j] == SCALE_NAN ? NAN : 0.f;       // (as the 8-bit instruction does)
                 s16x8 b[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) b[q] = codes_to_bf16(fb[j][2 * q], fb[j][2 * q + 1]);
 #pragma unroll
                 for (int i = 0; i < S::FM; ++i) {
-                    f32x4 block = {0.f, 0.f, 0.f, 0.f};
+                    f32x4 block = {start, start, start, start};
 #pragma unroll
                     for (int q = 0; q < 4; ++q) block = Bf16::mfma(codes_to_bf16(fa[i][2 * q], fa[i][2 * q + 1]), b[q], block);
 #pragma unroll
