@@ -56,7 +56,6 @@ __device__ __forceinline__ void put_up_to_4(typename Stored<DT>::type *p, f32x4 
 // of two costs is up to one bit at the small end of 2^15 : 1.)  Values that are not finite do not count for e and become the code of NaN.
 
 constexpr int QBLOCK = 128;
-constexpr int SCALE_NAN = 255;                         // as a scale's byte; never written here
 
 __device__ __forceinline__ unsigned finite_magnitude(float x)
 {
@@ -319,9 +318,12 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         sb.copy(at + S::BM * STEP_BYTES, k0 + s * QBLOCK, k_end, 0);
     };
     // The scales of SCALE_STEPS steps into LDS, read four at a time, all under way before the first is needed.
+    constexpr int ROWS = S::BN + WEIGHT_BLOCKS, ROUNDS = (ROWS * SCALE_WORDS + S::THREADS - 1) / S::THREADS;
+    static_assert(ROUNDS <= 32, "a bit of `nan` each");
+    static_assert(SCALE_WORDS == 16 && S::THREADS % 64 == 0, "a row's words are read by 16 lanes side by side");
+    // (fp32: behind a row's scales whether it has held the byte 255, the NaN of e8m0, up to now)
     auto scales = [&](int s0) {
         const int count = steps - s0 < SCALE_STEPS ? steps - s0 : SCALE_STEPS;
-        constexpr int ROWS = S::BN + WEIGHT_BLOCKS, ROUNDS = (ROWS * SCALE_WORDS + S::THREADS - 1) / S::THREADS;
         unsigned word[ROUNDS];
 #pragma unroll
         for (int k = 0; k < ROUNDS; ++k) {
@@ -339,6 +341,11 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         for (int k = 0; k < ROUNDS; ++k) {
             const int i = k * S::THREADS + (int)threadIdx.x, r = i / SCALE_WORDS, q = i % SCALE_WORDS;
             if (r < ROWS) *reinterpret_cast<unsigned *>(scale_bytes + r * SCALE_PITCH + 4 * q) = word[k];
+            if constexpr (DT == SVIP_F32) {
+                const bool nan = (__ballot((~word[k] - 0x01010101u) & word[k] & 0x80808080u) >> (lane & 48) & 0xffffu) != 0;
+                unsigned char *const held = scale_bytes + r * SCALE_PITCH + SCALE_STEPS;
+                if (r < ROWS && q == 0 && (nan || s0 == 0)) *held = nan;
+            }
         }
     };
     const int w_row = (v0 % QBLOCK + wm) / QBLOCK;
@@ -376,13 +383,12 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         } else {
 #pragma unroll
             for (int j = 0; j < S::FN; ++j) {
-                const float start = sca == SCALE_NAN || scb[j] == SCALE_NAN ? NAN : 0.f;       // (as the 8-bit instruction does)
                 s16x8 b[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) b[q] = codes_to_bf16(fb[j][2 * q], fb[j][2 * q + 1]);
 #pragma unroll
                 for (int i = 0; i < S::FM; ++i) {
-                    f32x4 block = {start, start, start, start};
+                    f32x4 block = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int q = 0; q < 4; ++q) block = Bf16::mfma(codes_to_bf16(fa[i][2 * q], fa[i][2 * q + 1]), b[q], block);
 #pragma unroll
@@ -391,6 +397,14 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
             }
         }
     }
+    // For the 8-bit instruction a scale of 255 is NaN, for the sum of exponents above 2^128: its row's or tokens' logits become NaN here.  (As a choice in
+    // each step 2 to 3 % of a call.)
+    if constexpr (DT == SVIP_F32)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+            if (hs[(wn + 16 * j + (lane & 15)) * SCALE_PITCH + SCALE_STEPS] | ws[w_row * SCALE_PITCH + SCALE_STEPS])
+#pragma unroll
+                for (int i = 0; i < S::FM; ++i) acc[i][j] = f32x4{NAN, NAN, NAN, NAN};
     using X = typename Stored<DT>::type;
     if (a.part) {
 #pragma unroll
