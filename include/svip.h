@@ -396,7 +396,7 @@ svip_status svip_warp_logits(const void *logits_in, void *logits_out, int dtype,
  * Their workspace: svip_head_workspace_bytes of the call's sizes or more, 256-byte aligned, that svip_workspace_reset has cleared
  * once (for its flag word).  It is not the one of the calls above, it holds nothing between calls, and calls that run concurrently
  * must use different ones.  Sizes: 1 <= N <= 2^20 rows of hidden states, 1 <= V <= 2^22, 1 <= D, K <= 2^17; row strides are at most
- * 2^23 elements (8-bit matrices: 2^24).  Same inputs give bit-identical outputs.
+ * 2^23 elements (8-bit matrices: 2^24); the gradient: N x D < 2^34, N filled up to fours and D to 256.  Same inputs give bit-identical outputs.
  */
 typedef enum {
     SVIP_HEAD_LOGITS = 0,            /* svip_head_logits; dtype: of logits_out, D: K */
@@ -413,7 +413,8 @@ size_t svip_head_workspace_bytes(int call, int dtype, int N, int V, int D);
  *   q_out[r, c] = x[r, c] / 2^e rounded to e4m3 (OCP: 4 exponent bits, 3 mantissa bits, no infinity), ties to even
  *   scale_out[r / block_rows, c / 128] = e + 127              (e8m0: a power of two)
  * so that the value kept is q * 2^e.  A value that is not finite becomes the code 0x7f (NaN).  Bytes of q_out past column K and of
- * scale_out past column K / 128 are not written.  No workspace.  rows <= 2^22, cols <= 2^17, fewer than 2^27 runs of 128 columns in all.
+ * scale_out past column K / 128 are not written.  No workspace.  rows <= 2^22, cols <= 2^17, fewer than 2^27 runs of 128 columns in all
+ * (fp32 with block_rows 1: 2^27 - 8 at most).
  */
 svip_status svip_quantize_blocks(
     const void *x, int dtype,        /* device, row r at element offset r * row_stride (any; x on its type's alignment) */

@@ -21,6 +21,8 @@ constexpr int HEAD_MAX_VOCAB = 1 << 22;
 constexpr int HEAD_MAX_WIDTH = 1 << 17;                // hidden channels
 constexpr long long HEAD_MAX_STRIDE = 1 << 23;         // elements: 256 rows of a tile lie within 32 bits of bytes
 
+constexpr long long MOST_THREADS = 0xffffffffLL;       // of a launch
+
 // A matrix of rows x cols of dtype: stride of a row in whole 16 bytes, within reach of a tile's 32-bit offsets.
 static svip_status check_matrix(const void *p, int dtype, int cols, long long stride)
 {
@@ -31,7 +33,7 @@ static svip_status check_matrix(const void *p, int dtype, int cols, long long st
 template <typename A>
 static bool launch(void (*kernel)(A), long long grid, unsigned block, hipStream_t st, const A &args)
 {
-    if (grid <= 0 || grid * block > 0xffffffffLL) return false;          // (threads of a launch)
+    if (grid <= 0 || grid * block > MOST_THREADS) return false;
     A copy = args;
     void *argv[] = {&copy};
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)grid), dim3(block), argv, 0, st) == hipSuccess;
@@ -150,7 +152,7 @@ struct HeadPlan {
     bool parts;                // fp32 as two fp16 parts
     bool fine;                 // 16-bit G' in two parts, with the rows' weights, for the gradient of the weight
     int planes, size, width;   // planes and bytes of what the products are made of; channels of its rows
-    int piece;                 // tokens of a piece of the vocabulary, a multiple of MOST_TILE
+    int piece;                 // tokens of a piece of the vocabulary, a multiple of MOST_TILE (of a loss without parts: nearly always all)
     ShapeId logits, hidden_grad, weight_grad;
     int splits, per_split;     // of a piece's tokens in the gradient of the hidden states
     size_t part, target, rows, maxima, hidden_parts, weighted, weight, grad, sum, bytes;     // offsets
@@ -182,8 +184,10 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     p.fine = grad && p.size == 2 && !p.parts && N <= FEW_ROWS;
     const int grad_planes = p.fine ? 3 : p.parts ? 2 : 1;      // (fine: G', high and low parts of the weighted one)
     const double terms = p.parts ? 3.0 : 1.0;
-    // pieces: of the softmax in the gradient, of the weight's parts in fp32; equal, so that none is a sliver
-    long long most = V;
+    // pieces: of the softmax in the gradient, of the weight's parts in fp32, of what a launch has the threads for (at most four for a token and 32 rows,
+    // whatever the tiles); equal, so that none is a sliver
+    long long most = V, threads = MOST_THREADS / (4LL * ceil_div(N, 32)) / MOST_TILE * MOST_TILE;
+    if (most > threads) most = threads;
     if (grad) most = (long long)(PIECE_BYTES / ((size_t)N * p.size * grad_planes));
     if (p.parts) most = most < (long long)(PIECE_BYTES / ((size_t)p.width * 4)) ? most : (long long)(PIECE_BYTES / ((size_t)p.width * 4));
     if (most < LEAST_PIECE) most = LEAST_PIECE;
@@ -253,6 +257,11 @@ static svip_status check_sizes(int N, int V, int D)
 {
     return N <= 0 || N > HEAD_MAX_ROWS || V <= 0 || V > HEAD_MAX_VOCAB || D <= 0 || D > HEAD_MAX_WIDTH ? SVIP_ERR_SHAPE : SVIP_OK;
 }
+// The join of the hidden states' gradient, four values of a row a thread, has more threads than other launches whose size is N x D.
+static svip_status check_grad_sizes(int N, int D)
+{
+    return (long long)ceil_div(N, JOIN_SLICES) * ceil_div(D, 4 * JOIN_COLUMNS) * (JOIN_COLUMNS * JOIN_SLICES) > MOST_THREADS ? SVIP_ERR_SHAPE : SVIP_OK;
+}
 static svip_status check_workspace(const void *ws, size_t bytes, size_t need)
 {
     return !ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || bytes < need ? SVIP_ERR_WORKSPACE : SVIP_OK;
@@ -275,6 +284,8 @@ static svip_status check_loss(const LossCall &c, const void *out, int call, size
     if (!c.hidden || !c.weight || !c.targets || !out) return SVIP_ERR_NULL;
     if (!dtype_ok(c.dtype)) return SVIP_ERR_DTYPE;
     if (svip_status s = check_sizes(c.N, c.V, c.D)) return s;
+    if (call == SVIP_HEAD_LOSS_GRAD)
+        if (svip_status s = check_grad_sizes(c.N, c.D)) return s;
     if (svip_status s = check_matrix(c.hidden, c.dtype, c.D, c.hidden_stride)) return s;
     if (svip_status s = check_matrix(c.weight, c.dtype, c.D, c.weight_stride)) return s;
     if (c.D * size_of(c.dtype) % 16 != 0) return SVIP_ERR_ALIGN;
@@ -376,10 +387,9 @@ static bool piece_args(const LossCall &c, const HeadPlan &p, int v0, int count, 
 static bool run_loss(const LossCall &c, const HeadPlan &p, float *loss, float *lse)
 {
     if (!prepare(c, p, nullptr, 1.f, false)) return false;
-    const int whole = p.parts ? p.piece : c.V;
     int records = 0;
-    for (int v0 = 0; v0 < c.V; v0 += whole) {
-        const int count = c.V - v0 < whole ? c.V - v0 : whole;
+    for (int v0 = 0; v0 < c.V; v0 += p.piece) {
+        const int count = c.V - v0 < p.piece ? c.V - v0 : p.piece;
         HeadArgs a;
         if (!piece_args(c, p, v0, count, &a)) return false;
         const bool ok = by_product(c.dtype, p.parts, [&](auto type, auto terms, auto) {
@@ -511,6 +521,7 @@ using namespace svip;
 size_t svip_head_workspace_bytes(int call, int dtype, int N, int V, int D)
 {
     if (call < SVIP_HEAD_LOGITS || call > SVIP_HEAD_LOSS_GRAD || !dtype_ok(dtype) || check_sizes(N, V, D)) return 0;
+    if (call == SVIP_HEAD_LOSS_GRAD && check_grad_sizes(N, D)) return 0;
     return plan(call, dtype, N, V, D).bytes;
 }
 
@@ -522,6 +533,8 @@ svip_status svip_quantize_blocks(const void *x, int dtype, int rows, int cols, l
     if (rows <= 0 || rows > HEAD_MAX_VOCAB || cols <= 0 || cols > HEAD_MAX_WIDTH || row_stride < cols) return SVIP_ERR_SHAPE;
     const int kb = ceil_div(cols, QBLOCK);
     if (q_stride < (long long)kb * QBLOCK || scale_stride < kb || (long long)rows * kb >= 1LL << 27) return SVIP_ERR_SHAPE;
+    // (fp32 in blocks of one row, 32 lanes a block: whole workgroups of 2^27 - 7 and more would be 2^32 threads)
+    if (dtype == SVIP_F32 && block_rows == 1 && (long long)rows * kb > (1LL << 27) - QUANT_WG * Stored<SVIP_F32>::VEC / QBLOCK) return SVIP_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(x) % size_of(dtype) != 0 || !aligned16(q_out) || q_stride % 16 != 0) return SVIP_ERR_ALIGN;
     if (block_rows != 1 && block_rows != QBLOCK) return SVIP_ERR_PARAM;
     QuantizeArgs a = {x, row_stride, rows, cols, kb, static_cast<unsigned char *>(q_out), q_stride, static_cast<unsigned char *>(scale_out), scale_stride};
