@@ -574,11 +574,17 @@ def merge_counters(cells, directory):
 
 
 def sources_digest():
-    """Digest of the kernel sources: a profile summary names the digest it was taken with, so a figure read
-    back from profiles/ can be told from one that belongs to older kernels."""
-    h = hashlib.sha256()
+    """Digest of the sources of the kernels measured here, svip_kernels.hip and what it includes: a profile summary names the
+    digest it was taken with, so a figure read back from profiles/ can be told from one that belongs to older kernels."""
     d = os.path.join(ROOT, "paper_2411_18462_amd", "csrc")
-    for f in sorted(os.listdir(d)):
+    files, left = set(), ["svip_kernels.hip"]
+    while left:
+        f = left.pop()
+        if f not in files and "/" not in f:                            # (not the headers of the ABI, which lie elsewhere)
+            files.add(f)
+            left += re.findall(r'^#include "([^"]+)"', open(os.path.join(d, f)).read(), re.M)
+    h = hashlib.sha256()
+    for f in sorted(files):
         h.update(open(os.path.join(d, f), "rb").read())
     return h.hexdigest()[:12]
 
