@@ -394,8 +394,9 @@ svip_status svip_warp_logits(const void *logits_in, void *logits_out, int dtype,
  * in 8 bits and trained in the storage types of the logits.
  *
  * Their workspace: svip_head_workspace_bytes of the call's sizes or more, 256-byte aligned, that svip_workspace_reset has cleared
- * once (for its flag word).  It is not the one of the calls above, it holds nothing between calls, and calls that run concurrently
- * must use different ones.  Sizes: 1 <= N <= 2^20 rows of hidden states, 1 <= V <= 2^22, 1 <= D, K <= 2^17; row strides are at most
+ * once (for its flag word).  A workspace for calls of several sizes has the most bytes that one of them needs, which need not be the one
+ * of the most rows.  It is not the one of the calls above, it holds nothing between calls, and calls that run concurrently must use
+ * different ones.  Sizes: 1 <= N <= 2^20 rows of hidden states, 1 <= V <= 2^22, 1 <= D, K <= 2^17; row strides are at most
  * 2^23 elements (8-bit matrices: 2^24); the gradient: N x D < 2^34, N filled up to fours and D to 256.  Same inputs give bit-identical outputs.
  */
 typedef enum {
@@ -428,8 +429,10 @@ svip_status svip_quantize_blocks(
  * Logits of hidden states and weight in 8 bits:
  *   logits_out[n, v] = sum over blocks b of 2^(s_n,b + s_v,b) * sum over k in block b of hidden_q[n, k] * weight_q[v, k]
  * with the scales of hidden_scale[n, b] (blocks of 1 x 128) and weight_scale[v / 128, b] (blocks of 128 x 128), as
- * svip_quantize_blocks writes them (255, the NaN of e8m0: its rows' or tokens' logits are NaN).  K is a multiple of 128.  Sums in fp32, rounded once to dtype.  logits_out has the layout
- * that the calls above take: rows of V values, 16-byte aligned, row n at element offset n * row_stride.
+ * svip_quantize_blocks writes them (255, the NaN of e8m0: its rows' or tokens' logits are NaN).  K is a multiple of 128.  Sums in fp32,
+ * rounded once to dtype; for 16-bit logits by the 8-bit matrix instruction, which drops, of 8 products next to one another along K,
+ * what lies below 2^-13 of the largest.  logits_out has the layout that the calls above take: rows of V values, 16-byte aligned, row n at
+ * element offset n * row_stride.
  */
 svip_status svip_head_logits(
     const void *hidden_q, const void *hidden_scale,    /* device [N, K] e4m3, [N, K / 128] e8m0 */
@@ -445,8 +448,9 @@ svip_status svip_head_logits(
  * never stored:
  *   lse_out[n]  = logsumexp over v of z[n, v]
  *   loss_out[n] = lse_out[n] - z[n, targets[n]],  0 where targets[n] is negative (a row without a target)
- * A target >= V counts as no target and sets SVIP_FLAG_BAD_TOKEN in the workspace.  Products and sums in fp32 (fp32 inputs: as two
- * 11-bit parts each, of a product all but low x low), joined in fp64.  D is a multiple of 16 bytes' worth of elements.
+ * A target >= V counts as no target and sets SVIP_FLAG_BAD_TOKEN in the workspace.  Products and sums in fp32 (fp32 inputs: as they
+ * are or, of some hundred rows on where that is faster, in two fp16 parts each, of a product all but low x low: parts keep 22 bits of a value, and
+ * never less than 2^-39 of the largest value of its row of hidden, or of weight), joined in fp64.  D is a multiple of 16 bytes' worth of elements.
  * hidden and weight are finite numbers; rows without a target may hold anything, and only their own lse_out depends on it.
  */
 svip_status svip_head_loss(
@@ -462,13 +466,14 @@ svip_status svip_head_loss(
  * Its gradient, for a loss of sum over n of grad_loss[n] * loss_out[n] (a mean over the rows with a target: 1 / their number):
  *   G[n, v] = (exp(z[n, v] - lse[n]) - [v = targets[n]]) * grad_loss[n] / temperature,  0 in rows without a target
  *   grad_hidden_out = G weight        grad_weight_out = G^T hidden
- * Either output may be NULL and is then not computed (a frozen head).  lse is svip_head_loss's; the logits are computed again, in pieces of the vocabulary, and the
- * difference of softmax and one-hot is held for one piece, in bf16 (bf16 inputs), in fp16 times 2^15 (fp16) or in two such
- * parts (fp32).  The hidden states that the weight's gradient sums are multiplied by grad_loss relative to the largest and rounded to their type
- * (fp32: in parts as above), which changes nothing where all rows have one grad_loss.  For up to 64 rows, where such roundings would not
- * even out, 16-bit types hold the difference in two parts, times the mantissa of grad_loss, and the hidden states are multiplied by its power of two
- * alone.  In fp16 and in parts of fp32 the weighted hidden states keep, besides their type's precision, 2^-38 of the largest |grad_loss x hidden|.
- * Rows without a target get gradients of zero and add none, whatever they and their grad_loss hold.
+ * Either output may be NULL and is then not computed (a frozen head).  lse is svip_head_loss's; the logits are computed again, in pieces of
+ * the vocabulary, and the difference of softmax and one-hot is held for one piece, in bf16 (bf16 inputs), in fp16 times 2^15 (fp16), in
+ * fp32 or, with inputs in parts, in two parts of fp16.  The hidden states that the weight's gradient sums are multiplied by grad_loss
+ * relative to the largest and rounded to their type (fp32: in parts as above), which changes nothing where all rows have one grad_loss.
+ * For up to 64 rows, where such roundings would not even out, 16-bit types hold the difference in two parts, times the mantissa of
+ * grad_loss, and the hidden states are multiplied by its power of two alone.  In fp16 and in parts of fp32 the weighted hidden states
+ * keep their type's precision down to 2^-38 of the largest |grad_loss x hidden|.  A grad_loss that is not finite makes its row's gradient
+ * and the weight's not finite.  Rows without a target get gradients of zero and add none, whatever they and their grad_loss hold.
  * The outputs must not overlap the inputs.
  */
 svip_status svip_head_loss_grad(

@@ -264,8 +264,9 @@ struct HeadLogitsArgs {
 constexpr int SCALE_STEPS = 64;                        // steps whose scales are in LDS at a time
 constexpr int SCALE_PITCH = SCALE_STEPS + 4, SCALE_WORDS = SCALE_STEPS / 4;
 
-// Logits of a tile.  1088 rows x 128256 x 4096: 597-609 us, 1.9 PFLOP/s, in large tiles of 8 us and 1.65 us a step; 64 rows x 128256 x 2048: 56 us, the
-// weight's bytes at 4.9 TB/s.  A step is 128 values of K: one block of each operand.
+// Logits of a tile.  1088 rows x 128256 x 4096: 600-609 us, 1.9 PFLOP/s, in large tiles of 8 us and 1.65 us a step, products under way in 51 % of the cycles
+// at 2.07 GHz (1088 rows are 1280 in such tiles; the first launches, before the card has settled its clock, take up to 720 us); 64 rows x
+// 128256 x 2048: 56 us, the weight's bytes at 4.9 TB/s.  A step is 128 values of K: one block of each operand.
 // For 16-bit logits the matrix cores multiply the codes, and take the scales as they are (16x16x128, one scale per 32 values; here all
 // of a step's are the same).  Their sums are not quite fp32: of 8 products next to one another along K, what lies below 2^-13 of the
 // largest is dropped (found with single products; random codes are off by 5e-5 of a sum's rms), which is nothing beside the
@@ -524,7 +525,7 @@ __device__ __forceinline__ float across_rows(float v, Op op)
 
 // Statistics of a tile of logits: per row the largest and the sum of exponentials over the tile's tokens, one record a row and tile, so that the
 // tiles need not wait for one another.  The products bound it: 8192 rows x 151936 x 2048 in bf16 take 3.66 to 3.78 ms (1.35 to 1.39 PFLOP/s, products under way
-// in 70 % of the cycles at the 1.72 GHz the card keeps under them), of which the exponentials are 3 of the 52 us of a tile.
+// in 69 % of the cycles at the 1.9 GHz the card keeps under them), of which the exponentials are 3 of the 52 us of a tile.
 template <typename T, typename S, int TERMS>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_stats(HeadArgs a)
 {
@@ -665,7 +666,7 @@ __global__ __launch_bounds__(FINISH_WG) static void k_head_finish(HeadFinishArgs
 // nothing: fp16 (and the two parts of an fp32 value) carry them times 2^15, which keeps 11 bits down to 2^-29.  bf16 keeps its 8 bits
 // at any magnitude: its rounding, at most 2^-8 of a value, is of the size of the rounding of the gradients themselves.  In a sum over many rows these roundings
 // even out; the weight's gradient of few rows takes a 16-bit G' in two parts, high and low: of 1 to 8 rows it was up to 1.8 times as far off with one part
-// (17 rows x 128256 x 2048 in bf16: 494 us with one, 509 with two).  These parts are of m G', m 2^e the rows' weights, and the hidden states are multiplied by 2^e
+// (17 rows x 128256 x 2048 in bf16: 494 us with one, 509 with two, 514 with the plane for the other gradient).  These parts are of m G', m 2^e the rows' weights, and the hidden states are multiplied by 2^e
 // alone, which rounds nothing, so that the gradient is off by its own rounding, whatever the weights (with the weights in the hidden
 // states it was up to 1.43 times as far off).  The gradient of the hidden states, and many rows' of the weight, read G' as it is: its -1 at the target is
 // exact, and m would make it a number that is rounded (1000 rows of one weight: 1.60 times as far off as an fp32 result rounded once, now 1.03).
@@ -859,7 +860,7 @@ struct HeadWeightArgs {
     long long out_stride;
 };
 // Gradient of the weight: G'^T (weighted H), both operands k strided: twice the LDS reads of 16 bytes a row, as the transposing read gives 8.
-// 4096 rows x 32256 tokens x 4096 in bf16: 0.82 to 0.85 ms, 1.27 to 1.32 PFLOP/s.
+// 4096 rows x 32256 tokens x 4096 in bf16: 0.82 ms, 1.32 PFLOP/s.
 template <typename T, typename S, int TERMS, int DT>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_head_grad_weight(HeadWeightArgs a)
 {

@@ -112,10 +112,11 @@ static bool by_shape(ShapeId id, F f)
 }
 
 // fp32 values go as two fp16 parts, at a third of the rate of 16-bit values and nearly three times that of fp32 products, where that gains more than
-// laying out the parts costs: in us, a few launches and 12 bytes (gradients: 16) for each value of the weight.  Measured, in parts / as they are,
-// 32000 x 1024: loss of 128 rows 203 / 70, 300 rows 235 / 159, 512 rows 239 / 244; loss and gradients of 128 rows 541 / 300, 200 rows 629 / 513,
-// 300 rows 693 / 737 (604 with the loss as it is and the gradients in parts); 128256 x 2048: loss of 200 rows 1065 / 944, 300 rows
-// 1261 / 1405, loss and gradients of 128 rows 2896 / 2086, 200 rows 3226 / 3768.
+// laying out the parts costs: in us, a few launches and 12 bytes (gradients: 16) for each value of the weight.  The line is drawn on the side of the
+// values as they are, which lose nothing.  Measured, in parts / as they are (with the loss as it is, where it differs), 32000 x 1024: loss of 128 rows
+// 118 / 69, 200 rows 120 / 125, 300 rows 149 / 160, 512 rows 150 / 242; loss and gradients of 128 rows 360 / 298, 200 rows 425 / 514, 300 rows
+// 510 / 682 (517), 512 rows 569 / 1001; 128256 x 2048: loss of 200 rows 1002 / 942, 300 rows 1195 / 1209; loss and gradients of 128
+// rows 2737 / 2091, 200 rows 3058 / 3821 (2951), 300 rows 3757 / 5164.
 static bool in_parts(int dtype, int call, int rows, int vocab, int width)
 {
     const double weight = (double)vocab * width, product = 2.0 * rows * weight;
