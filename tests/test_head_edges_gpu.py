@@ -69,3 +69,53 @@ def test_one_workspace_for_calls_of_several_sizes(svip, dtype):
         h, w, y, r = (t.contiguous() for t in inputs(N, V, D, dtype, N))
         want, got = run_loss(svip, h, w, y, 1.0, r), run_loss(svip, h, w, y, 1.0, r, ws)
         assert all(torch.equal(want[k], got[k]) for k in want)
+
+
+@pytest.mark.parametrize("dtype,N,V,D", [("f16", 33, 3000, 256), ("f16", 300, 3000, 256), ("bf16", 33, 3000, 256), ("f32", 1024, 20000, 520)])
+def test_replayed_graph_of_rows_of_different_weights(svip, dtype, N, V, D):
+    """Loss and gradients captured once and replayed over new inputs between eager work, rows of other weights and other rows without a target each
+    time; fp32 in parts, whose maxima the workspace holds.  One workspace for the eager calls and the graph, one after the other."""
+    h, w, y, r = (t.contiguous() for t in inputs(N, V, D, dtype, 43))
+    ws = svip.new_head_workspace(svip.HEAD_LOSS_GRAD, h.dtype, N, V, D)
+    out = run_loss(svip, h, w, y, 1.0, r, ws)
+
+    def step():
+        svip.head_loss(h, w, y, loss_out=out["loss"], lse_out=out["lse"], workspace=ws)
+        svip.head_loss_grad(h, w, y, lse=out["lse"], grad_loss=r, grad_hidden_out=out["dh"], grad_weight_out=out["dw"], workspace=ws)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        g = gen(200 + i)
+        h.copy_(torch.randn(N, D, device="cuda", generator=g) * 4.0 ** i)
+        w.copy_(torch.randn(V, D, device="cuda", generator=g) * 0.05)
+        y.copy_(torch.randint(-V // 4, V, (N,), device="cuda", generator=g))
+        r.copy_(10.0 ** (i - 4.0 * torch.rand(N, device="cuda", generator=g)))
+        step()
+        torch.cuda.synchronize()
+        want = {k: v.clone() for k, v in out.items()}
+        for v in out.values():
+            v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in out:
+            assert torch.equal(out[k].view(torch.uint8), want[k].view(torch.uint8)), (i, k)
+
+
+def test_two_calls_at_once_on_streams_of_their_own(svip):
+    """fp16 and fp32 in parts, each in its own workspace full of what another call left."""
+    cases = [tuple(t.contiguous() for t in inputs(N, V, D, dtype, N)) for N, V, D, dtype in
+             ((300, 5000, 256, "f16"), (40, 9000, 136, "f16"), (1024, 20000, 520, "f32"))]
+    spaces = [svip.new_head_workspace(svip.HEAD_LOSS_GRAD, h.dtype, h.shape[0], w.shape[0], h.shape[1]) for h, w, _, _ in cases]
+    want = [run_loss(svip, h, w, y, 1.0, r) for h, w, y, r in cases]
+    for ws in spaces:
+        ws[256:] = 0x7f
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in cases], []
+    for (h, w, y, r), ws, s in zip(cases, spaces, streams):
+        with torch.cuda.stream(s):
+            got.append(run_loss(svip, h, w, y, 1.0, r, ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a[k], b[k]) for a, b in zip(want, got) for k in a)
