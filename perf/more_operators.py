@@ -218,7 +218,7 @@ def prepare(case, seed):
         import paper_2411_18462_amd as svip
 
         if kind == "logits":
-            s["workspace"] = svip.new_head_workspace(svip.HEAD_LOGITS_MX4, DTYPES[case["out"]], case["N"], case["V"], case["K"])
+            s["workspace"] = svip.new_head_workspace(svip.HEAD_LOGITS_MX, DTYPES[case["out"]], case["N"], case["V"], case["K"])
         elif kind == "sample":
             s["workspace"] = svip.new_sample_workspace(DTYPES[case["dtype"]], case["N"], case["V"])
     return s
@@ -231,14 +231,14 @@ def _own(s):
 
     kind = s["case"]["kind"]
     if kind == "quantize":
-        svip.quantize_mx4(s["x"], q_out=s["q"], scale_out=s["scale"])
-        svip.mx4_rows(s["q"], s["scale"], out=s["values"])
+        svip.quantize_mx(s["x"], q_out=s["q"], scale_out=s["scale"])
+        svip.mx_rows(s["q"], s["scale"], out=s["values"])
         return {"values": s["values"]}
     if kind == "rows":
-        svip.mx4_rows(s["q"], s["scale"], ids=s["ids"], out=s["values"])
+        svip.mx_rows(s["q"], s["scale"], ids=s["ids"], out=s["values"])
         return {"values": s["values"]}
     if kind == "logits":
-        svip.head_logits_mx4(s["hq"], s["hs"], s["wq"], s["ws"], logits_out=s["logits"], workspace=s["workspace"])
+        svip.head_logits_mx(s["hq"], s["hs"], s["wq"], s["ws"], logits_out=s["logits"], workspace=s["workspace"])
         return {"logits": s["logits"]}
     svip.sample(s["logits"], u=s["u"], temperature=s["temperature"], top_k=s["top_k"], top_p=s["top_p"], min_p=s["min_p"], token_out=s["token"],
                 prob_out=s["prob"], kept_out=s["kept"], workspace=s["workspace"])
