@@ -16,13 +16,15 @@ _native = None
 MAX_K = 1024
 FLAG_BAD_TOKEN = 1
 FLAG_BAD_DRAFT_LEN = 2
+FLAG_BAD_SETTING = 4
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 # every symbol include/svip.h declares
 EXPORTS = ("svip_status_string", "svip_workspace_bytes", "svip_workspace_needed", "svip_workspace_reset",
            "svip_workspace_flags", "svip_draft_step", "svip_draft_step_static", "svip_verify", "svip_draft_step_greedy",
            "svip_verify_greedy", "svip_pair_stats", "svip_warp_logits", "svip_loop_workspace_bytes", "svip_loop_init", "svip_loop_run",
-           "svip_head_workspace_bytes", "svip_quantize_blocks", "svip_head_logits", "svip_head_loss", "svip_head_loss_grad")
+           "svip_head_workspace_bytes", "svip_quantize_blocks", "svip_head_logits", "svip_head_loss", "svip_head_loss_grad",
+           "svip_quantize_mx", "svip_mx_rows", "svip_head_logits_mx", "svip_sample_workspace_bytes", "svip_sample")
 # every symbol include/svip_bench.h declares (benchmark and experiment hooks, not the product ABI)
 BENCH_EXPORTS = ("svip_bench_time_kernels", "svip_bench_events_used", "svip_bench_set_tuning",
                  "svip_bench_warp_routes", "svip_bench_empty_kernel", "svip_bench_stream_sink_words", "svip_bench_stream_read")
@@ -109,6 +111,16 @@ def load():
     lib.svip_head_loss.argtypes = [vp, vp, i, i, i, i, ll, ll, f, vp, vp, vp, vp, sz, vp]
     lib.svip_head_loss_grad.restype = i
     lib.svip_head_loss_grad.argtypes = [vp, vp, i, i, i, i, ll, ll, f, vp, vp, vp, vp, ll, vp, ll, vp, sz, vp]
+    lib.svip_quantize_mx.restype = i
+    lib.svip_quantize_mx.argtypes = [vp, i, i, i, ll, vp, ll, vp, ll, vp]
+    lib.svip_mx_rows.restype = i
+    lib.svip_mx_rows.argtypes = [vp, vp, i, i, ll, ll, vp, i, vp, i, ll, vp]
+    lib.svip_head_logits_mx.restype = i
+    lib.svip_head_logits_mx.argtypes = [vp, vp, i, vp, vp, i, i, i, ll, ll, ll, ll, vp, i, ll, vp, sz, vp]
+    lib.svip_sample_workspace_bytes.restype = sz
+    lib.svip_sample_workspace_bytes.argtypes = [i, i, i]
+    lib.svip_sample.restype = i
+    lib.svip_sample.argtypes = [vp, i, i, i, ll, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.svip_bench_time_kernels.restype = i
     lib.svip_bench_time_kernels.argtypes = [i, ctypes.POINTER(vp), ctypes.POINTER(vp), i]
     lib.svip_bench_events_used.restype = i
@@ -127,7 +139,8 @@ def load():
 
     _marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                     for f in (lib.svip_draft_step, lib.svip_draft_step_greedy, lib.svip_verify, lib.svip_verify_greedy,
-                            lib.svip_quantize_blocks, lib.svip_head_logits)))
+                            lib.svip_quantize_blocks, lib.svip_head_logits, lib.svip_quantize_mx, lib.svip_mx_rows, lib.svip_head_logits_mx,
+                            lib.svip_sample)))
     _lib, _native = lib, _marshal
     return lib
 
@@ -441,12 +454,12 @@ class Loop:
         return workspace_flags(self.workspace)
 
 
-HEAD_LOGITS, HEAD_LOSS, HEAD_LOSS_GRAD = 0, 1, 2
+HEAD_LOGITS, HEAD_LOSS, HEAD_LOSS_GRAD, HEAD_LOGITS_MX = 0, 1, 2, 3
 HEAD_BLOCK = 128
 
 
 def head_workspace_bytes(call: int, dtype, N: int, V: int, D: int) -> int:
-    """svip_head_workspace_bytes; dtype a torch dtype, call HEAD_LOGITS, HEAD_LOSS or HEAD_LOSS_GRAD."""
+    """svip_head_workspace_bytes; dtype a torch dtype, call HEAD_LOGITS, HEAD_LOSS, HEAD_LOSS_GRAD or HEAD_LOGITS_MX."""
     return int(load().svip_head_workspace_bytes(int(call), _DTYPES.get(dtype, -1), int(N), int(V), int(D)))
 
 
@@ -561,6 +574,121 @@ def head_loss_grad(hidden, weight, targets, *, temperature=1.0, lse, grad_loss, 
             outs += _rows(t, tuple(like.shape), hidden.dtype, name) if t is not None else (None, 0)
         _check(load().svip_head_loss_grad(*head, _vector(lse, N, torch.float32, "lse"), _vector(grad_loss, N, torch.float32, "grad_loss"), *outs,
                                           _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+
+
+MX_BLOCK = 32
+
+
+def _mx(q, scale, rows, name):
+    """Pointers and strides of a 4-bit matrix and its scales, and its K."""
+    if q.dim() != 2:
+        raise ValueError(f"{name}_q must be a matrix")
+    rows, K = q.shape[0] if rows is None else rows, 2 * q.shape[1]
+    pq, sq = _rows(q, (rows, K // 2), torch.float4_e2m1fn_x2, f"{name}_q")
+    ps, ss = _rows(scale, (rows, K // MX_BLOCK), torch.float8_e8m0fnu, f"{name}_scale")
+    return pq, sq, ps, ss, K
+
+
+def quantize_mx(x, *, q_out, scale_out, stream=None):
+    """svip_quantize_mx.  x [rows, cols] float32, bfloat16 or float16; q_out [rows, K / 2] float4_e2m1fn_x2, K = cols filled up to a multiple of
+    128; scale_out [rows, K / 32] float8_e8m0fnu."""
+    status = (_native or _load_native()).quantize_mx(x, q_out, scale_out, None if stream is None else _stream(stream))
+    if status != _DECLINED:
+        return _check(status) if status else None
+    if x.dtype not in _DTYPES:
+        raise SvipError(3, "x must be float32, bfloat16 or float16")
+    with _on_one_device(x=x, q_out=q_out, scale_out=scale_out):
+        px, sx = _rows(x, None, None, "x")
+        rows, cols = x.shape
+        K = -(-cols // HEAD_BLOCK) * HEAD_BLOCK
+        if q_out.dim() != 2 or q_out.shape[1] != K // 2:
+            raise ValueError(f"q_out must be a matrix [{rows}, {K // 2}]")
+        pq, sq, ps, ss, _ = _mx(q_out, scale_out, rows, "out")
+        _check(load().svip_quantize_mx(px, _DTYPES[x.dtype], rows, cols, sx, pq, sq, ps, ss, _stream(stream)))
+
+
+def mx_rows(q, scale, *, ids=None, out, stream=None):
+    """svip_mx_rows.  q [rows, K / 2] float4_e2m1fn_x2, scale [rows, K / 32] float8_e8m0fnu; ids int32 [n] or None (rows 0 .. n - 1); out [n, cols]
+    float32, bfloat16 or float16, K - 128 < cols <= K."""
+    status = (_native or _load_native()).mx_rows(q, scale, ids, out, None if stream is None else _stream(stream))
+    if status != _DECLINED:
+        return _check(status) if status else None
+    if out.dtype not in _DTYPES:
+        raise SvipError(3, "out must be float32, bfloat16 or float16")
+    with _on_one_device(q=q, scale=scale, ids=ids, out=out):
+        pq, sq, ps, ss, K = _mx(q, scale, None, "matrix")
+        po, so = _rows(out, None, None, "out")
+        n, cols = out.shape
+        if -(-cols // HEAD_BLOCK) * HEAD_BLOCK != K:
+            raise ValueError(f"out must have {K} columns, or fewer of its last {HEAD_BLOCK}")
+        pi = _vector(ids, n, torch.int32, "ids") if ids is not None else None
+        _check(load().svip_mx_rows(pq, ps, q.shape[0], cols, sq, ss, pi, n, po, _DTYPES[out.dtype], so, _stream(stream)))
+
+
+def head_logits_mx(hidden_q, hidden_scale, weight_q, weight_scale, *, logits_out, workspace, stream=None):
+    """svip_head_logits_mx.  weight_q [V, K / 2] float4_e2m1fn_x2, weight_scale [V, K / 32] float8_e8m0fnu; hidden_q [N, K / 2] and hidden_scale
+    [N, K / 32] of the same types, or hidden_q [N, K] float8_e4m3fn and hidden_scale [N, K / 128]; logits_out [N, V] float32 (4-bit hidden states
+    only), bfloat16 or float16."""
+    status = (_native or _load_native()).head_logits_mx(hidden_q, hidden_scale, weight_q, weight_scale, logits_out, workspace,
+                                                         None if stream is None else _stream(stream))
+    if status != _DECLINED:
+        return _check(status) if status else None
+    bits = {torch.float4_e2m1fn_x2: 4, torch.float8_e4m3fn: 8}.get(hidden_q.dtype)
+    if bits is None:
+        raise SvipError(3, "hidden_q must be float4_e2m1fn_x2 or float8_e4m3fn")
+    if logits_out.dtype not in _DTYPES or (bits == 8 and logits_out.dtype == torch.float32):
+        raise SvipError(3, "logits_out must be float32 (4-bit hidden states only), bfloat16 or float16")
+    with _on_one_device(hidden_q=hidden_q, hidden_scale=hidden_scale, weight_q=weight_q, weight_scale=weight_scale, logits_out=logits_out,
+                        workspace=workspace):
+        pw, sw, pws, sws, K = _mx(weight_q, weight_scale, None, "weight")
+        V, N = weight_q.shape[0], hidden_q.shape[0]
+        if bits == 4:
+            ph, sh, phs, shs, Kh = _mx(hidden_q, hidden_scale, None, "hidden")
+            if Kh != K:
+                raise ValueError(f"hidden_q must be a matrix [{N}, {K // 2}]")
+        else:
+            ph, sh = _rows(hidden_q, (N, K), torch.float8_e4m3fn, "hidden_q")
+            phs, shs = _rows(hidden_scale, (N, K // HEAD_BLOCK), torch.float8_e8m0fnu, "hidden_scale")
+        po, so = _rows(logits_out, (N, V), None, "logits_out")
+        _check(load().svip_head_logits_mx(ph, phs, bits, pw, pws, N, V, K, sh, shs, sw, sws, po, _DTYPES[logits_out.dtype], so,
+                                           _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+
+
+def sample_workspace_bytes(dtype, N: int, V: int) -> int:
+    """svip_sample_workspace_bytes; dtype a torch dtype."""
+    return int(load().svip_sample_workspace_bytes(_DTYPES.get(dtype, -1), int(N), int(V)))
+
+
+def new_sample_workspace(dtype, N: int, V: int, device="cuda", stream=None) -> torch.Tensor:
+    """Allocate a workspace for sample() of up to these sizes and zero its flag word."""
+    n = sample_workspace_bytes(dtype, N, V)
+    if n == 0:
+        raise SvipError(2, "svip_sample_workspace_bytes: bad dtype, N or V")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    with torch.cuda.device(ws.device):
+        _check(load().svip_workspace_reset(ws.data_ptr(), n, _stream(stream)))
+    return ws
+
+
+def sample(logits, *, u, temperature=None, top_k=None, top_p=None, min_p=None, token_out, prob_out=None, kept_out=None, workspace, stream=None):
+    """svip_sample.  logits [N, V] (unit stride along V) float32, bfloat16 or float16; u, temperature, top_p, min_p float32 [N], top_k int32 [N],
+    the settings each or None (1, off, off, off); token_out int32 [N]; prob_out float32 [N] and kept_out int32 [N], or None."""
+    status = (_native or _load_native()).sample(logits, u, temperature, top_k, top_p, min_p, token_out, prob_out, kept_out, workspace,
+                                                None if stream is None else _stream(stream))
+    if status != _DECLINED:
+        return _check(status) if status else None
+    if logits.dtype not in _DTYPES:
+        raise SvipError(3, "logits must be float32, bfloat16 or float16")
+    with _on_one_device(logits=logits, u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, token_out=token_out, prob_out=prob_out,
+                        kept_out=kept_out, workspace=workspace):
+        pz, sz = _rows(logits, None, None, "logits")
+        N, V = logits.shape
+        f32, i32 = torch.float32, torch.int32
+        vector = lambda t, dtype, name: _vector(t, N, dtype, name) if t is not None else None  # noqa: E731
+        _check(load().svip_sample(
+            pz, _DTYPES[logits.dtype], N, V, sz, vector(temperature, f32, "temperature"), vector(top_k, i32, "top_k"), vector(top_p, f32, "top_p"),
+            vector(min_p, f32, "min_p"), _vector(u, N, f32, "u"), _vector(token_out, N, i32, "token_out"), vector(prob_out, f32, "prob_out"),
+            vector(kept_out, i32, "kept_out"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
 
 
 def bench_time_kernels(kernel_class: int, start_events, stop_events):

@@ -9,7 +9,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", "svip_kernels.hip"), os.path.join(HERE, "csrc", "svip_loop.hip"),
-           os.path.join(HERE, "csrc", "svip_head.hip")]
+           os.path.join(HERE, "csrc", "svip_head.hip"), os.path.join(HERE, "csrc", "svip_mx.hip"), os.path.join(HERE, "csrc", "svip_sample.hip")]
 ABI = os.path.join(ROOT, "include", "svip.h")
 HEADERS = sorted(os.path.join(HERE, "csrc", f) for f in os.listdir(os.path.join(HERE, "csrc")) if f.endswith(".h")) + [ABI]
 LIB = os.path.join(HERE, "libsvip.so")

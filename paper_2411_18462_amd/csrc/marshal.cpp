@@ -24,6 +24,10 @@ decltype(&svip_verify) g_verify;
 decltype(&svip_verify_greedy) g_verify_greedy;
 decltype(&svip_quantize_blocks) g_quantize_blocks;
 decltype(&svip_head_logits) g_head_logits;
+decltype(&svip_quantize_mx) g_quantize_mx;
+decltype(&svip_mx_rows) g_mx_rows;
+decltype(&svip_head_logits_mx) g_head_logits_mx;
+decltype(&svip_sample) g_sample;
 
 // A plain dense device tensor, or nullptr: no subclass, nothing wrapped by a transform (those have no pointer to give).
 const at::Tensor *device_tensor(PyObject *o)
@@ -108,6 +112,13 @@ struct Args {
         }
         *stride = t->size(0) > 1 ? t->stride(0) : (t->size(1) + 15) / 16 * 16;       // (of one row there is none: any that is aligned)
         return t;
+    }
+    // A 4-bit matrix [rows, cols / 2], rows and cols of any size where negative, and its scales, which come next
+    const at::Tensor *mx(long long rows, long long cols, long long *stride, const at::Tensor **scale, long long *scale_stride)
+    {
+        const at::Tensor *q = matrix(at::ScalarType::Float4_e2m1fn_x2, rows, cols < 0 ? cols : cols / 2, stride);
+        *scale = ok ? matrix(at::kFloat8_e8m0fnu, q->size(0), q->size(1) / 16, scale_stride) : nullptr;
+        return q;
     }
     const at::Tensor *workspace()
     {
@@ -317,15 +328,140 @@ PyObject *head_logits(PyObject *, PyObject *const *argv, Py_ssize_t n)
     });
 }
 
-// bind(addresses of svip_draft_step, svip_draft_step_greedy, svip_verify, svip_verify_greedy, svip_quantize_blocks, svip_head_logits)
+// quantize_mx(x, q_out, scale_out, stream)
+PyObject *quantize_mx(PyObject *, PyObject *const *argv, Py_ssize_t n)
+{
+    return answer([&]() -> long {
+        if (n != 4) return DECLINED;
+        Args a{argv};
+        long long sx = 0, sq = 0, ss = 0;
+        const at::Tensor *x = a.matrix(at::ScalarType::Undefined, -1, -1, &sx);
+        if (!a.ok) return DECLINED;
+        const int dtype = dtype_of(*x);
+        const long long rows = x->size(0), cols = x->size(1);
+        const at::Tensor *s = nullptr, *q = a.mx(rows, (cols + 127) / 128 * 128, &sq, &s, &ss);
+        if (!a.ok) return DECLINED;
+        void *stream = a.stream();
+        if (!a.ok || dtype < 0 || !fits(rows) || !fits(cols)) return DECLINED;
+        const void *xp = x->data_ptr();
+        void *qp = q->data_ptr(), *sp = s->data_ptr();
+        long status;
+        Py_BEGIN_ALLOW_THREADS
+        status = g_quantize_mx(xp, dtype, (int)rows, (int)cols, sx, qp, sq, sp, ss, stream);
+        Py_END_ALLOW_THREADS
+        return status;
+    });
+}
+
+// mx_rows(q, scale, ids or None, out, stream)
+PyObject *mx_rows(PyObject *, PyObject *const *argv, Py_ssize_t n)
+{
+    return answer([&]() -> long {
+        if (n != 5) return DECLINED;
+        Args a{argv};
+        long long sq = 0, ss = 0, so = 0;
+        const at::Tensor *s = nullptr, *q = a.mx(-1, -1, &sq, &s, &ss);
+        if (!a.ok) return DECLINED;
+        const at::Tensor *ids = argv[a.i] == Py_None ? nullptr : device_tensor(argv[a.i]);
+        if (argv[a.i++] != Py_None && (!ids || ids->scalar_type() != at::kInt || ids->dim() != 1 || !ids->is_contiguous())) return DECLINED;
+        const at::Tensor *out = a.matrix(at::ScalarType::Undefined, ids ? ids->size(0) : -1, -1, &so);
+        if (!a.ok) return DECLINED;
+        const int dtype = dtype_of(*out);
+        const long long rows = q->size(0), count = out->size(0), cols = out->size(1);
+        void *stream = a.stream();
+        if (!a.ok || dtype < 0 || !fits(rows) || !fits(count) || !fits(cols) || (cols + 127) / 128 * 128 != 2 * q->size(1) ||
+            (ids && ids->device() != q->device()))
+            return DECLINED;
+        const void *qp = q->data_ptr(), *sp = s->data_ptr();
+        const int *ip = ids ? static_cast<const int *>(ids->data_ptr()) : nullptr;
+        void *op = out->data_ptr();
+        long status;
+        Py_BEGIN_ALLOW_THREADS
+        status = g_mx_rows(qp, sp, (int)rows, (int)cols, sq, ss, ip, (int)count, op, dtype, so, stream);
+        Py_END_ALLOW_THREADS
+        return status;
+    });
+}
+
+// head_logits_mx(hidden_q, hidden_scale, weight_q, weight_scale, logits_out, workspace, stream)
+PyObject *head_logits_mx(PyObject *, PyObject *const *argv, Py_ssize_t n)
+{
+    return answer([&]() -> long {
+        if (n != 7) return DECLINED;
+        Args a{argv};
+        long long sh = 0, shs = 0, sw = 0, sws = 0, so = 0;
+        const at::Tensor *first = device_tensor(argv[0]);
+        if (!first) return DECLINED;
+        const int bits = first->scalar_type() == at::ScalarType::Float4_e2m1fn_x2 ? 4 : first->scalar_type() == at::kFloat8_e4m3fn ? 8 : 0;
+        if (!bits) return DECLINED;
+        const at::Tensor *h = a.matrix(first->scalar_type(), -1, -1, &sh);
+        if (!a.ok) return DECLINED;
+        const long long N = h->size(0), K = h->size(1) * 8 / bits;
+        const at::Tensor *hs = a.matrix(at::kFloat8_e8m0fnu, N, bits == 4 ? K / 32 : K / 128, &shs), *ws = nullptr;
+        if (!a.ok) return DECLINED;
+        const at::Tensor *w = a.mx(-1, K, &sw, &ws, &sws);
+        if (!a.ok) return DECLINED;
+        const long long V = w->size(0);
+        const at::Tensor *out = a.matrix(at::ScalarType::Undefined, N, V, &so);
+        const at::Tensor *space = a.workspace();
+        void *stream = a.stream();
+        if (!a.ok || !fits(N) || !fits(V) || !fits(K) || space->device() != h->device()) return DECLINED;
+        const int dtype = dtype_of(*out);
+        if (dtype < 0 || (bits == 8 && dtype == SVIP_F32)) return DECLINED;
+        const void *hp = h->data_ptr(), *hsp = hs->data_ptr(), *wp = w->data_ptr(), *wsp = ws->data_ptr();
+        void *op = out->data_ptr(), *sp = space->data_ptr();
+        const size_t sn = (size_t)space->numel();
+        long status;
+        Py_BEGIN_ALLOW_THREADS
+        status = g_head_logits_mx(hp, hsp, bits, wp, wsp, (int)N, (int)V, (int)K, sh, shs, sw, sws, op, dtype, so, sp, sn, stream);
+        Py_END_ALLOW_THREADS
+        return status;
+    });
+}
+
+// sample(logits, u, temperature, top_k, top_p, min_p, token_out, prob_out, kept_out, workspace, stream), settings, prob_out and kept_out each or None
+PyObject *sample(PyObject *, PyObject *const *argv, Py_ssize_t n)
+{
+    return answer([&]() -> long {
+        if (n != 11) return DECLINED;
+        Args a{argv};
+        long long sz = 0;
+        const at::Tensor *z = a.matrix(at::ScalarType::Undefined, -1, -1, &sz);
+        if (!a.ok) return DECLINED;
+        const int dtype = dtype_of(*z);
+        const long long N = z->size(0), V = z->size(1);
+        const float *u = a.array<float>(at::kFloat, false, N), *T = a.array<float>(at::kFloat, true, N);
+        const int *k = a.array<int>(at::kInt, true, N);
+        const float *p = a.array<float>(at::kFloat, true, N), *m = a.array<float>(at::kFloat, true, N);
+        int *token = a.array<int>(at::kInt, false, N);
+        float *prob = a.array<float>(at::kFloat, true, N);
+        int *kept = a.array<int>(at::kInt, true, N);
+        const at::Tensor *space = a.workspace();
+        void *stream = a.stream();
+        if (!a.ok || dtype < 0 || !fits(N) || !fits(V)) return DECLINED;
+        for (int i = 1; i < 10; ++i)
+            if (argv[i] != Py_None && device_tensor(argv[i])->device() != z->device()) return DECLINED;
+        const void *zp = z->data_ptr();
+        void *sp = space->data_ptr();
+        const size_t sn = (size_t)space->numel();
+        long status;
+        Py_BEGIN_ALLOW_THREADS
+        status = g_sample(zp, dtype, (int)N, (int)V, sz, T, k, p, m, u, token, prob, kept, sp, sn, stream);
+        Py_END_ALLOW_THREADS
+        return status;
+    });
+}
+
+// bind(addresses of svip_draft_step, svip_draft_step_greedy, svip_verify, svip_verify_greedy, svip_quantize_blocks, svip_head_logits,
+//      svip_quantize_mx, svip_mx_rows, svip_head_logits_mx, svip_sample)
 PyObject *bind(PyObject *, PyObject *const *argv, Py_ssize_t n)
 {
-    void *f[6];
-    if (n != 6) {
-        PyErr_SetString(PyExc_TypeError, "bind takes six addresses");
+    void *f[10];
+    if (n != 10) {
+        PyErr_SetString(PyExc_TypeError, "bind takes ten addresses");
         return nullptr;
     }
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < 10; ++i) {
         f[i] = PyLong_AsVoidPtr(argv[i]);
         if (!f[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: a null address");
@@ -338,6 +474,10 @@ PyObject *bind(PyObject *, PyObject *const *argv, Py_ssize_t n)
     g_verify_greedy = reinterpret_cast<decltype(g_verify_greedy)>(f[3]);
     g_quantize_blocks = reinterpret_cast<decltype(g_quantize_blocks)>(f[4]);
     g_head_logits = reinterpret_cast<decltype(g_head_logits)>(f[5]);
+    g_quantize_mx = reinterpret_cast<decltype(g_quantize_mx)>(f[6]);
+    g_mx_rows = reinterpret_cast<decltype(g_mx_rows)>(f[7]);
+    g_head_logits_mx = reinterpret_cast<decltype(g_head_logits_mx)>(f[8]);
+    g_sample = reinterpret_cast<decltype(g_sample)>(f[9]);
     Py_RETURN_NONE;
 }
 
@@ -348,6 +488,10 @@ PyMethodDef methods[] = {
     {"verify_greedy", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(verify_greedy)), METH_FASTCALL, nullptr},
     {"quantize_blocks", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(quantize_blocks)), METH_FASTCALL, nullptr},
     {"head_logits", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(head_logits)), METH_FASTCALL, nullptr},
+    {"quantize_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(quantize_mx)), METH_FASTCALL, nullptr},
+    {"mx_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(mx_rows)), METH_FASTCALL, nullptr},
+    {"head_logits_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(head_logits_mx)), METH_FASTCALL, nullptr},
+    {"sample", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(sample)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "native argument marshalling of binding.py", -1, methods};
 

@@ -1,0 +1,370 @@
+// Kernels of the head in 4 bits: quantisation, rows read back by token, and the product with the hidden states.
+//
+// A value is a code of e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, two to a byte, the even column's in the low half) times its block's
+// scale, a power of two as e8m0, for 32 neighbours of a row.  The matrix cores multiply such codes and take a scale for each 32 values along K
+// themselves (16x16x128: lane l holds 32 values of row l % 16, those of block l / 16).  All products of two codes of a block lie within 2^8 of one another,
+// so nothing is lost ahead of the sums in fp32.
+#pragma once
+#include "../../include/svip.h"
+#include "head_store.h"
+
+namespace svip {
+
+constexpr int MX_BLOCK = 32, MX_RUN = 128;             // values to a scale; rows are filled up to whole runs
+constexpr int E8M0_NAN = 255;
+
+// ---- quantisation ------------------------------------------------------------------------------------------------------------------------
+//
+// The scale is 2^e with the least e >= -127 that brings the block's largest magnitude to 6, the largest e2m1 number, or below (no value is
+// cut off); dividing by it is exact, so a code is x / 2^e rounded once.  e2m1 has no NaN: a block that holds a value that is not finite has the
+// scale 255, the NaN of e8m0, and codes of zero.
+
+__device__ __forceinline__ int mx_scale_code(unsigned amax)         // of the bits of the largest magnitude, e + 127; 127 for a block of zeros
+{
+    if (amax >= 0x7f800000u) return E8M0_NAN;
+    if (amax == 0u) return 127;
+    const int e = (int)(amax >> 23) - 2 + ((amax & 0x7fffffu) > 0x400000u);        // 6 = 1.5 * 2^2
+    return e < 0 ? 0 : e;
+}
+// 2^(127 - code): at most 253 for finite values
+__device__ __forceinline__ float mx_inverse(int code) { return code == E8M0_NAN ? 0.f : __uint_as_float((unsigned)(254 - code) << 23); }
+// 2^(code - 127)
+__device__ __forceinline__ float mx_scale(int code)
+{
+    return code == E8M0_NAN ? NAN : __uint_as_float(code == 0 ? 0x00400000u : (unsigned)code << 23);
+}
+
+struct MxQuantizeArgs {
+    const void *x;
+    long long row_stride;      // elements
+    int rows, cols, runs;      // runs: of 128 columns in a row
+    unsigned char *q;
+    long long q_stride;
+    unsigned char *scale;
+    long long scale_stride;
+};
+
+constexpr int MX_WG = 256;
+// 16 lanes (fp32: 32) a run, one load and one store a lane.
+template <int DT>
+__global__ __launch_bounds__(MX_WG) void k_mx_quantize(MxQuantizeArgs a)
+{
+    constexpr int VEC = Stored<DT>::VEC, LANES = MX_RUN / VEC, PER_BLOCK = MX_BLOCK / VEC;
+    using X = typename Stored<DT>::type;
+    const unsigned run = blockIdx.x * (MX_WG / LANES) + threadIdx.x / LANES;
+    if (run >= (unsigned)a.rows * (unsigned)a.runs) return;
+    const unsigned r = run / (unsigned)a.runs, c = (run - r * (unsigned)a.runs) * MX_RUN + threadIdx.x % LANES * VEC;
+    const X *p = static_cast<const X *>(a.x) + (long long)r * a.row_stride + c;
+    float v[VEC];
+    if ((int)c + VEC <= a.cols) {              // (the memory takes a load of 16 bytes at any address)
+        typedef X vec __attribute__((ext_vector_type(VEC), aligned(sizeof(X))));
+        const vec w = *reinterpret_cast<const vec *>(p);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = (float)w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = (int)c + i < a.cols ? (float)p[i] : 0.f;
+    }
+    unsigned m = 0u;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = PER_BLOCK / 2; o; o /= 2) m = max(m, (unsigned)__shfl_xor((int)m, o));
+    const int code = mx_scale_code(m);
+    const float inv = mx_inverse(code);
+    unsigned q = 0u;
+    if (code != E8M0_NAN) {
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[0] * inv, v[1] * inv, 1.f, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[2] * inv, v[3] * inv, 1.f, 1);
+        if constexpr (VEC == 8) {
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4] * inv, v[5] * inv, 1.f, 2);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6] * inv, v[7] * inv, 1.f, 3);
+        }
+    }
+    unsigned char *to = a.q + (long long)r * a.q_stride + c / 2;
+    if constexpr (VEC == 8)
+        *reinterpret_cast<unsigned *>(to) = q;
+    else
+        *reinterpret_cast<unsigned short *>(to) = (unsigned short)q;
+    if (threadIdx.x % PER_BLOCK == 0) a.scale[(long long)r * a.scale_stride + c / MX_BLOCK] = (unsigned char)code;
+}
+
+// ---- rows read back ------------------------------------------------------------------------------------------------------------------------
+
+struct MxRowsArgs {
+    const unsigned char *q;
+    long long q_stride;
+    const unsigned char *scale;
+    long long scale_stride;
+    int rows, cols, chunks;    // chunks: of 8 columns in a row of the result
+    const int *ids;            // [n], or null: rows 0 .. n - 1
+    int n;
+    void *out;
+    long long out_stride;      // elements
+};
+
+// 8 values a lane: 4 bytes of codes, 16 or 32 bytes of values.
+template <int DT>
+__global__ __launch_bounds__(MX_WG) void k_mx_rows(MxRowsArgs a)
+{
+    using X = typename Stored<DT>::type;
+    const unsigned i = blockIdx.x * MX_WG + threadIdx.x, row = i / (unsigned)a.chunks;
+    if (row >= (unsigned)a.n) return;
+    const int c = (int)(i - row * (unsigned)a.chunks) * 8;
+    const int id = a.ids ? a.ids[row] : (int)row;
+    float v[8];
+    if (id >= 0 && id < a.rows) {
+        const unsigned q = *reinterpret_cast<const unsigned *>(a.q + id * a.q_stride + c / 2);
+        const float s = mx_scale(a.scale[id * a.scale_stride + c / MX_BLOCK]);
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const f2 w[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 3)};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = w[e / 2][e % 2] * s;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = id < 0 ? 0.f : NAN;
+    }
+    X *to = static_cast<X *>(a.out) + (long long)row * a.out_stride + c;
+    if (c + 8 <= a.cols) {
+        typedef X vec __attribute__((ext_vector_type(8), aligned(sizeof(X))));
+        vec w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (X)v[e];
+        *reinterpret_cast<vec *>(to) = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < a.cols) to[e] = (X)v[e];
+    }
+}
+
+// ---- logits --------------------------------------------------------------------------------------------------------------------------------
+
+struct MxLogitsArgs {
+    Operand weight, hidden;    // codes, in bytes; m = vocabulary, n = rows
+    Operand weight_scale, hidden_scale;
+    int N, V, K;               // K: values
+    Tiles tiles;
+    void *out;
+    long long out_stride;      // elements
+    int per_split;             // of K, a multiple of the step
+    float *part;               // [splits][N][part_stride] where there are several, null: one
+    long long part_stride;
+};
+
+constexpr int MX_STEP = 2 * STEP_BYTES;                // values of K to a step
+
+// Copies 4 bytes a lane into LDS at `lds` (wave-uniform) + 4 * lane; see copy_to_lds.
+__device__ __forceinline__ void copy4_to_lds(const char *lane_address, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(lane_address) : "memory", "m0");
+}
+
+// The scales of a step of ROWS rows of 4-bit codes: 8 bytes each, [ROWS][8] in LDS.
+template <int ROWS, int THREADS>
+struct ScaleStager {
+    static constexpr int WORDS = ROWS * 2, ROUNDS = WORDS > THREADS ? WORDS / THREADS : 1, BYTES = ROWS * 8;
+    static_assert(WORDS % 64 == 0 && (WORDS >= THREADS ? WORDS % THREADS == 0 : THREADS % WORDS == 0), "whole waves copy");
+    const char *base;
+    unsigned voff[ROUNDS], lds[ROUNDS];
+    __device__ void init(const Operand &o, int rows)
+    {
+        base = o.base;
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int c = (r * THREADS + (int)threadIdx.x) % WORDS, row = c >> 1;
+            lds[r] = (unsigned)__builtin_amdgcn_readfirstlane(c & ~63) * 4u;
+            voff[r] = (unsigned)(row < rows ? row : rows - 1) * (unsigned)o.stride + (unsigned)(c & 1) * 4u;
+        }
+    }
+    // k: of the step, k_end: values, a multiple of 128 (a step's second half may lie past it)
+    __device__ __forceinline__ void copy(unsigned at, int k, int k_end) const
+    {
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int mine = k + ((int)threadIdx.x & 1) * MX_RUN;
+            copy4_to_lds(mine < k_end ? base + (k / MX_BLOCK + voff[r]) : reinterpret_cast<const char *>(zero_line), at + lds[r]);
+        }
+    }
+};
+// Of a row's 8 scales those of the blocks that lane group g multiplies, g of either half: bytes 0 and 1.
+__device__ __forceinline__ int scales_of(const char *tile, int row, unsigned pick)
+{
+    const uint2 v = *reinterpret_cast<const uint2 *>(tile + row * 8);
+    return (int)__builtin_amdgcn_perm(v.y, v.x, pick);
+}
+
+// Scales of hidden states in 8 bits, one for 128 values: those of HELD steps in LDS at a time.
+constexpr int HELD = 32, HELD_PITCH = 2 * HELD + 4;
+
+__device__ __forceinline__ i32x8 wide(i32x4 v) { return __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1); }
+
+// Logits of a tile.  BITS: of the hidden states.
+template <typename S, int BITS, int DT>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_mx_logits(MxLogitsArgs a)
+{
+    constexpr int PLANES = BITS / 4;                   // a step of 8-bit hidden states is two tiles of 128 bytes a row
+    constexpr int STAGE = (S::BM + PLANES * S::BN) * STEP_BYTES, SCALES = (S::BM + (BITS == 4 ? S::BN : 0)) * 8;
+    __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * (STAGE + SCALES)];
+    __shared__ __attribute__((aligned(4))) unsigned char held[BITS == 8 ? S::BN * HELD_PITCH : 4];
+    const unsigned tiles = (unsigned)a.tiles.m * (unsigned)a.tiles.n, split = blockIdx.x / tiles;
+    int tm, tn;
+    tile_of(blockIdx.x - split * tiles, a.tiles, 4, tm, tn);
+    const int v0 = tm * S::BM, n0 = tn * S::BN, k0 = (int)split * a.per_split, k_end = min(a.K, k0 + a.per_split);
+    const auto from = [](Operand o, int row) {
+        o.base += (long long)row * o.stride;
+        return o;
+    };
+    Stager<KC, S::BM, S::THREADS, 1> sa;
+    Stager<KC, S::BN, S::THREADS, 1> sb;
+    ScaleStager<S::BM, S::THREADS> sw;
+    ScaleStager<S::BN, S::THREADS> sh;
+    sa.init(from(a.weight, v0), a.V - v0);
+    sb.init(from(a.hidden, n0), a.N - n0);
+    sw.init(from(a.weight_scale, v0), a.V - v0);
+    if (BITS == 4) sh.init(from(a.hidden_scale, n0), a.N - n0);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN, g = lane >> 4, l16 = lane & 15;
+    const unsigned pick = 0x0c0c0400u + 0x0101u * (unsigned)g;
+    Reader<KC, S::BM, 1> ra;
+    Reader<KC, S::BN, 1> rb;
+    ra.init(lane);
+    rb.init(lane);
+    f32x4 acc[S::FM][S::FN];
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    constexpr int COPIES = decltype(sa)::ROUNDS + PLANES * decltype(sb)::ROUNDS + decltype(sw)::ROUNDS + (BITS == 4 ? decltype(sh)::ROUNDS : 0);
+    const int steps = (k_end - k0 + MX_STEP - 1) / MX_STEP;
+    const unsigned lds0 = (unsigned)(uintptr_t)smem;
+    auto copy = [&](int s) {
+        const unsigned at = lds0 + (unsigned)(s % S::STAGES) * (STAGE + SCALES);
+        const int k = k0 + s * MX_STEP;
+        sa.copy(at, k / 2, k_end / 2, 0);
+        if (BITS == 4) {
+            sb.copy(at + S::BM * STEP_BYTES, k / 2, k_end / 2, 0);
+        } else {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) sb.copy(at + (S::BM + p * S::BN) * STEP_BYTES, k + p * MX_RUN, k_end, 0);
+        }
+        sw.copy(at + STAGE, k, k_end);
+        if (BITS == 4) sh.copy(at + STAGE + S::BM * 8, k, k_end);
+    };
+    // (8 bits) the scales of the steps from s0 on; nobody reads those of the steps before any more
+    auto hold = [&](int s0) {
+        const int count = min(2 * HELD, (k_end - k0) / MX_RUN - 2 * s0);
+        for (int i = threadIdx.x; i < S::BN * HELD / 2; i += S::THREADS) {
+            const int r = i / (HELD / 2), q = i % (HELD / 2) * 4, n = min(n0 + r, a.N - 1);
+            const char *p = a.hidden_scale.base + n * a.hidden_scale.stride + k0 / MX_RUN + 2 * s0 + q;
+            unsigned word = 0u;
+            if (q + 4 <= count)
+                __builtin_memcpy(&word, p, 4);
+            else
+                for (int e = 0; e < count - q; ++e) word |= (unsigned)(unsigned char)p[e] << (8 * e);
+            *reinterpret_cast<unsigned *>(held + r * HELD_PITCH + q) = word;
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s)
+        if (s < steps) copy(s);
+    for (int s = 0; s < steps; ++s) {
+        if (BITS == 8 && s % HELD == 0) {
+            if (s) __syncthreads();
+            hold(s);                       // (the barrier below publishes them)
+        }
+        if (s + S::STAGES - 2 < steps)
+            wait_copies_and_meet<(S::STAGES - 2) * COPIES>();
+        else
+            wait_copies_and_meet<0>();
+        if (s + S::STAGES - 1 < steps) copy(s + S::STAGES - 1);
+        const char *ta = smem + (s % S::STAGES) * (STAGE + SCALES), *tb = ta + S::BM * STEP_BYTES, *ts = ta + STAGE;
+        int sca[S::FM], scb[S::FN];
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) sca[i] = scales_of(ts, wm + 16 * i + l16, pick);
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            const int n = wn + 16 * j + l16;
+            scb[j] = BITS == 4 ? scales_of(ts + S::BM * 8, n, pick) : *reinterpret_cast<const unsigned short *>(held + n * HELD_PITCH + s % HELD * 2);
+        }
+        const auto half = [&](auto which) {
+            constexpr int H = decltype(which)::value;
+            i32x8 fa[S::FM], fb[S::FN];
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) {
+                if constexpr (BITS == 4) {
+                    s16x8 v;
+                    rb.half(tb, wn + 16 * j, H, v);
+                    fb[j] = wide(__builtin_bit_cast(i32x4, v));
+                } else {
+                    fb[j] = rb.whole(tb + H * S::BN * STEP_BYTES, wn + 16 * j);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                s16x8 v;
+                ra.half(ta, wm + 16 * i, H, v);
+                fa[i] = wide(__builtin_bit_cast(i32x4, v));
+            }
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 4, BITS == 4 ? 4 : 0, H, sca[i], H, scb[j]);
+        };
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
+    }
+    using X = typename Stored<DT>::type;
+    if (a.part) {
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            const int n = n0 + wn + 16 * j + l16;
+            if (n >= a.N) continue;
+            float *row = a.part + ((long long)split * a.N + n) * a.part_stride;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int v = v0 + wm + 16 * i + 4 * g;
+                if (v < a.part_stride) *reinterpret_cast<f32x4 *>(row + v) = acc[i][j];       // (V filled up to fours)
+            }
+        }
+    } else if constexpr (DT != SVIP_F32) {
+        store_rows<S, X>(smem, a.N - n0, a.V - v0, static_cast<X *>(a.out) + n0 * a.out_stride + v0, a.out_stride, [&](int i, int j) { return acc[i][j]; });
+    } else {
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            const int n = n0 + wn + 16 * j + l16;
+            if (n >= a.N) continue;
+            X *row = static_cast<X *>(a.out) + n * a.out_stride;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int v = v0 + wm + 16 * i + 4 * g;
+                if (v < a.V) put_up_to_4<DT>(row + v, acc[i][j], a.V - v);
+            }
+        }
+    }
+}
+
+struct MxJoinArgs {
+    const float *part;
+    long long part_stride;
+    int splits, N, V;
+    void *out;
+    long long out_stride;
+};
+// The sums of the splits of K, four logits a thread.
+template <int DT>
+__global__ __launch_bounds__(256) void k_mx_join(MxJoinArgs a)
+{
+    const int groups = (int)((a.part_stride + 1023) / 1024), n = blockIdx.x / groups;
+    const int v = ((blockIdx.x - n * groups) * 256 + (int)threadIdx.x) * 4;
+    if (v >= a.V) return;
+    const float *p = a.part + n * a.part_stride + v;
+    f32x4 s = *reinterpret_cast<const f32x4 *>(p);
+    for (int k = 1; k < a.splits; ++k) s += *reinterpret_cast<const f32x4 *>(p + (long long)k * a.N * a.part_stride);
+    put_up_to_4<DT>(static_cast<typename Stored<DT>::type *>(a.out) + n * a.out_stride + v, s, a.V - v);
+}
+
+}  // namespace svip

@@ -6,45 +6,16 @@
 #include <type_traits>
 
 #include "head_kernels.h"
+#include "host_calls.h"
+#include "svip_internal.h"
 
 namespace svip {
-
-static bool dtype_ok(int d) { return d == SVIP_F32 || d == SVIP_BF16 || d == SVIP_F16; }
-static int size_of(int d) { return d == SVIP_F32 ? 4 : 2; }
-static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
-static int up(int n, int to) { return (n + to - 1) / to * to; }
-static int ceil_div(long long n, long long d) { return (int)((n + d - 1) / d); }
-
-constexpr int HEAD_MAX_ROWS = 1 << 20;                 // of hidden states
-constexpr int HEAD_MAX_VOCAB = 1 << 22;
-constexpr int HEAD_MAX_WIDTH = 1 << 17;                // hidden channels
-constexpr long long HEAD_MAX_STRIDE = 1 << 23;         // elements: 256 rows of a tile lie within 32 bits of bytes
-
-constexpr long long MOST_THREADS = 0xffffffffLL;       // of a launch
 
 // A matrix of rows x cols of dtype: stride of a row in whole 16 bytes, within reach of a tile's 32-bit offsets.
 static svip_status check_matrix(const void *p, int dtype, int cols, long long stride)
 {
     if (stride < cols || stride > HEAD_MAX_STRIDE) return SVIP_ERR_SHAPE;
     return aligned16(p) && stride * size_of(dtype) % 16 == 0 ? SVIP_OK : SVIP_ERR_ALIGN;
-}
-
-template <typename A>
-static bool launch(void (*kernel)(A), long long grid, unsigned block, hipStream_t st, const A &args)
-{
-    if (grid <= 0 || grid * block > MOST_THREADS) return false;
-    A copy = args;
-    void *argv[] = {&copy};
-    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)grid), dim3(block), argv, 0, st) == hipSuccess;
-}
-
-template <typename F>
-static bool by_dtype(int d, F f)
-{
-    if (d == SVIP_F32) return f(std::integral_constant<int, SVIP_F32>{});
-    if (d == SVIP_BF16) return f(std::integral_constant<int, SVIP_BF16>{});
-    return f(std::integral_constant<int, SVIP_F16>{});
 }
 
 // ---- shapes of the tiles -------------------------------------------------------------------------------------------------------------------
@@ -254,20 +225,11 @@ static HeadPlan plan(int call, int dtype, int N, int V, int D)
     return p;
 }
 
-static svip_status check_sizes(int N, int V, int D)
-{
-    return N <= 0 || N > HEAD_MAX_ROWS || V <= 0 || V > HEAD_MAX_VOCAB || D <= 0 || D > HEAD_MAX_WIDTH ? SVIP_ERR_SHAPE : SVIP_OK;
-}
 // The join of the hidden states' gradient, four values of a row a thread, has more threads than other launches whose size is N x D.
 static svip_status check_grad_sizes(int N, int D)
 {
     return (long long)ceil_div(N, JOIN_SLICES) * ceil_div(D, 4 * JOIN_COLUMNS) * (JOIN_COLUMNS * JOIN_SLICES) > MOST_THREADS ? SVIP_ERR_SHAPE : SVIP_OK;
 }
-static svip_status check_workspace(const void *ws, size_t bytes, size_t need)
-{
-    return !ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || bytes < need ? SVIP_ERR_WORKSPACE : SVIP_OK;
-}
-
 // ---- loss and gradient -----------------------------------------------------------------------------------------------------------------------------
 
 struct LossCall {
@@ -521,7 +483,8 @@ using namespace svip;
 
 size_t svip_head_workspace_bytes(int call, int dtype, int N, int V, int D)
 {
-    if (call < SVIP_HEAD_LOGITS || call > SVIP_HEAD_LOSS_GRAD || !dtype_ok(dtype) || check_sizes(N, V, D)) return 0;
+    if (call < SVIP_HEAD_LOGITS || call > SVIP_HEAD_LOGITS_MX || !dtype_ok(dtype) || check_sizes(N, V, D)) return 0;
+    if (call == SVIP_HEAD_LOGITS_MX) return D % QBLOCK == 0 ? mx_logits_workspace(N, V, D) : 0;
     if (call == SVIP_HEAD_LOSS_GRAD && check_grad_sizes(N, D)) return 0;
     return plan(call, dtype, N, V, D).bytes;
 }

@@ -1,0 +1,45 @@
+// svip_sample: entry point and workspace (kernels: sample_kernels.h).
+#include "sample_kernels.h"
+
+#include "host_calls.h"
+
+namespace svip {
+
+constexpr int SAMPLE_MAX_ROWS = 1 << 20, SAMPLE_MAX_VOCAB = 1 << 22;
+
+static svip_status check_sample_sizes(int N, int V)
+{
+    return N <= 0 || N > SAMPLE_MAX_ROWS || V <= 0 || V > SAMPLE_MAX_VOCAB ? SVIP_ERR_SHAPE : SVIP_OK;
+}
+
+}  // namespace svip
+
+using namespace svip;
+
+size_t svip_sample_workspace_bytes(int dtype, int N, int V)
+{
+    if (!dtype_ok(dtype) || check_sample_sizes(N, V)) return 0;
+    return 512;
+}
+
+svip_status svip_sample(const void *logits, int dtype, int N, int V, long long row_stride, const float *temperature, const int *top_k,
+                        const float *top_p, const float *min_p, const float *u, int *token_out, float *prob_out, int *kept_out, void *workspace,
+                        size_t workspace_bytes, void *hip_stream)
+{
+    if (!logits || !u || !token_out) return SVIP_ERR_NULL;
+    if (!dtype_ok(dtype)) return SVIP_ERR_DTYPE;
+    if (svip_status s = check_sample_sizes(N, V)) return s;
+    if (row_stride < V) return SVIP_ERR_SHAPE;
+    if (!aligned16(logits) || row_stride * size_of(dtype) % 16 != 0) return SVIP_ERR_ALIGN;
+    if (svip_status s = check_workspace(workspace, workspace_bytes, svip_sample_workspace_bytes(dtype, N, V))) return s;
+    SampleArgs a = {logits, row_stride, V, temperature, top_k, top_p, min_p, u, token_out, prob_out, kept_out, static_cast<unsigned *>(workspace), 0};
+    int log2_v = 0;
+    while ((1 << log2_v) < V) ++log2_v;
+    a.unit_bits = 62 - log2_v < 51 ? 62 - log2_v : 51;
+    const bool ok = by_dtype(dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        using X = std::conditional_t<DT == SVIP_F32, float, std::conditional_t<DT == SVIP_BF16, bf16, f16>>;
+        return launch(k_sample_rows<X>, N, SAMPLE_WG, static_cast<hipStream_t>(hip_stream), a);
+    });
+    return ok ? SVIP_OK : SVIP_ERR_HIP;
+}
