@@ -554,8 +554,9 @@ svip_status svip_head_logits_mx(
  * give bit-identical outputs.
  *
  * logits: as everywhere, row n at element offset n * row_stride.  temperature, top_k, top_p, min_p: device [N], each or NULL (1, off, off, off).
- * 1 <= N <= 2^20, 1 <= V <= 2^22.  workspace: svip_sample_workspace_bytes of the call's sizes or more, 256-byte aligned, that svip_workspace_reset has
- * cleared once; not the one of the calls above; calls that run concurrently must use different ones.
+ * 1 <= N <= 2^20, 1 <= V <= 2^22, N * ceil(V / 16384) < 2^24.  workspace: svip_sample_workspace_bytes of the call's sizes or more, 256-byte aligned, that
+ * svip_workspace_reset has cleared once (for its flag word).  As with the head's calls it is not the one of the calls above, it holds nothing between
+ * calls, one for calls of several sizes has the most bytes that one of them needs, and calls that run concurrently must use different ones.
  */
 size_t svip_sample_workspace_bytes(int dtype, int N, int V);          /* pure host function; 0 on bad arguments */
 svip_status svip_sample(

@@ -7,11 +7,12 @@ namespace svip {
 
 constexpr int SAMPLE_MAX_ROWS = 1 << 20, SAMPLE_MAX_VOCAB = 1 << 22;
 
+static int sample_tiles(int V) { return ceil_div(V, SAMPLE_TILE); }
 static svip_status check_sample_sizes(int N, int V)
 {
-    return N <= 0 || N > SAMPLE_MAX_ROWS || V <= 0 || V > SAMPLE_MAX_VOCAB ? SVIP_ERR_SHAPE : SVIP_OK;
+    if (N <= 0 || N > SAMPLE_MAX_ROWS || V <= 0 || V > SAMPLE_MAX_VOCAB) return SVIP_ERR_SHAPE;
+    return (long long)N * ceil_div(sample_tiles(V), TILES_WAVES) * TILES_WG > MOST_THREADS ? SVIP_ERR_SHAPE : SVIP_OK;
 }
-
 }  // namespace svip
 
 using namespace svip;
@@ -19,7 +20,7 @@ using namespace svip;
 size_t svip_sample_workspace_bytes(int dtype, int N, int V)
 {
     if (!dtype_ok(dtype) || check_sample_sizes(N, V)) return 0;
-    return 512;
+    return 512 + up256((size_t)N * sample_tiles(V) * sizeof(TileData));          // flag word, tiles
 }
 
 svip_status svip_sample(const void *logits, int dtype, int N, int V, long long row_stride, const float *temperature, const int *top_k,
@@ -32,14 +33,18 @@ svip_status svip_sample(const void *logits, int dtype, int N, int V, long long r
     if (row_stride < V) return SVIP_ERR_SHAPE;
     if (!aligned16(logits) || row_stride * size_of(dtype) % 16 != 0) return SVIP_ERR_ALIGN;
     if (svip_status s = check_workspace(workspace, workspace_bytes, svip_sample_workspace_bytes(dtype, N, V))) return s;
-    SampleArgs a = {logits, row_stride, V, temperature, top_k, top_p, min_p, u, token_out, prob_out, kept_out, static_cast<unsigned *>(workspace), 0};
+    SampleArgs a = {logits, row_stride, V, temperature, top_k, top_p, min_p, u, token_out, prob_out, kept_out, static_cast<unsigned *>(workspace)};
     int log2_v = 0;
     while ((1 << log2_v) < V) ++log2_v;
     a.unit_bits = 62 - log2_v < 51 ? 62 - log2_v : 51;
+    a.tiles = sample_tiles(V);
+    a.groups = ceil_div(a.tiles, TILES_WAVES);
+    a.tile_data = static_cast<char *>(workspace) + 512;
     const bool ok = by_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         using X = std::conditional_t<DT == SVIP_F32, float, std::conditional_t<DT == SVIP_BF16, bf16, f16>>;
-        return launch(k_sample_rows<X>, N, SAMPLE_WG, static_cast<hipStream_t>(hip_stream), a);
+        const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+        return launch(k_sample_tiles<X>, (long long)N * a.groups, TILES_WG, st, a) && launch(k_sample_rows<X>, N, SAMPLE_WG, st, a);
     });
     return ok ? SVIP_OK : SVIP_ERR_HIP;
 }
