@@ -6,15 +6,15 @@
 // 17 instructions against 7.  Sums that decide are integers in units of 2^-S of the largest weight (S = 62 - ceil(log2 V)), so that no
 // order of additions changes a result and atomics may be used.
 //
-// Two launches.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, a lane a chunk of 64 of them.  k_sample_rows, a workgroup
-// each row, does what the row's settings need beside that.  What a wave leaves for the row:
+// Two launches, three where a call has top_p or min_p.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, a lane a chunk of 64
+// of them.  k_sample_rows, a workgroup each row, does what the row's settings need beside that.  What a wave leaves for the row:
 //   T = 0         the tile's maximum
 //   no filter     and its mass; the draw finds the tile by the masses and goes through that tile alone again
 //   top-k         and the maximum of every chunk.  The k-th largest of those is no larger than the k-th largest logit, so chunks below it hold no
 //                 candidate: the others are read again, what is at or above it goes into a list in LDS, and all settings are decided on the list
 //   top-p, min-p  and the mass of the tile's logits from the top down to each of 512 steps of 1/16 in log2 w.  From the tiles' masses follows the step
-//                 that holds the border, exactly; a sweep over the row without exponentials fetches that step's logits into the list, which decides
-//                 what of it stays; the draw goes by the tiles' masses and through one tile.
+//                 that holds the border, exactly; k_sample_border reads such rows again, without exponentials, counts what lies above that step and
+//                 marks what lies in it, tile by tile; a list of those decides what of them stays, and the draw goes by the tiles' masses and through one tile.
 // Rows that do not fit these (a top_k of more than 1024, a list that runs over, +inf, a border below 2^-31 of the largest weight) are swept as
 // often as a radix select over their keys needs (row_by_sweeps).
 #pragma once
@@ -37,7 +37,8 @@ struct SampleArgs {
     unsigned *flags;
     int unit_bits;             // S
     int tiles, groups;         // of a row; groups: workgroups of k_sample_tiles
-    char *tile_data;           // [N][tiles] TileData
+    int border_groups;         // of k_sample_border
+    char *data;                // [N] RowData, [tiles] TileData
 };
 
 constexpr int TILES_WG = 256, TILES_WAVES = TILES_WG / 64;             // k_sample_tiles
@@ -45,9 +46,10 @@ constexpr int SAMPLE_WG = 512, SAMPLE_WAVES = SAMPLE_WG / 64;          // k_samp
 constexpr int SAMPLE_CHUNK = 64, SAMPLE_TILE = 64 * SAMPLE_CHUNK;       // logits of a lane and of a wave
 constexpr int SAMPLE_STEPS = 512;                      // of log2 w, a 16th each
 constexpr float STEPS_PER_OCTAVE = 16.f;
-constexpr int TILE_UNIT_BITS = 50;                     // masses of a tile, relative to its own largest weight: 2^12 of them fit 64 bits
+constexpr int TILE_UNIT_BITS = 50;                     // masses of a tile, relative to its own R: 2^12 weights of up to 2^1/2 fit 64 bits
 constexpr int SAMPLE_BINS = 1024;
 constexpr int SAMPLE_LIST = 4096;
+constexpr int SMALL_LIST = 128;
 constexpr int SAMPLE_TOP_K = 1024;
 constexpr int SAMPLE_MAX_TILES = (1 << 22) / SAMPLE_TILE;
 
@@ -55,41 +57,44 @@ constexpr int SAMPLE_MAX_TILES = (1 << 22) / SAMPLE_TILE;
 struct TileData {
     float top;                             // the largest logit
     int count;                             // logits above -inf
-    double mass;                           // relative to it
+    double mass;                           // relative to 2^R of its own
     unsigned long long down_to[SAMPLE_STEPS];      // mass from the top down to the end of each step
     float chunk_top[64];
+    unsigned long long above;              // k_sample_border: mass above the row's border step, in the row's units
+    int kept, undecided;                   // logits above it and in it
+    unsigned long long in_step[64];        // which those are: value e of a lane's vector u is that lane's bit of word u N + e
 };
+// Of a row, in front of its tiles: what k_sample_border found, and k_sample_rows goes by.
+struct RowData {
+    int found;                             // 0: for the sweeps
+    int by_mass;                           // top_p's border is in the step (or min_p alone decides)
+    float upper, lower;                    // logits from upper on are above the step, from lower on in it (and not below min_p)
+    unsigned long long target;             // top_p: the mass that what stays has to reach
+    unsigned long long pad[5];
+};
+__host__ __device__ inline size_t row_bytes(int tiles) { return sizeof(RowData) + (size_t)tiles * sizeof(TileData); }
+__device__ __forceinline__ RowData *row_data(char *data, int n, int tiles) { return reinterpret_cast<RowData *>(data + n * row_bytes(tiles)); }
+__device__ __forceinline__ TileData *tiles_of(RowData *row) { return reinterpret_cast<TileData *>(row + 1); }
 
-// 2^x for x <= 0; below 2^-1000, and for NaN, 2^-1000 (which is nothing in any unit here).  2^n times the series of 2^f = exp(f ln 2), |f| <= 1/2: what it
-// leaves out is below 2.3e-13 of the result.  The coefficients are kept in scalar registers: as constants each of them would be moved into
-// a vector register pair for every weight, two more instructions to each of ten.
+// 2^f for |f| <= 1/2, by the Chebyshev series of exp(f ln 2) up to f^9: off by at most 1.9e-14 of the result.  The coefficients are kept in scalar
+// registers: as constants each of them would be moved into a vector register pair for every weight, two more instructions to each of ten.
+constexpr double ROUND_64 = 6755399441055744.0;        // 1.5 * 2^52: added to a number below 2^51 it leaves it, rounded to a whole one, in the low bits
 struct Exp2Series {
-    double c[11];
+    double c[10];
     __device__ __forceinline__ Exp2Series()
-        : c{1.0,
-            6.9314718055994531e-1,
-            2.4022650695910072e-1,
-            5.5504108664821580e-2,
-            9.6181291076284772e-3,
-            1.3333558146428443e-3,
-            1.5403530393381610e-4,
-            1.5252733804059841e-5,
-            1.3215486790144309e-6,
-            1.0178086009239699e-7,
-            7.0549116208011234e-9}
+        : c{1.0000000000000135, 0.69314718055995, 0.240226506956403, 0.05550410866444782, 0.009618129193942278, 0.0013333558230151053, 0.0001540343374614693,
+            1.5252657267483816e-05, 1.3259646267083092e-06, 1.0208689005253291e-07}
     {
 #pragma unroll
-        for (int i = 1; i < 11; ++i) asm("" : "+s"(c[i]));
+        for (int i = 0; i < 10; ++i) asm("" : "+s"(c[i]));
     }
-    __device__ __forceinline__ double operator()(double x) const
+    // 2^(n + f - from), n in the low bits of `rounded`, n - from >= -1000
+    __device__ __forceinline__ double operator()(double rounded, double f, int from) const
     {
-        x = fmax(x, -1000.0);
-        const double t = x + 6755399441055744.0;       // 1.5 * 2^52: x rounded to a whole number in the low bits
-        const double f = x - (t - 6755399441055744.0);
-        double r = c[10];
+        double r = c[9];
 #pragma unroll
-        for (int i = 9; i >= 0; --i) r = fma(r, f, c[i]);
-        return __hiloint2double(__double2hiint(r) + (__double2loint(t) << 20), __double2loint(r));
+        for (int i = 8; i >= 0; --i) r = fma(r, f, c[i]);
+        return __hiloint2double(__double2hiint(r) + ((__double2loint(rounded) - from) << 20), __double2loint(r));
     }
 };
 // 2^(52 - bits): added to a weight of at most 1 it leaves the weight in units of 2^-bits, rounded, in the low bits of the sum
@@ -99,16 +104,44 @@ __device__ __forceinline__ unsigned long long units_of(double w, double unit)
     return (unsigned long long)__double_as_longlong(w + unit) - (unsigned long long)__double_as_longlong(unit);
 }
 
+// Weights relative to 2^R, R = m c rounded to a whole number: that of the largest logit is between 2^-1/2 and 2^1/2, and weights relative to different
+// R differ by a power of two.
 struct SampleWeights {
     double m, c;               // the largest logit; log2(e) / T
+    double least;              // the logit whose weight is 2^-1000; smaller ones, and NaN, are taken for it (which is nothing in any unit here)
+    double part;               // m c - R
     double unit;
+    int R;
+    bool near;                 // |m c| < 2^30: of_tile may be used
     Exp2Series exp2;
-    __device__ __forceinline__ SampleWeights(float top, double c_, int unit_bits) : m(top), c(c_), unit(unit_of(unit_bits)) {}
+    __device__ __forceinline__ SampleWeights(float top, double c_, int unit_bits) : m(top), c(c_), unit(unit_of(unit_bits))
+    {
+        const double mc = m * c;
+        near = fabs(mc) < 1073741824.0;
+        R = near ? (int)rint(mc) : 0;
+        part = near ? fma(m, c, -(double)R) : 0.0;
+        least = ((double)R - 1000.0) / c;
+    }
     __device__ __forceinline__ double log2_of(float z) const { return (double)z == m ? 0.0 : ((double)z - m) * c; }      // (m may be +inf)
-    __device__ __forceinline__ double operator()(float z) const { return exp2(log2_of(z)); }
-    __device__ __forceinline__ double of_tile(float z) const { return exp2(((double)z - m) * c); }       // (what a +inf makes of a tile, nobody looks at)
+    // 2^(z c - R).  Whatever m and c are; of_tile: in two instructions less, where m c is near
+    __device__ __forceinline__ double operator()(float z) const
+    {
+        const double x = fmax(log2_of(z) + part, -1000.0), t = x + ROUND_64;
+        return exp2(t, x - (t - ROUND_64), 0);
+    }
+    __device__ __forceinline__ double of_tile(float z) const
+    {
+        const double x = fmax((double)z, least), t = fma(x, c, ROUND_64);
+        return exp2(t, fma(x, c, -(t - ROUND_64)), R);
+    }
     __device__ __forceinline__ unsigned long long units(float z) const { return units_of((*this)(z), unit); }
 };
+// What a tile's mass is to be multiplied by, as a power of two, in the row's units (a tile that is too far below the row's R weighs nothing).
+__device__ __forceinline__ double in_row(double mass, float tile_top, const SampleWeights &row, int bits)
+{
+    const double R = rint((double)tile_top * row.c);
+    return R >= (double)row.R - 1000.0 ? ldexp(mass, bits + (int)(R - (double)row.R)) : 0.0;
+}
 
 // What a row asks for.
 enum SampleMode { SAMPLE_BAD, SAMPLE_GREEDY, SAMPLE_PLAIN, SAMPLE_TOPK, SAMPLE_STEPPED, SAMPLE_SWEPT };
@@ -145,12 +178,12 @@ struct SampleLds {
     unsigned key[SAMPLE_LIST], index[SAMPLE_LIST];
     unsigned long long tile_mass[SAMPLE_MAX_TILES];
     float tile_top[SAMPLE_MAX_TILES];
-    unsigned long long wave_tot[SAMPLE_WAVES];
+    unsigned long long wave_tot[SAMPLE_WAVES], wave_sum[3][SAMPLE_WAVES];
     float best[SAMPLE_WAVES];
-    unsigned long long found_before, total;
+    unsigned long long found_before, total;          // (total: of draw_by_tiles)
     int found;
     unsigned count, n_list;
-    unsigned low, high;
+    unsigned low;
     int last;
 };
 
@@ -179,37 +212,45 @@ __device__ __forceinline__ void sample_sweep(const DT *row, int V, F f)
     }
 }
 
-template <typename T>
-__device__ __forceinline__ T sum_of_all(T v, SampleLds &L)        // ends behind a barrier
+// The sum over all threads.  Sums one after the other go through different slots, so that one barrier each does: by the time a slot is written again
+// everybody has been through the barrier of another sum.
+template <int SLOT>
+__device__ __forceinline__ unsigned long long sum_of_all(unsigned long long v, SampleLds &L)
 {
     v = wave_reduce(v, OpSum{});
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) L.wave_tot[threadIdx.x >> 6] = (unsigned long long)v;
+    if ((threadIdx.x & 63) == 0) L.wave_sum[SLOT][threadIdx.x >> 6] = v;
     __syncthreads();
     unsigned long long t = 0ull;
 #pragma unroll
-    for (int w = 0; w < SAMPLE_WAVES; ++w) t += L.wave_tot[w];
-    __syncthreads();
-    return (T)t;
+    for (int w = 0; w < SAMPLE_WAVES; ++w) t += L.wave_sum[SLOT][w];
+    return t;
 }
 
-// Of hist[0 .. SAMPLE_BINS), in ascending order if UP and descending if not, the first bin at which the running sum reaches `target` (>= 1), and the sum
-// before it; -1 if the total falls short.  All threads; L.hist is complete behind a barrier; ends behind one, and so may a next call begin.
-template <bool UP>
-__device__ __forceinline__ int find_bin(SampleLds &L, unsigned long long target, unsigned long long *before)
+// Of hist[0 .. SAMPLE_BINS), in ascending order if UP and descending if not, the first bin at which the running sum reaches target_of(total) (>= 1), and the sum
+// before it; -1 if the total falls short.  All threads, behind a barrier that completes the histogram; ends behind one and leaves the bins at zero, as the
+// next histogram finds them.
+template <bool UP, typename T>
+__device__ __forceinline__ int find_bin(SampleLds &L, T target_of, unsigned long long *before, unsigned long long *total)
 {
     constexpr int PER = SAMPLE_BINS / SAMPLE_WG;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     unsigned long long h[PER], sum = 0ull;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += h[i] = L.hist[UP ? tid * PER + i : SAMPLE_BINS - 1 - (tid * PER + i)];
+    for (int i = 0; i < PER; ++i) {
+        unsigned long long &bin = L.hist[UP ? tid * PER + i : SAMPLE_BINS - 1 - (tid * PER + i)];
+        sum += h[i] = bin;
+        bin = 0ull;
+    }
     const unsigned long long incl = wave_inclusive_sum_u64(sum);
     if (lane == 63) L.wave_tot[wave] = incl;
-    if (tid == 0) L.found = -1;
     __syncthreads();
-    unsigned long long ahead = 0ull;
-    for (int w = 0; w < wave; ++w) ahead += L.wave_tot[w];
-    unsigned long long run = ahead + incl - sum;
+    unsigned long long run = incl - sum, all = 0ull;
+#pragma unroll
+    for (int w = 0; w < SAMPLE_WAVES; ++w) {
+        if (w < wave) run += L.wave_tot[w];
+        all += L.wave_tot[w];
+    }
+    const unsigned long long target = target_of(all);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         if (run < target && run + h[i] >= target) {
@@ -218,19 +259,10 @@ __device__ __forceinline__ int find_bin(SampleLds &L, unsigned long long target,
         }
         run += h[i];
     }
-    if (tid == SAMPLE_WG - 1) L.total = run;
     __syncthreads();
     *before = L.found_before;
-    const int found = L.found;
-    __syncthreads();
-    return found;
-}
-__device__ __forceinline__ void clear_hist(SampleLds &L)
-{
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < SAMPLE_BINS / SAMPLE_WG; ++i) L.hist[threadIdx.x + i * SAMPLE_WG] = 0ull;
-    __syncthreads();
+    *total = all;
+    return all < target ? -1 : L.found;
 }
 
 // The largest key v with measure(keys >= v) >= target, among those between lo and hi that each(f) calls f(key, value) for; lo if all of them fall short.
@@ -242,13 +274,13 @@ __device__ __forceinline__ unsigned select_key(Each each, unsigned lo, unsigned 
     *above = 0ull;
     while ((hi - lo) >> LOW) {
         const int shift = max(0, 22 - __clz((int)(hi - lo)));         // (hi - lo) >> shift < 1024
-        clear_hist(L);
         each([&](unsigned key, float z) {
             if (key >= lo && key <= hi) atomicAdd(&L.hist[(key - lo) >> shift], measure(z));
         });
         __syncthreads();
-        unsigned long long before;
-        const int bin = find_bin<false>(L, target - *above, &before);
+        unsigned long long before, total;
+        const unsigned long long left = target - *above;
+        const int bin = find_bin<false>(L, [&](unsigned long long) { return left; }, &before, &total);
         if (bin < 0) return lo;
         *above += before;
         hi = lo + min(hi - lo, (((unsigned)bin + 1u) << shift) - 1u);
@@ -294,7 +326,6 @@ __device__ __forceinline__ void draw_in_range(const SampleArgs &a, int n, const 
         }
     }
     const unsigned long long incl = wave_inclusive_sum_u64(mass);
-    __syncthreads();
     if (lane == 63) L.wave_tot[wave] = incl;
     if (tid == 0) L.last = -1;
     __syncthreads();
@@ -347,13 +378,12 @@ __device__ __forceinline__ void row_by_sweeps(const SampleArgs &a, int n, const 
     if (s.top_p < 1.0) {
         unsigned long long mass = 0ull;
         each([&](unsigned key, float z) { mass += key >= low ? mass_of(z) : 0ull; });
-        mass = sum_of_all(mass, L);
+        mass = sum_of_all<0>(mass, L);
         low = select_key<KEY_LOW<DT>>(each, low, high, max(1ull, (unsigned long long)ceil(s.top_p * (double)mass)), L, mass_of, &above);
     }
     const Keep keep = {low, s.log2_min_p, w};
     // masses of runs of vectors, in index order
     const int nvec = (V + N - 1) / N, chunks = (nvec + 63) / 64, per = (chunks + SAMPLE_BINS - 1) / SAMPLE_BINS;
-    clear_hist(L);
     unsigned kept = 0u;
     for (int c = wave; c < chunks; c += SAMPLE_WAVES) {
         const int v = c * 64 + lane;
@@ -368,13 +398,11 @@ __device__ __forceinline__ void row_by_sweeps(const SampleArgs &a, int n, const 
         mass = wave_reduce(mass, OpSum{});
         if (lane == 0) atomicAdd(&L.hist[c / per], mass);
     }
-    kept = (unsigned)sum_of_all((unsigned long long)kept, L);
-    unsigned long long before;
-    find_bin<true>(L, ~0ull, &before);
-    const unsigned long long total = L.total, at = (unsigned long long)(s.u * (double)total);
-    __syncthreads();
-    const int bin = find_bin<true>(L, at + 1ull, &before);
-    draw_in_range<DT>(a, n, row, bin * per * 64, min(nvec, (bin + 1) * per * 64), keep, at - before, total, (int)kept, L);
+    kept = (unsigned)sum_of_all<1>(kept, L);           // (and the barrier behind the histogram)
+    unsigned long long before, total;
+    const auto at = [&](unsigned long long all) { return (unsigned long long)(s.u * (double)all); };
+    const int bin = find_bin<true>(L, [&](unsigned long long all) { return at(all) + 1ull; }, &before, &total);
+    draw_in_range<DT>(a, n, row, bin * per * 64, min(nvec, (bin + 1) * per * 64), keep, at(total) - before, total, (int)kept, L);
 }
 
 // Appends to the list those of a vector's logits that pass; L.n_list counts them all, also those that have no place.
@@ -397,11 +425,52 @@ __device__ __forceinline__ void append(SampleLds &L, const float (&z)[N], int in
         }
 }
 
+// The same for a list that has four threads for each candidate: every candidate against every other, in place of selects.
+__device__ __forceinline__ void row_by_small_list(const SampleArgs &a, int n, const Settings &s, const SampleWeights &w, SampleLds &L)
+{
+    static_assert(SAMPLE_WG == 4 * SMALL_LIST && SMALL_LIST <= SAMPLE_BINS, "");
+    const int len = (int)L.n_list, i = threadIdx.x >> 2, part = threadIdx.x & 3;
+    if (threadIdx.x < SMALL_LIST) L.hist[threadIdx.x] = (int)threadIdx.x < len ? w.units(key_value(L.key[threadIdx.x])) : 0ull;
+    __syncthreads();
+    const bool mine = i < len;
+    const unsigned key = mine ? L.key[i] : 0u, index = mine ? L.index[i] : 0u;
+    const unsigned long long units = L.hist[i];
+    int over = 0;
+    unsigned long long above = 0ull;
+    const auto over_four = [](auto v) {
+        v += dpp_mov<DPP_QUAD_XOR1>(v);
+        return v + dpp_mov<DPP_QUAD_XOR2>(v);
+    };
+    if (mine)
+        for (int j = part; j < len; j += 4)
+            if (L.key[j] > key) ++over, above += L.hist[j];
+    over = over_four(over);
+    above = over_four(above);
+    bool keep = mine && over < s.top_k;
+    if (s.top_p < 1.0) {
+        const unsigned long long mass = sum_of_all<0>(keep && part == 0 ? units : 0ull, L);
+        keep = keep && above < max(1ull, (unsigned long long)ceil(s.top_p * (double)mass));
+    }
+    keep = keep && w.log2_of(key_value(key)) >= s.log2_min_p;
+    const unsigned long long total = sum_of_all<1>(keep && part == 0 ? units : 0ull, L), count = sum_of_all<2>(keep && part == 0 ? 1ull : 0ull, L);
+    if (part == 0 && !keep) L.hist[i] = 0ull;
+    __syncthreads();
+    const unsigned long long at = (unsigned long long)(s.u * (double)total);
+    unsigned long long before = 0ull;
+    if (keep)
+        for (int j = part; j < len; j += 4)
+            if (L.index[j] < index) before += L.hist[j];
+    before = over_four(before);
+    if (keep && part == 0 && before <= at && before + units > at)
+        sample_answer(a, n, (int)index, (float)(w(key_value(key)) / ldexp((double)total, -a.unit_bits)), (int)count);
+}
+
 // All settings decided on the list of candidates, which holds every logit from the top_k-th largest on.
 template <typename DT>
 __device__ __forceinline__ void row_by_list(const SampleArgs &a, int n, const DT *row, const Settings &s, const SampleWeights &w, unsigned lo, SampleLds &L)
 {
     const unsigned len = L.n_list, high = value_key((float)w.m);
+    if (len <= SMALL_LIST) return row_by_small_list(a, n, s, w, L);
     const auto each = [&](auto f) {
         for (unsigned i = threadIdx.x; i < len; i += SAMPLE_WG) f(L.key[i], key_value(L.key[i]));
     };
@@ -411,7 +480,7 @@ __device__ __forceinline__ void row_by_list(const SampleArgs &a, int n, const DT
     if (s.top_p < 1.0) {
         unsigned long long mass = 0ull;
         each([&](unsigned key, float z) { mass += key >= low ? mass_of(z) : 0ull; });
-        mass = sum_of_all(mass, L);
+        mass = sum_of_all<0>(mass, L);
         low = select_key<KEY_LOW<DT>>(each, low, high, max(1ull, (unsigned long long)ceil(s.top_p * (double)mass)), L, mass_of, &above);
     }
     const Keep keep = {low, s.log2_min_p, w};
@@ -419,8 +488,8 @@ __device__ __forceinline__ void row_by_list(const SampleArgs &a, int n, const DT
     each([&](unsigned, float z) {
         if (keep(z)) mass += mass_of(z), ++count;
     });
-    mass = sum_of_all(mass, L);
-    count = sum_of_all(count, L);
+    mass = sum_of_all<1>(mass, L);
+    count = sum_of_all<2>(count, L);
     const unsigned long long at = (unsigned long long)(s.u * (double)mass);
     // by index, upwards: keys are their complements
     const auto by_index = [&](auto f) {
@@ -443,34 +512,45 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
     constexpr int N = VecOf<DT>::N, U = SAMPLE_CHUNK / N;
     const int tid = threadIdx.x, chunks = a.tiles * 64;
     const unsigned high = value_key(top), none = value_key(neg_inf());
-    const auto each = [&](auto f) {        // two chunks at a time
-        for (int i = tid; i < chunks / 2; i += SAMPLE_WG) {
-            const unsigned long long two = reinterpret_cast<const unsigned long long *>(tiles[i / 32].chunk_top)[i % 32];
-            f(2 * i, value_key(__uint_as_float((unsigned)two)));
-            f(2 * i + 1, value_key(__uint_as_float((unsigned)(two >> 32))));
+    constexpr int HELD = 4;                // pairs of chunks that a thread keeps; those of more than 4096 chunks are read each time
+    const auto pair = [&](int i) { return reinterpret_cast<const float2 *>(tiles[i / 32].chunk_top)[i % 32]; };
+    float2 held[HELD];
+#pragma unroll
+    for (int q = 0; q < HELD; ++q) held[q] = tid + q * SAMPLE_WG < chunks / 2 ? pair(tid + q * SAMPLE_WG) : make_float2(neg_inf(), neg_inf());
+    const auto each = [&](auto f) {
+#pragma unroll
+        for (int q = 0; q < HELD; ++q) {
+            f(2 * (tid + q * SAMPLE_WG), held[q].x);
+            f(2 * (tid + q * SAMPLE_WG) + 1, held[q].y);
+        }
+        for (int i = tid + HELD * SAMPLE_WG; i < chunks / 2; i += SAMPLE_WG) {
+            const float2 two = pair(i);
+            f(2 * i, two.x);
+            f(2 * i + 1, two.y);
         }
     };
     // the least of the maxima, and a thousandth of the span from the largest at a time
-    unsigned least = high;
-    each([&](int, unsigned key) { least = key > none ? min(least, key) : least; });
+    float lowest_top = INFINITY;
+    each([&](int, float z) { lowest_top = z > neg_inf() ? fminf(lowest_top, z) : lowest_top; });
+    lowest_top = -wave_max(-lowest_top);
     if (tid == 0) L.low = high, L.n_list = 0u, L.count = 0u;
-    clear_hist(L);
-    atomicMin(&L.low, least);
     __syncthreads();
-    least = L.low;
+    if ((tid & 63) == 0 && lowest_top < INFINITY) atomicMin(&L.low, value_key(lowest_top));
+    __syncthreads();
+    const unsigned least = L.low;
     const int shift = high == least ? 0 : max(0, 22 - __clz((int)(high - least)));
-    each([&](int, unsigned key) {
-        if (key > none) atomicAdd(&L.hist[(key - least) >> shift], 1ull);
+    each([&](int, float z) {
+        if (z > neg_inf()) atomicAdd(&L.hist[(value_key(z) - least) >> shift], 1ull);
     });
     __syncthreads();
-    unsigned long long before;
-    const int bin = find_bin<false>(L, (unsigned long long)top_k, &before);
+    unsigned long long before, total;
+    const int bin = find_bin<false>(L, [&](unsigned long long) { return (unsigned long long)top_k; }, &before, &total);
     const unsigned pivot = bin < 0 ? none + 1u : least + ((unsigned)bin << shift);
-    // the chunks that reach the pivot, then their logits (the chunks' numbers where the histogram was)
-    unsigned short *const reach = reinterpret_cast<unsigned short *>(L.hist);
-    constexpr unsigned MOST = sizeof(L.hist) / 2;
-    each([&](int chunk, unsigned key) {
-        if (key >= pivot && key > none) {
+    // the chunks that reach the pivot, then their logits (the chunks' numbers where other settings have the tiles' masses)
+    unsigned short *const reach = reinterpret_cast<unsigned short *>(L.tile_mass);
+    constexpr unsigned MOST = sizeof(L.tile_mass) / 2;
+    each([&](int chunk, float z) {
+        if (z > neg_inf() && value_key(z) >= pivot) {
             const unsigned slot = lds_add(&L.count, 1u);
             if (slot < MOST) reach[slot] = (unsigned short)chunk;
         }
@@ -478,14 +558,27 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
     __syncthreads();
     if (L.count > MOST || chunks > 65536) return false;
     const int items = (int)L.count * U;
-    for (int i = tid; i < items; i += SAMPLE_WG) {
-        const int chunk = reach[i / U], v = (chunk / 64 * U + i % U) * 64 + chunk % 64;
-        if (v * N >= a.V) continue;
-        float z[N];
-        unpack<DT>(warp_load<DT>(row, v, a.V), z);
+    constexpr int AT_ONCE = 4;
+    for (int i0 = tid; i0 < items; i0 += AT_ONCE * SAMPLE_WG) {
+        typename RawOf<DT>::type raw[AT_ONCE];
+        int at[AT_ONCE];
 #pragma unroll
-        for (int e = 0; e < N; ++e) z[e] = sample_logit(z[e]);
-        append<N>(L, z, v * N, [&](float x) { return x > neg_inf() && value_key(x) >= pivot; });
+        for (int b = 0; b < AT_ONCE; ++b) {
+            const int i = min(i0 + b * SAMPLE_WG, items - 1), chunk = reach[i / U];
+            at[b] = (chunk / 64 * U + i % U) * 64 + chunk % 64;
+            const bool mine = i0 + b * SAMPLE_WG < items && at[b] * N < a.V;
+            raw[b] = warp_load<DT>(row, mine ? at[b] : 0, a.V);
+            if (!mine) at[b] = -1;
+        }
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) {
+            if (at[b] < 0) continue;
+            float z[N];
+            unpack<DT>(raw[b], z);
+#pragma unroll
+            for (int e = 0; e < N; ++e) z[e] = sample_logit(z[e]);
+            append<N>(L, z, at[b] * N, [&](float x) { return x > neg_inf() && value_key(x) >= pivot; });
+        }
     }
     __syncthreads();
     *lowest = pivot;
@@ -549,153 +642,73 @@ __device__ __forceinline__ void draw_by_tiles(const SampleArgs &a, int n, const 
     draw_in_range<DT>(a, n, row, v0, min((a.V + N - 1) / N, v0 + SAMPLE_TILE / N), keep, left, total, kept, L);
 }
 
-// top_p and min_p by the tiles' masses down to each step.  false: for the sweeps.
+// top_p and min_p by what k_sample_border found.
 template <typename DT>
-__device__ __forceinline__ bool row_by_steps(const SampleArgs &a, int n, const DT *row, const Settings &s, const SampleWeights &w, const TileData *tiles, SampleLds &L)
+__device__ __forceinline__ void row_by_steps(const SampleArgs &a, int n, const DT *row, const Settings &s, const SampleWeights &w, const RowData &found,
+                                             const TileData *tiles, SampleLds &L)
 {
     constexpr int N = VecOf<DT>::N;
-    const int tid = threadIdx.x;
-    const float scale = (float)(s.c * (double)STEPS_PER_OCTAVE), first = step_of((float)w.m, scale);
-    if (!(fabsf(first) < 8388608.f)) return false;     // (numbers of steps are whole numbers in fp32)
-    // mass of tile t down to the end of the row's step r (counted from its first, downwards), in the row's units
-    const auto tile_down_to = [&](int t, int r) -> unsigned long long {
-        const float top = L.tile_top[t];
-        if (!(top > neg_inf())) return 0ull;
-        const float i = (float)r - (first - step_of(top, scale));
-        if (!(i >= 0.f)) return 0ull;
-        const unsigned long long mass = tiles[t].down_to[i < (float)SAMPLE_STEPS ? (int)i : SAMPLE_STEPS - 1];
-        return (unsigned long long)rint(ldexp((double)mass, a.unit_bits - TILE_UNIT_BITS) * w(top));
-    };
-    // of the row down to the end of eight steps side by side: the waves have the sum of a step each
-    static_assert(SAMPLE_WAVES == 8, "a step each");
-    const int wave = tid >> 6;
-    const auto row_down_to = [&](int r) {
-        unsigned long long mass = 0ull;
-        for (int t = tid & 63; t < a.tiles; t += 64) mass += tile_down_to(t, r);
-        return wave_reduce(mass, OpSum{});
-    };
-    int lo = SAMPLE_STEPS, hi = SAMPLE_STEPS;          // steps from lo to hi are undecided; above all stays, below nothing
-    unsigned long long target = ~0ull;
-    if (s.top_p < 1.0) {
-        int base = 0, found = -1;
-        unsigned long long mass = row_down_to(64 * wave + 63);
-        if (tid == SAMPLE_WG - 1) L.total = mass;
-        __syncthreads();
-        target = max(1ull, (unsigned long long)ceil(s.top_p * (double)L.total));
-#pragma unroll 1
-        for (int width = 64; ; width /= 8) {           // 64, 8, 1
-            if (tid == 0) L.found = 8;
-            __syncthreads();
-            if (mass >= target) atomicMin(&L.found, wave);
-            __syncthreads();
-            found = L.found;
-            __syncthreads();
-            if (found == 8) return false;
-            base += found * width;
-            if (width == 1) break;
-            mass = row_down_to(base + width / 8 * (wave + 1) - 1);
-        }
-        if (base >= SAMPLE_STEPS - 1) return false;    // (the last step of a tile is all that lies below it too)
-        lo = hi = base;
+    const int tid = threadIdx.x, lane = tid & 63;
+    unsigned long long above = 0ull, kept = 0ull, len = 0ull;
+    for (int t = tid; t < a.tiles; t += SAMPLE_WG) {
+        above += L.tile_mass[t] = tiles[t].above;
+        kept += (unsigned)tiles[t].kept;
+        len += (unsigned)tiles[t].undecided;
     }
-    if (s.log2_min_p > -INFINITY) {
-        const float step = first - step_of((float)(w.m + s.log2_min_p / w.c), scale);
-        if (step < (float)(SAMPLE_STEPS - 2)) {        // one more on either side for the border's own rounding
-            lo = min(lo, max(0, (int)step - 1));
-            hi = min(hi, (int)step + 1);
-        } else if (hi >= SAMPLE_STEPS) {
-            return false;
-        }
-    }
-    // masses above the undecided steps, and their logits
-    unsigned long long above = 0ull;
-    for (int t = tid; t < a.tiles; t += SAMPLE_WG) above += L.tile_mass[t] = tile_down_to(t, lo - 1);
-    above = sum_of_all(above, L);
-    if (tid == 0) L.n_list = 0u, L.low = ~0u, L.high = 0u;
-    __syncthreads();
-    unsigned kept = 0u, least = ~0u, most = 0u;
-    // the least logit of a step not below `step`: those keys are searched 64 at a time
-    const auto least_of = [&](float step) {
-        unsigned at = value_key(neg_inf());
-#pragma unroll 1
-        for (int bits = 26; bits >= -4; bits -= 6) {
-            const unsigned unit = 1u << max(0, bits), key = at + min((unsigned)(tid & 63) * unit, value_key(INFINITY) - at);
-            const unsigned long long reach = __ballot(step_of(key_value(key), scale) >= step);
-            const int before = reach ? max(0, __ffsll((long long)reach) - 2) : 63;      // the last that does not, or the first
-            at += min((unsigned)before * unit, value_key(INFINITY) - at);
-        }
-        return key_value(step_of(key_value(at), scale) >= step ? at : at + 1u);
-    };
-    const float upper = least_of(first - (float)lo + 1.f), lower = least_of(first - (float)hi);       // from upper on above, from lower on undecided
-    sample_sweep(row, a.V, [&](int v, const float(&z)[N]) {
-        unsigned over = 0u, from = 0u;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            over += z[e] >= upper;
-            from += z[e] >= lower;
-        }
-        kept += over;
-        if (from == over) return;
-        unsigned slot = lds_add(&L.n_list, from - over);
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (z[e] >= lower && !(z[e] >= upper)) {
-                const unsigned key = value_key(z[e]);
-                if (slot < SAMPLE_LIST) {
-                    L.key[slot] = key;
-                    L.index[slot] = (unsigned)(v * N + e);
-                }
-                ++slot;
-                least = min(least, key);
-                most = max(most, key);
-            }
-    });
-    atomicMin(&L.low, least);
-    atomicMax(&L.high, most);
-    __syncthreads();
-    unsigned low = L.low;
-    const unsigned high = L.high, len = L.n_list;
-    unsigned long long more;
+    if (tid == 0) L.n_list = 0u;
+    above = sum_of_all<0>(above, L);
+    kept = sum_of_all<1>(kept, L);
+    len = sum_of_all<2>(len, L);
+    const unsigned long long target = found.target;
+    const bool by_mass = found.by_mass && target > above;
     const auto mass_of = [&](float z) { return w.units(z); };
-    const bool by_mass = s.top_p < 1.0 && len && target > above;
+    unsigned low = value_key(found.lower);
+    const unsigned high = value_key(found.upper) - 1u;
+    unsigned long long more, stay = 0ull;
     if (len <= SAMPLE_LIST) {
-        const auto each = [&](auto f) {
-            for (unsigned i = tid; i < len; i += SAMPLE_WG) f(L.key[i], key_value(L.key[i]));
-        };
-        if (by_mass) low = select_key<KEY_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
-        const Keep keep = {len ? low : value_key(neg_inf()) + 1u, s.log2_min_p, w};
-        __syncthreads();
-        for (unsigned i = tid; i < len; i += SAMPLE_WG) {
-            const float z = key_value(L.key[i]);
-            if (!keep(z)) continue;
-            ++kept;
-            atomicAdd(&L.tile_mass[L.index[i] / SAMPLE_TILE], w.units(z));
+        for (int t = tid >> 6; t < a.tiles; t += SAMPLE_WAVES) {
+            unsigned long long word = tiles[t].in_step[lane];
+            const unsigned count = (unsigned)__popcll(word), incl = (unsigned)wave_inclusive_sum_u64(count), all = (unsigned)read_lane((int)incl, 63);
+            unsigned to = lane == 0 && all ? atomicAdd(&L.n_list, all) : 0u;
+            to = (unsigned)__builtin_amdgcn_readfirstlane((int)to) + incl - count;
+            const unsigned first = (unsigned)t * SAMPLE_TILE + lane / N * 64 * N + lane % N;
+            for (; word; word &= word - 1ull) L.index[to++] = first + (unsigned)(__ffsll((long long)word) - 1) * N;
         }
-        kept = (unsigned)sum_of_all((unsigned long long)kept, L);
-        draw_by_tiles<DT>(a, n, row, s, keep, (int)kept, L);
-        return true;
-    }
-    // more than the list holds: from the row again
-    const auto each_index = [&](auto f) {
-        sample_sweep(row, a.V, [&](int v, const float(&z)[N]) {
+        __syncthreads();
+        constexpr int AT_ONCE = SAMPLE_LIST / SAMPLE_WG;
+        float z[AT_ONCE];
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                if (z[e] >= lower && !(z[e] >= upper)) f(v * N + e, z[e]);
-            }
+        for (int i = 0; i < AT_ONCE; ++i) z[i] = tid + i * SAMPLE_WG < (int)len ? widen(row[L.index[tid + i * SAMPLE_WG]]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+            if (tid + i * SAMPLE_WG < (int)len) L.key[tid + i * SAMPLE_WG] = value_key(z[i]);        // (read by this thread alone)
+        const auto each = [&](auto f) {
+            for (unsigned i = tid; i < (unsigned)len; i += SAMPLE_WG) f(L.key[i], key_value(L.key[i]));
+        };
+        if (by_mass && len) low = select_key<KEY_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
+        for (unsigned i = tid; i < (unsigned)len; i += SAMPLE_WG) {
+            if (L.key[i] < low) continue;
+            ++stay;
+            atomicAdd(&L.tile_mass[L.index[i] / SAMPLE_TILE], w.units(key_value(L.key[i])));
+        }
+    } else {                               // more than the lists hold: from the row again
+        const auto each_index = [&](auto f) {
+            sample_sweep(row, a.V, [&](int v, const float(&z)[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (z[e] >= found.lower && !(z[e] >= found.upper)) f(v * N + e, z[e]);
+            });
+        };
+        const auto each = [&](auto f) { each_index([&](int, float z) { f(value_key(z), z); }); };
+        if (by_mass) low = select_key<KEY_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
+        each_index([&](int i, float z) {
+            if (value_key(z) < low) return;
+            ++stay;
+            atomicAdd(&L.tile_mass[i / SAMPLE_TILE], w.units(z));
         });
-    };
-    const auto each = [&](auto f) { each_index([&](int, float z) { f(value_key(z), z); }); };
-    if (by_mass) low = select_key<KEY_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
-    const Keep keep = {low, s.log2_min_p, w};
-    __syncthreads();
-    each_index([&](int i, float z) {
-        if (!keep(z)) return;
-        ++kept;
-        atomicAdd(&L.tile_mass[i / SAMPLE_TILE], w.units(z));
-    });
-    kept = (unsigned)sum_of_all((unsigned long long)kept, L);
-    draw_by_tiles<DT>(a, n, row, s, keep, (int)kept, L);
-    return true;
+    }
+    kept += sum_of_all<0>(stay, L);
+    draw_by_tiles<DT>(a, n, row, s, {low, -INFINITY, w}, (int)kept, L);
 }
 
 template <typename DT>
@@ -708,7 +721,7 @@ __global__ __launch_bounds__(TILES_WG, VecOf<DT>::N == 8 ? 8 : 4) void k_sample_
     const DT *row = static_cast<const DT *>(a.logits) + n * a.row_stride;
     const int tile = group * TILES_WAVES + wave, v0 = tile * (U * 64) + lane;
     if (tile >= a.tiles) return;
-    TileData *const mine = reinterpret_cast<TileData *>(a.tile_data) + (size_t)n * a.tiles + tile;
+    TileData *const mine = tiles_of(row_data(a.data, n, a.tiles)) + tile;
     typename RawOf<DT>::type raw[U];
     if ((tile + 1) * SAMPLE_TILE <= V) {
 #pragma unroll
@@ -777,13 +790,154 @@ __global__ __launch_bounds__(TILES_WG, VecOf<DT>::N == 8 ? 8 : 4) void k_sample_
     for (int i = 0; i < PER; ++i) mine->down_to[lane * PER + i] = run += h[i];
 }
 
+// The least number for which pass(z) holds, a property of all from some number on (of +inf for certain): keys are searched 64 at a time.
+template <typename P>
+__device__ __forceinline__ float least_that(P pass)
+{
+    const unsigned end = value_key(INFINITY);
+    unsigned at = value_key(neg_inf());
+#pragma unroll 1
+    for (int bits = 26; bits >= -4; bits -= 6) {       // the last of 64 that does not pass, or the first
+        const unsigned unit = 1u << max(0, bits), key = at + min((unsigned)(threadIdx.x & 63) * unit, end - at);
+        const unsigned long long reach = __ballot(pass(key_value(key)));
+        at += min((unsigned)(reach ? max(0, __ffsll((long long)reach) - 2) : 63) * unit, end - at);
+    }
+    return key_value(pass(key_value(at)) ? at : at + 1u);
+}
+
+// Rows with top_p or min_p and no top_k: the step that holds the border, by every workgroup of the row for itself, and what its tiles have in it.
+template <typename DT>
+__global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
+{
+    constexpr int N = VecOf<DT>::N, U = SAMPLE_CHUNK / N;
+    __shared__ float tile_top[SAMPLE_MAX_TILES];
+    __shared__ float wave_top[TILES_WAVES];
+    __shared__ unsigned long long all;
+    __shared__ int first_group;
+    const int n = blockIdx.x / (unsigned)a.border_groups, group = blockIdx.x - n * a.border_groups;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = a.V;
+    const Settings s = settings_of(a, n);
+    if (s.mode != SAMPLE_STEPPED) return;
+    const DT *row = static_cast<const DT *>(a.logits) + n * a.row_stride;
+    typename RawOf<DT>::type raw[U];
+    const auto load = [&](int tile) {
+        const int v0 = tile * (U * 64) + lane;
+        if ((tile + 1) * SAMPLE_TILE <= V) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = *(reinterpret_cast<const typename RawOf<DT>::type *>(row) + v0 + u * 64);
+        } else {
+            load_raw_tail<DT, U, 64>(row, v0, V, raw);
+        }
+    };
+    int tile = group * TILES_WAVES + wave;
+    if (tile < a.tiles) load(tile);        // (they arrive while the border is looked for)
+    RowData *const found = row_data(a.data, n, a.tiles);
+    TileData *const tiles = tiles_of(found);
+    float top = neg_inf();
+    for (int t = tid; t < a.tiles; t += TILES_WG) top = vmax(top, tile_top[t] = tiles[t].top);
+    top = wave_max(top);
+    if (lane == 0) wave_top[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TILES_WAVES; ++i) top = vmax(top, wave_top[i]);
+    const SampleWeights w(top, s.c, a.unit_bits);
+    const float scale = (float)(s.c * (double)STEPS_PER_OCTAVE), first = step_of(top, scale);
+    const auto give_up = [&]() {
+        if (group == 0 && tid == 0) found->found = 0;
+    };
+    if (!(top > neg_inf() && fabsf(first) < 8388608.f && w.near)) return give_up();      // (numbers of steps are whole numbers in fp32)
+    // mass of tile t down to the end of the row's step r (counted from its first, downwards), in the row's units
+    const auto tile_down_to = [&](int t, int r) -> unsigned long long {
+        if (!(tile_top[t] > neg_inf())) return 0ull;
+        const float i = (float)r - (first - step_of(tile_top[t], scale));
+        if (!(i >= 0.f)) return 0ull;
+        const unsigned long long mass = tiles[t].down_to[i < (float)SAMPLE_STEPS ? (int)i : SAMPLE_STEPS - 1];
+        return (unsigned long long)rint(in_row((double)mass, tile_top[t], w, a.unit_bits - TILE_UNIT_BITS));
+    };
+    // of the row down to the end of eight steps side by side: threads 32 i .. 32 i + 31 have the sum of r(i)
+    static_assert(TILES_WG == 8 * 32 && SAMPLE_STEPS == 8 * 8 * 8, "a step each, three times");
+    const auto row_down_to = [&](int r) {
+        unsigned long long mass = 0ull;
+        for (int t = tid & 31; t < a.tiles; t += 32) mass += tile_down_to(t, r);
+        mass = row_reduce(mass, OpSum{});
+        const auto lo = __builtin_amdgcn_permlane16_swap((unsigned)mass, (unsigned)mass, false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap((unsigned)(mass >> 32), (unsigned)(mass >> 32), false, false);
+        return ((unsigned long long)hi[0] << 32 | lo[0]) + ((unsigned long long)hi[1] << 32 | lo[1]);
+    };
+    int step = SAMPLE_STEPS;               // above it all stays, below nothing
+    unsigned long long target = 0ull;
+    if (s.top_p < 1.0) {
+        unsigned long long mass = row_down_to(64 * (tid / 32) + 63);
+        if (tid == TILES_WG - 1) all = mass;
+        __syncthreads();
+        target = max(1ull, (unsigned long long)ceil(s.top_p * (double)all));
+        step = 0;
+#pragma unroll 1
+        for (int width = 64;; width /= 8) {
+            if (tid == 0) first_group = 8;
+            __syncthreads();
+            if ((tid & 31) == 0 && mass >= target) atomicMin(&first_group, tid / 32);
+            __syncthreads();
+            step += first_group * width;
+            if (first_group == 8 || width == 1) break;
+            mass = row_down_to(step + width / 8 * (tid / 32 + 1) - 1);
+            __syncthreads();
+        }
+    }
+    float lower = neg_inf();
+    bool by_mass = s.top_p < 1.0;
+    if (s.log2_min_p > -INFINITY) {
+        lower = least_that([&](float z) { return w.log2_of(z) >= s.log2_min_p; });
+        const float its = first - step_of(lower, scale);
+        if (its < (float)step) {
+            step = (int)its;
+            by_mass = false;
+        }
+    }
+    if (step >= SAMPLE_STEPS - 1) return give_up();    // (the last step of a tile is all that lies below it too)
+    const float upper = least_that([&](float z) { return step_of(z, scale) >= first - (float)step + 1.f; });
+    lower = fmaxf(lower, least_that([&](float z) { return step_of(z, scale) >= first - (float)step; }));
+    if (group == 0 && tid == 0) {
+        found->found = 1;
+        found->by_mass = by_mass;
+        found->upper = upper;
+        found->lower = lower;
+        found->target = target;
+    }
+    for (; tile < a.tiles; tile += a.border_groups * TILES_WAVES) {
+        if (tile >= a.border_groups * TILES_WAVES) load(tile);
+        TileData *const mine = tiles + tile;
+        int kept = 0, undecided = 0;
+        unsigned long long word = 0ull;    // (lane u N + e's)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float z[N];
+            unpack<DT>(raw[u], z);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const unsigned long long over = __ballot(z[e] >= upper), in = __ballot(z[e] >= lower) & ~over;
+                kept += __popcll(over);
+                undecided += __popcll(in);
+                word = lane == u * N + e ? in : word;
+            }
+        }
+        mine->in_step[lane] = word;
+        if (lane == 0) {
+            mine->above = tile_down_to(tile, step - 1);
+            mine->kept = kept;
+            mine->undecided = undecided;
+        }
+    }
+}
+
 template <typename DT>
 __global__ __launch_bounds__(SAMPLE_WG) void k_sample_rows(SampleArgs a)
 {
     __shared__ SampleLds L;
     const int n = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const DT *row = static_cast<const DT *>(a.logits) + n * a.row_stride;
-    const TileData *const tiles = reinterpret_cast<const TileData *>(a.tile_data) + (size_t)n * a.tiles;
+    RowData *const found = row_data(a.data, n, a.tiles);
+    const TileData *const tiles = tiles_of(found);
     const Settings s = settings_of(a, n);
     if (s.mode == SAMPLE_BAD) {
         if (tid == 0) {
@@ -801,6 +955,8 @@ __global__ __launch_bounds__(SAMPLE_WG) void k_sample_rows(SampleArgs a)
     }
     top = wave_max(top);
     if (lane == 0) L.best[wave] = top;
+#pragma unroll
+    for (int i = 0; i < SAMPLE_BINS / SAMPLE_WG; ++i) L.hist[tid + i * SAMPLE_WG] = 0ull;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < SAMPLE_WAVES; ++i) top = vmax(top, L.best[i]);
@@ -818,11 +974,11 @@ __global__ __launch_bounds__(SAMPLE_WG) void k_sample_rows(SampleArgs a)
         return;
     }
     const SampleWeights w(top, s.c, a.unit_bits);
-    if (top < INFINITY) {
+    if (top < INFINITY && w.near) {
         if (s.mode == SAMPLE_PLAIN) {
             for (int t = tid; t < a.tiles; t += SAMPLE_WG)
-                L.tile_mass[t] = L.tile_top[t] > neg_inf() ? (unsigned long long)rint(ldexp(tiles[t].mass * w(L.tile_top[t]), a.unit_bits)) : 0ull;
-            count = sum_of_all(count, L);
+                L.tile_mass[t] = L.tile_top[t] > neg_inf() ? (unsigned long long)rint(in_row(tiles[t].mass, L.tile_top[t], w, a.unit_bits)) : 0ull;
+            count = sum_of_all<0>(count, L);
             draw_by_tiles<DT>(a, n, row, s, {value_key(neg_inf()) + 1u, -INFINITY, w}, (int)count, L);
             return;
         }
@@ -833,7 +989,10 @@ __global__ __launch_bounds__(SAMPLE_WG) void k_sample_rows(SampleArgs a)
                 return;
             }
         }
-        if (s.mode == SAMPLE_STEPPED && row_by_steps<DT>(a, n, row, s, w, tiles, L)) return;
+        if (s.mode == SAMPLE_STEPPED && found->found) {
+            row_by_steps<DT>(a, n, row, s, w, *found, tiles, L);
+            return;
+        }
         __syncthreads();
     }
     row_by_sweeps<DT>(a, n, row, s, w, L);

@@ -20,7 +20,7 @@ using namespace svip;
 size_t svip_sample_workspace_bytes(int dtype, int N, int V)
 {
     if (!dtype_ok(dtype) || check_sample_sizes(N, V)) return 0;
-    return 512 + up256((size_t)N * sample_tiles(V) * sizeof(TileData));          // flag word, tiles
+    return 512 + up256((size_t)N * row_bytes(sample_tiles(V)));          // flag word, rows
 }
 
 svip_status svip_sample(const void *logits, int dtype, int N, int V, long long row_stride, const float *temperature, const int *top_k,
@@ -39,12 +39,17 @@ svip_status svip_sample(const void *logits, int dtype, int N, int V, long long r
     a.unit_bits = 62 - log2_v < 51 ? 62 - log2_v : 51;
     a.tiles = sample_tiles(V);
     a.groups = ceil_div(a.tiles, TILES_WAVES);
-    a.tile_data = static_cast<char *>(workspace) + 512;
+    // a workgroup looks for the border for itself, 6 us: where there are many, for 16 tiles at a time and not for four
+    a.border_groups = (long long)N * a.groups <= 2048 ? a.groups : ceil_div(a.groups, 4);
+    a.data = static_cast<char *>(workspace) + 512;
     const bool ok = by_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         using X = std::conditional_t<DT == SVIP_F32, float, std::conditional_t<DT == SVIP_BF16, bf16, f16>>;
         const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-        return launch(k_sample_tiles<X>, (long long)N * a.groups, TILES_WG, st, a) && launch(k_sample_rows<X>, N, SAMPLE_WG, st, a);
+        const long long grid = (long long)N * a.groups;
+        if (!launch(k_sample_tiles<X>, grid, TILES_WG, st, a)) return false;
+        if ((top_p || min_p) && !launch(k_sample_border<X>, (long long)N * a.border_groups, TILES_WG, st, a)) return false;
+        return launch(k_sample_rows<X>, N, SAMPLE_WG, st, a);
     });
     return ok ? SVIP_OK : SVIP_ERR_HIP;
 }
