@@ -6,17 +6,17 @@
 // 17 instructions against 7.  Sums that decide are integers in units of 2^-S of the largest weight (S = 62 - ceil(log2 V)), so that no
 // order of additions changes a result and atomics may be used.
 //
-// Two launches, three where a call has top_p or min_p.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, a lane a chunk of 64
-// of them.  k_sample_rows, a workgroup each row, does what the row's settings need beside that.  What a wave leaves for the row:
+// Two launches, three where a call has top_p or min_p.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, in chunks
+// of 64 neighbours.  k_sample_rows, a workgroup each row, does what the row's settings need beside that.  What a wave leaves for the row:
 //   T = 0         the tile's maximum
 //   no filter     and its mass; the draw finds the tile by the masses and goes through that tile alone again
 //   top-k         and the maximum of every chunk.  The k-th largest of those is no larger than the k-th largest logit, so chunks below it hold no
 //                 candidate: the others are read again, what is at or above it goes into a list in LDS, and all settings are decided on the list
-//   top-p, min-p  and the mass of the tile's logits from the top down to each of 512 steps of 1/16 in log2 w.  From the tiles' masses follows the step
+//   top-p, min-p  and the mass of the tile's logits from the top down to each of 512 equal steps of log2 w, which reach as far as the border can be.  From the tiles' masses follows the step
 //                 that holds the border, exactly; k_sample_border reads such rows again, without exponentials, counts what lies above that step and
 //                 marks what lies in it, tile by tile; a list of those decides what of them stays, and the draw goes by the tiles' masses and through one tile.
-// Rows that do not fit these (a top_k of more than 1024, a list that runs over, +inf, a border below 2^-31 of the largest weight) are swept as
-// often as a radix select over their keys needs (row_by_sweeps).
+// Rows that do not fit these (a top_k of more than 1024, a list that runs over, +inf, logits of more than 2^18 octaves) are swept as often as a
+// radix select over their keys needs (row_by_sweeps).
 #pragma once
 #include "../../include/svip.h"
 #include "warp_kernels.h"
@@ -43,9 +43,8 @@ struct SampleArgs {
 
 constexpr int TILES_WG = 256, TILES_WAVES = TILES_WG / 64;             // k_sample_tiles
 constexpr int SAMPLE_WG = 512, SAMPLE_WAVES = SAMPLE_WG / 64;          // k_sample_rows
-constexpr int SAMPLE_CHUNK = 64, SAMPLE_TILE = 64 * SAMPLE_CHUNK;       // logits of a lane and of a wave
-constexpr int SAMPLE_STEPS = 512;                      // of log2 w, a 16th each
-constexpr float STEPS_PER_OCTAVE = 16.f;
+constexpr int SAMPLE_CHUNK = 64, SAMPLE_TILE = 64 * SAMPLE_CHUNK;       // logits of a chunk and of a wave, which has as many as lanes
+constexpr int SAMPLE_STEPS = 512;                      // of log2 w
 constexpr int TILE_UNIT_BITS = 50;                     // masses of a tile, relative to its own R: 2^12 weights of up to 2^1/2 fit 64 bits
 constexpr int SAMPLE_BINS = 1024;
 constexpr int SAMPLE_LIST = 4096;
@@ -151,6 +150,7 @@ struct Settings {
     double top_p;              // 1: off
     double log2_min_p;         // -inf: off
     double u;
+    float step_scale;          // logit -> steps of log2 w
     SampleMode mode;
 };
 __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int n)
@@ -164,6 +164,10 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int n)
     s.top_p = p < 1.f ? (double)p : 1.0;
     s.log2_min_p = m > 0.f ? log2((double)m) : -INFINITY;
     s.u = u;
+    // What lies below (1 - top_p) / V of the largest weight has less than 1 - top_p of the mass in all, so the border is above it, and it is not below min_p.  On
+    // flat rows, where a step has the more logits the wider it is, this is 25 steps to the octave for top_p 0.9 of 128256, and 118 for min_p 0.05.
+    const double octaves = fmin(p < 1.f ? log2((double)a.V / (1.0 - (double)p)) : INFINITY, -s.log2_min_p);
+    s.step_scale = (float)(s.c * (double)(SAMPLE_STEPS - 4) / (octaves + 0.5));
     s.mode = bad                      ? SAMPLE_BAD
              : T == 0.f               ? SAMPLE_GREEDY
              : s.top_k > SAMPLE_TOP_K ? SAMPLE_SWEPT
@@ -187,6 +191,7 @@ struct SampleLds {
     int last;
 };
 
+constexpr int DPP_HALF_MIRROR = 0x141;  // row_half_mirror: lane i of 8 has lane 7 - i's
 // NaN counts as -inf.
 __device__ __forceinline__ float sample_logit(float z) { return z == z ? z : neg_inf(); }
 
@@ -265,6 +270,8 @@ __device__ __forceinline__ int find_bin(SampleLds &L, T target_of, unsigned long
     return all < target ? -1 : L.found;
 }
 
+// Spans of keys in which a storage type has one number at most are below 2^this.
+template <typename DT> constexpr int SPAN_LOW = std::is_same<DT, bf16>::value ? 16 : VecOf<DT>::N == 8 ? 13 : 0;
 // The largest key v with measure(keys >= v) >= target, among those between lo and hi that each(f) calls f(key, value) for; lo if all of them fall short.
 // A thousandth of the span at a time, down to spans of 2^LOW (where one number of the storage type has room, what is found may be a lower key that
 // separates it from the next one as well).  *above: the measure of the keys above it.
@@ -373,13 +380,13 @@ __device__ __forceinline__ void row_by_sweeps(const SampleArgs &a, int n, const 
         });
     };
     unsigned long long above;
-    if (s.top_k) low = select_key<KEY_LOW<DT>>(each, low, high, (unsigned long long)s.top_k, L, [](float) { return 1ull; }, &above);
+    if (s.top_k) low = select_key<SPAN_LOW<DT>>(each, low, high, (unsigned long long)s.top_k, L, [](float) { return 1ull; }, &above);
     const auto mass_of = [&](float z) { return w.units(z); };
     if (s.top_p < 1.0) {
         unsigned long long mass = 0ull;
         each([&](unsigned key, float z) { mass += key >= low ? mass_of(z) : 0ull; });
         mass = sum_of_all<0>(mass, L);
-        low = select_key<KEY_LOW<DT>>(each, low, high, max(1ull, (unsigned long long)ceil(s.top_p * (double)mass)), L, mass_of, &above);
+        low = select_key<SPAN_LOW<DT>>(each, low, high, max(1ull, (unsigned long long)ceil(s.top_p * (double)mass)), L, mass_of, &above);
     }
     const Keep keep = {low, s.log2_min_p, w};
     // masses of runs of vectors, in index order
@@ -405,24 +412,45 @@ __device__ __forceinline__ void row_by_sweeps(const SampleArgs &a, int n, const 
     draw_in_range<DT>(a, n, row, bin * per * 64, min(nvec, (bin + 1) * per * 64), keep, at(total) - before, total, (int)kept, L);
 }
 
-// Appends to the list those of a vector's logits that pass; L.n_list counts them all, also those that have no place.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ unsigned dpp_mov_or_zero_u32(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xF, true);
+}
+// Inclusive prefix sum over the lanes of a wave, as wave_inclusive_sum but on 32-bit integers.
+__device__ __forceinline__ unsigned wave_inclusive_sum_u32(unsigned v)
+{
+    v += dpp_mov_or_zero_u32<0x111, 0xF>(v);
+    v += dpp_mov_or_zero_u32<0x112, 0xF>(v);
+    v += dpp_mov_or_zero_u32<0x114, 0xF>(v);
+    v += dpp_mov_or_zero_u32<0x118, 0xF>(v);
+    v += dpp_mov_or_zero_u32<0x142, 0xA>(v);
+    v += dpp_mov_or_zero_u32<0x143, 0xC>(v);
+    return v;
+}
+
+// Appends to the list those of a vector's logits that pass; L.n_list counts them all, also those that have no place.  All lanes of a wave.
 template <int N, typename P>
 __device__ __forceinline__ void append(SampleLds &L, const float (&z)[N], int index, P pass)
 {
     unsigned at = 0u;
 #pragma unroll
     for (int e = 0; e < N; ++e) at |= pass(z[e]) ? 1u << e : 0u;
-    if (!at) return;
-    unsigned slot = lds_add(&L.n_list, (unsigned)__popc(at));
+    if (!__ballot(at != 0u)) return;
+    const unsigned count = (unsigned)__popc(at), incl = wave_inclusive_sum_u32(count), all = (unsigned)read_lane((int)incl, 63);
+    unsigned slot = (threadIdx.x & 63) == 0 ? lds_add(&L.n_list, all) : 0u;
+    slot = (unsigned)__builtin_amdgcn_readfirstlane((int)slot) + incl - count;
+    for (; at; at &= at - 1u) {
+        const int e = __ffs((int)at) - 1;
+        float v = z[0];
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-        if (at >> e & 1u) {
-            if (slot < SAMPLE_LIST) {
-                L.key[slot] = value_key(z[e]);
-                L.index[slot] = (unsigned)(index + e);
-            }
-            ++slot;
+        for (int i = 1; i < N; ++i) v = e == i ? z[i] : v;
+        if (slot < SAMPLE_LIST) {
+            L.key[slot] = value_key(v);
+            L.index[slot] = (unsigned)(index + e);
         }
+        ++slot;
+    }
 }
 
 // The same for a list that has four threads for each candidate: every candidate against every other, in place of selects.
@@ -476,12 +504,12 @@ __device__ __forceinline__ void row_by_list(const SampleArgs &a, int n, const DT
     };
     const auto mass_of = [&](float z) { return w.units(z); };
     unsigned long long above;
-    unsigned low = select_key<KEY_LOW<DT>>(each, lo, high, (unsigned long long)s.top_k, L, [](float) { return 1ull; }, &above);
+    unsigned low = select_key<SPAN_LOW<DT>>(each, lo, high, (unsigned long long)s.top_k, L, [](float) { return 1ull; }, &above);
     if (s.top_p < 1.0) {
         unsigned long long mass = 0ull;
         each([&](unsigned key, float z) { mass += key >= low ? mass_of(z) : 0ull; });
         mass = sum_of_all<0>(mass, L);
-        low = select_key<KEY_LOW<DT>>(each, low, high, max(1ull, (unsigned long long)ceil(s.top_p * (double)mass)), L, mass_of, &above);
+        low = select_key<SPAN_LOW<DT>>(each, low, high, max(1ull, (unsigned long long)ceil(s.top_p * (double)mass)), L, mass_of, &above);
     }
     const Keep keep = {low, s.log2_min_p, w};
     unsigned long long mass = 0ull, count = 0ull;
@@ -510,7 +538,7 @@ template <typename DT>
 __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, const TileData *tiles, int top_k, float top, unsigned *lowest, SampleLds &L)
 {
     constexpr int N = VecOf<DT>::N, U = SAMPLE_CHUNK / N;
-    const int tid = threadIdx.x, chunks = a.tiles * 64;
+    const int tid = threadIdx.x, lane = tid & 63, chunks = a.tiles * 64;
     const unsigned high = value_key(top), none = value_key(neg_inf());
     constexpr int HELD = 4;                // pairs of chunks that a thread keeps; those of more than 4096 chunks are read each time
     const auto pair = [&](int i) { return reinterpret_cast<const float2 *>(tiles[i / 32].chunk_top)[i % 32]; };
@@ -523,8 +551,9 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
             f(2 * (tid + q * SAMPLE_WG), held[q].x);
             f(2 * (tid + q * SAMPLE_WG) + 1, held[q].y);
         }
-        for (int i = tid + HELD * SAMPLE_WG; i < chunks / 2; i += SAMPLE_WG) {
-            const float2 two = pair(i);
+        for (int i0 = HELD * SAMPLE_WG; i0 < chunks / 2; i0 += SAMPLE_WG) {        // (by whole waves)
+            const int i = i0 + tid;
+            const float2 two = i < chunks / 2 ? pair(i) : make_float2(neg_inf(), neg_inf());
             f(2 * i, two.x);
             f(2 * i + 1, two.y);
         }
@@ -549,34 +578,37 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
     // the chunks that reach the pivot, then their logits (the chunks' numbers where other settings have the tiles' masses)
     unsigned short *const reach = reinterpret_cast<unsigned short *>(L.tile_mass);
     constexpr unsigned MOST = sizeof(L.tile_mass) / 2;
-    each([&](int chunk, float z) {
-        if (z > neg_inf() && value_key(z) >= pivot) {
-            const unsigned slot = lds_add(&L.count, 1u);
-            if (slot < MOST) reach[slot] = (unsigned short)chunk;
-        }
+    each([&](int chunk, float z) {         // (a slot for each lane from one addition to the count: 64 additions to one address take 64 turns)
+        const bool reaches = z > neg_inf() && value_key(z) >= pivot;
+        const unsigned long long mask = __ballot(reaches);
+        if (!mask) return;
+        unsigned slot = lane == 0 ? lds_add(&L.count, (unsigned)__popcll(mask)) : 0u;
+        slot = (unsigned)__builtin_amdgcn_readfirstlane((int)slot) + __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+        if (reaches && slot < MOST) reach[slot] = (unsigned short)chunk;
     });
     __syncthreads();
     if (L.count > MOST || chunks > 65536) return false;
     const int items = (int)L.count * U;
     constexpr int AT_ONCE = 4;
-    for (int i0 = tid; i0 < items; i0 += AT_ONCE * SAMPLE_WG) {
+    for (int i0 = 0; i0 < items; i0 += AT_ONCE * SAMPLE_WG) {
         typename RawOf<DT>::type raw[AT_ONCE];
         int at[AT_ONCE];
 #pragma unroll
         for (int b = 0; b < AT_ONCE; ++b) {
-            const int i = min(i0 + b * SAMPLE_WG, items - 1), chunk = reach[i / U];
-            at[b] = (chunk / 64 * U + i % U) * 64 + chunk % 64;
-            const bool mine = i0 + b * SAMPLE_WG < items && at[b] * N < a.V;
+            if (i0 + b * SAMPLE_WG >= items) break;
+            const int i = i0 + b * SAMPLE_WG + tid, chunk = reach[min(i, items - 1) / U];
+            at[b] = chunk * U + i % U;
+            const bool mine = i < items && at[b] * N < a.V;
             raw[b] = warp_load<DT>(row, mine ? at[b] : 0, a.V);
             if (!mine) at[b] = -1;
         }
 #pragma unroll
         for (int b = 0; b < AT_ONCE; ++b) {
-            if (at[b] < 0) continue;
+            if (i0 + b * SAMPLE_WG >= items) break;
             float z[N];
             unpack<DT>(raw[b], z);
 #pragma unroll
-            for (int e = 0; e < N; ++e) z[e] = sample_logit(z[e]);
+            for (int e = 0; e < N; ++e) z[e] = at[b] < 0 ? neg_inf() : sample_logit(z[e]);
             append<N>(L, z, at[b] * N, [&](float x) { return x > neg_inf() && value_key(x) >= pivot; });
         }
     }
@@ -668,7 +700,7 @@ __device__ __forceinline__ void row_by_steps(const SampleArgs &a, int n, const D
     if (len <= SAMPLE_LIST) {
         for (int t = tid >> 6; t < a.tiles; t += SAMPLE_WAVES) {
             unsigned long long word = tiles[t].in_step[lane];
-            const unsigned count = (unsigned)__popcll(word), incl = (unsigned)wave_inclusive_sum_u64(count), all = (unsigned)read_lane((int)incl, 63);
+            const unsigned count = (unsigned)__popcll(word), incl = wave_inclusive_sum_u32(count), all = (unsigned)read_lane((int)incl, 63);
             unsigned to = lane == 0 && all ? atomicAdd(&L.n_list, all) : 0u;
             to = (unsigned)__builtin_amdgcn_readfirstlane((int)to) + incl - count;
             const unsigned first = (unsigned)t * SAMPLE_TILE + lane / N * 64 * N + lane % N;
@@ -685,7 +717,7 @@ __device__ __forceinline__ void row_by_steps(const SampleArgs &a, int n, const D
         const auto each = [&](auto f) {
             for (unsigned i = tid; i < (unsigned)len; i += SAMPLE_WG) f(L.key[i], key_value(L.key[i]));
         };
-        if (by_mass && len) low = select_key<KEY_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
+        if (by_mass && len) low = select_key<SPAN_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
         for (unsigned i = tid; i < (unsigned)len; i += SAMPLE_WG) {
             if (L.key[i] < low) continue;
             ++stay;
@@ -700,7 +732,7 @@ __device__ __forceinline__ void row_by_steps(const SampleArgs &a, int n, const D
             });
         };
         const auto each = [&](auto f) { each_index([&](int, float z) { f(value_key(z), z); }); };
-        if (by_mass) low = select_key<KEY_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
+        if (by_mass) low = select_key<SPAN_LOW<DT>>(each, low, high, target - above, L, mass_of, &more);
         each_index([&](int i, float z) {
             if (value_key(z) < low) return;
             ++stay;
@@ -715,7 +747,7 @@ template <typename DT>
 __global__ __launch_bounds__(TILES_WG, VecOf<DT>::N == 8 ? 8 : 4) void k_sample_tiles(SampleArgs a)
 {
     constexpr int N = VecOf<DT>::N, U = SAMPLE_CHUNK / N, PER = SAMPLE_STEPS / 64;
-    __shared__ unsigned long long all_steps[TILES_WAVES][SAMPLE_STEPS];
+    __shared__ unsigned long long all_steps[TILES_WAVES][SAMPLE_STEPS - 1 + 64];       // (the last, which many share, for each lane)
     const int n = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - n * a.groups;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), V = a.V;
     const DT *row = static_cast<const DT *>(a.logits) + n * a.row_stride;
@@ -731,16 +763,24 @@ __global__ __launch_bounds__(TILES_WG, VecOf<DT>::N == 8 ? 8 : 4) void k_sample_
     }
     const Settings s = settings_of(a, n);
     if (s.mode == SAMPLE_BAD) return;
-    float top = neg_inf();
+    float top = neg_inf(), chunk_top = neg_inf();
     int count = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        float z[N];
+        float z[N], most = neg_inf();
         unpack<DT>(raw[u], z);
 #pragma unroll
-        for (int e = 0; e < N; ++e) top = vmax(top, vmax(z[e], z[e]));         // (a signalling NaN is quiet then, and passed over)
+        for (int e = 0; e < N; ++e) most = vmax(most, vmax(z[e], z[e]));       // (a signalling NaN is quiet then, and passed over)
+        top = vmax(top, most);
+        if (s.mode == SAMPLE_TOPK) {       // a chunk is U lanes side by side: of vector u lane u of each U keeps it
+            most = vmax(most, dpp_mov<DPP_QUAD_XOR1>(most));
+            most = vmax(most, dpp_mov<DPP_QUAD_XOR2>(most));
+            most = vmax(most, dpp_mov<DPP_HALF_MIRROR>(most));
+            if (U == 16) most = vmax(most, dpp_mov<DPP_ROW_ROR8>(most));
+            chunk_top = lane % U == u ? most : chunk_top;
+        }
     }
-    if (s.mode == SAMPLE_TOPK) mine->chunk_top[lane] = top;
+    if (s.mode == SAMPLE_TOPK) mine->chunk_top[lane % U * (64 / U) + lane / U] = chunk_top;
     top = wave_max(top);
     const SampleWeights w(top, s.c, TILE_UNIT_BITS);
     double mass = 0.0;
@@ -767,9 +807,10 @@ __global__ __launch_bounds__(TILES_WG, VecOf<DT>::N == 8 ? 8 : 4) void k_sample_
     if (s.mode != SAMPLE_STEPPED || !(top > neg_inf())) return;
     unsigned long long *const steps = all_steps[wave];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) steps[lane + 64 * i] = 0ull;
+    for (int i = 0; i <= PER; ++i)
+        if (lane + 64 * i < SAMPLE_STEPS - 1 + 64) steps[lane + 64 * i] = 0ull;
     __builtin_amdgcn_wave_barrier();
-    const float scale = (float)(s.c * (double)STEPS_PER_OCTAVE), first = step_of(top, scale);
+    const float scale = s.step_scale, first = step_of(top, scale);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         float z[N];
@@ -777,14 +818,17 @@ __global__ __launch_bounds__(TILES_WG, VecOf<DT>::N == 8 ? 8 : 4) void k_sample_
         unpack<DT>(raw[u], z);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            atomicAdd(&steps[(int)fminf(first - step_of(z[e], scale), (float)(SAMPLE_STEPS - 1))], units_of(w.of_tile(z[e]), w.unit));
+            const float step = first - step_of(z[e], scale);
+            atomicAdd(&steps[step < (float)(SAMPLE_STEPS - 1) ? (int)step : SAMPLE_STEPS - 1 + lane], units_of(w.of_tile(z[e]), w.unit));
             if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
     }
     __builtin_amdgcn_wave_barrier();
+    unsigned long long rest = steps[SAMPLE_STEPS - 1 + lane];
+    rest = wave_reduce(rest, OpSum{});
     unsigned long long h[PER], sum = 0ull;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += h[i] = steps[lane * PER + i];
+    for (int i = 0; i < PER; ++i) sum += h[i] = lane * PER + i < SAMPLE_STEPS - 1 ? steps[lane * PER + i] : rest;
     unsigned long long run = wave_inclusive_sum_u64(sum) - sum;
 #pragma unroll
     for (int i = 0; i < PER; ++i) mine->down_to[lane * PER + i] = run += h[i];
@@ -804,6 +848,11 @@ __device__ __forceinline__ float least_that(P pass)
     }
     return key_value(pass(key_value(at)) ? at : at + 1u);
 }
+
+// v with lane `lane` set to a uniform value.  (Clang names no builtin for this instruction; as inline assembly it would miss the two wait states that it needs
+// behind a vector instruction's write of the scalar register.)
+__device__ unsigned llvm_writelane(unsigned value, unsigned lane, unsigned v) __asm("llvm.amdgcn.writelane.i32");
+__device__ __forceinline__ unsigned write_lane(unsigned v, unsigned lane, unsigned value) { return llvm_writelane(value, lane, v); }
 
 // Rows with top_p or min_p and no top_k: the step that holds the border, by every workgroup of the row for itself, and what its tiles have in it.
 template <typename DT>
@@ -841,17 +890,17 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
 #pragma unroll
     for (int i = 0; i < TILES_WAVES; ++i) top = vmax(top, wave_top[i]);
     const SampleWeights w(top, s.c, a.unit_bits);
-    const float scale = (float)(s.c * (double)STEPS_PER_OCTAVE), first = step_of(top, scale);
+    const float scale = s.step_scale, first = step_of(top, scale);
     const auto give_up = [&]() {
         if (group == 0 && tid == 0) found->found = 0;
     };
     if (!(top > neg_inf() && fabsf(first) < 8388608.f && w.near)) return give_up();      // (numbers of steps are whole numbers in fp32)
-    // mass of tile t down to the end of the row's step r (counted from its first, downwards), in the row's units
+    // mass of tile t down to the end of the row's step r (counted from its first, downwards; of the last: all of it), in the row's units
     const auto tile_down_to = [&](int t, int r) -> unsigned long long {
         if (!(tile_top[t] > neg_inf())) return 0ull;
-        const float i = (float)r - (first - step_of(tile_top[t], scale));
+        const float i = r < SAMPLE_STEPS - 1 ? (float)r - (first - step_of(tile_top[t], scale)) : (float)(SAMPLE_STEPS - 1);
         if (!(i >= 0.f)) return 0ull;
-        const unsigned long long mass = tiles[t].down_to[i < (float)SAMPLE_STEPS ? (int)i : SAMPLE_STEPS - 1];
+        const unsigned long long mass = tiles[t].down_to[(int)i];
         return (unsigned long long)rint(in_row((double)mass, tile_top[t], w, a.unit_bits - TILE_UNIT_BITS));
     };
     // of the row down to the end of eight steps side by side: threads 32 i .. 32 i + 31 have the sum of r(i)
@@ -907,21 +956,24 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
     for (; tile < a.tiles; tile += a.border_groups * TILES_WAVES) {
         if (tile >= a.border_groups * TILES_WAVES) load(tile);
         TileData *const mine = tiles + tile;
-        int kept = 0, undecided = 0;
-        unsigned long long word = 0ull;    // (lane u N + e's)
+        int kept = 0;
+        unsigned lo = 0u, hi = 0u;         // the word of each lane
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float z[N];
             unpack<DT>(raw[u], z);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const unsigned long long over = __ballot(z[e] >= upper), in = __ballot(z[e] >= lower) & ~over;
-                kept += __popcll(over);
-                undecided += __popcll(in);
-                word = lane == u * N + e ? in : word;
+                kept += z[e] >= upper;
+                const unsigned long long in = __ballot(z[e] >= lower && !(z[e] >= upper));
+                lo = write_lane(lo, u * N + e, (unsigned)in);
+                hi = write_lane(hi, u * N + e, (unsigned)(in >> 32));
+                __builtin_amdgcn_sched_barrier(0);     // (or 128 scalar registers are held for the words)
             }
         }
-        mine->in_step[lane] = word;
+        mine->in_step[lane] = (unsigned long long)hi << 32 | lo;
+        const int undecided = wave_reduce((int)(__popc(lo) + __popc(hi)), OpSum{});
+        kept = wave_reduce(kept, OpSum{});
         if (lane == 0) {
             mine->above = tile_down_to(tile, step - 1);
             mine->kept = kept;

@@ -39,8 +39,8 @@ svip_status svip_sample(const void *logits, int dtype, int N, int V, long long r
     a.unit_bits = 62 - log2_v < 51 ? 62 - log2_v : 51;
     a.tiles = sample_tiles(V);
     a.groups = ceil_div(a.tiles, TILES_WAVES);
-    // a workgroup looks for the border for itself, 6 us: where there are many, for 16 tiles at a time and not for four
-    a.border_groups = (long long)N * a.groups <= 2048 ? a.groups : ceil_div(a.groups, 4);
+    // a workgroup looks for the border for itself, 6 us: where there are many, for eight tiles at a time and not for four
+    a.border_groups = (long long)N * a.groups <= 2048 ? a.groups : ceil_div(a.groups, 2);
     a.data = static_cast<char *>(workspace) + 512;
     const bool ok = by_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
