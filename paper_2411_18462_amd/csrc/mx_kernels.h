@@ -140,6 +140,12 @@ __global__ __launch_bounds__(MX_WG) void k_mx_rows(MxRowsArgs a)
 }
 
 // ---- logits --------------------------------------------------------------------------------------------------------------------------------
+//
+// Tiles of the product as in head_tile.h, copied into LDS step by step of K, two buffers deep or more.  A step is 128 bytes of a row: 256 values of 4-bit
+// hidden states, multiplied in two halves, and 128 values of 8-bit ones, with 64 bytes of the weight.  A copy takes a compute unit 7 cycles for each cache
+// line that it touches, whether 128 bytes of it or 4, and scales copied step by step would be as many lines as the codes; they come in groups of GROUP steps.
+
+template <int BITS> constexpr int MX_STEP = BITS == 4 ? 2 * MX_RUN : MX_RUN;       // values of K to a step; BITS: of the hidden states
 
 struct MxLogitsArgs {
     Operand weight, hidden;    // codes, in bytes; m = vocabulary, n = rows
@@ -153,61 +159,100 @@ struct MxLogitsArgs {
     long long part_stride;
 };
 
-constexpr int MX_STEP = 2 * STEP_BYTES;                // values of K to a step
-
 // Copies 4 bytes a lane into LDS at `lds` (wave-uniform) + 4 * lane; see copy_to_lds.
-__device__ __forceinline__ void copy4_to_lds(const char *lane_address, unsigned lds)
+__device__ __forceinline__ void copy4_to_lds(const char *base, unsigned voff, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(lane_address) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
 
-// The scales of a step of ROWS rows of 4-bit codes: 8 bytes each, [ROWS][8] in LDS.
+constexpr int MX_HALF = MX_RUN / 2;                    // bytes of a run
+
+// A tile of codes in 4 bits in LDS with steps of 128 values: lines of 128 bytes hold two rows of 64.  The 16 bytes q (0 .. 3) of row r are chunk
+// (4 (r % 2) + q) ^ (r / 4) % 4 of line r / 2, so that the same bytes of 16 neighbour rows, which 16 lanes read at a time, lie in different banks.
+__device__ __forceinline__ unsigned mx_place(int row, int q) { return (unsigned)((row >> 1) * 128 + (((row & 1) * 4 + q) ^ (row >> 2 & 3)) * 16); }
 template <int ROWS, int THREADS>
-struct ScaleStager {
-    static constexpr int WORDS = ROWS * 2, ROUNDS = WORDS > THREADS ? WORDS / THREADS : 1, BYTES = ROWS * 8;
-    static_assert(WORDS % 64 == 0 && (WORDS >= THREADS ? WORDS % THREADS == 0 : THREADS % WORDS == 0), "whole waves copy");
+struct CodeStager {
+    static constexpr int CHUNKS = ROWS * 4, ROUNDS = CHUNKS > THREADS ? CHUNKS / THREADS : 1, BYTES = ROWS * MX_HALF;
+    static_assert(CHUNKS % 64 == 0 && (CHUNKS >= THREADS ? CHUNKS % THREADS == 0 : THREADS % CHUNKS == 0), "whole waves copy");
     const char *base;
-    unsigned voff[ROUNDS], lds[ROUNDS];
+    unsigned voff[ROUNDS], lds[ROUNDS];                // lds: wave-uniform
     __device__ void init(const Operand &o, int rows)
     {
         base = o.base;
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
-            const int c = (r * THREADS + (int)threadIdx.x) % WORDS, row = c >> 1;
-            lds[r] = (unsigned)__builtin_amdgcn_readfirstlane(c & ~63) * 4u;
-            voff[r] = (unsigned)(row < rows ? row : rows - 1) * (unsigned)o.stride + (unsigned)(c & 1) * 4u;
+            const int c = (r * THREADS + (int)threadIdx.x) % CHUNKS, x = (c & 7) ^ (c >> 4 & 3), row = (c >> 3) * 2 + (x >> 2);
+            lds[r] = (unsigned)__builtin_amdgcn_readfirstlane(c & ~63) * 16u;
+            voff[r] = (unsigned)min(row, rows - 1) * (unsigned)o.stride + (unsigned)(x & 3) * 16u;
         }
     }
-    // k: of the step, k_end: values, a multiple of 128 (a step's second half may lie past it)
-    __device__ __forceinline__ void copy(unsigned at, int k, int k_end) const
+    __device__ __forceinline__ void copy(unsigned at, long long byte, long long, int) const
     {
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const int mine = k + ((int)threadIdx.x & 1) * MX_RUN;
-            copy4_to_lds(mine < k_end ? base + (k / MX_BLOCK + voff[r]) : reinterpret_cast<const char *>(zero_line), at + lds[r]);
-        }
+        for (int r = 0; r < ROUNDS; ++r) copy_to_lds(base + byte, voff[r], at + lds[r]);
     }
 };
-// Of a row's 8 scales those of the blocks that lane group g multiplies, g of either half: bytes 0 and 1.
-__device__ __forceinline__ int scales_of(const char *tile, int row, unsigned pick)
-{
-    const uint2 v = *reinterpret_cast<const uint2 *>(tile + row * 8);
-    return (int)__builtin_amdgcn_perm(v.y, v.x, pick);
-}
 
-// Scales of hidden states in 8 bits, one for 128 values: those of HELD steps in LDS at a time.
-constexpr int HELD = 32, HELD_PITCH = 2 * HELD + 4;
+// The scales of RUNS runs of 128 values of ROWS rows in 4 bits: [ROWS][4 RUNS] in LDS.  Rows past the end are read as the last one.
+template <int ROWS, int THREADS, int RUNS>
+struct ScaleStager {
+    static constexpr int PITCH = 4 * RUNS, BYTES = ROWS * PITCH, ROUNDS = ROWS * RUNS / THREADS;
+    static_assert(ROWS * RUNS % THREADS == 0 && THREADS % RUNS == 0, "whole rounds");
+    const char *base;
+    unsigned stride;
+    int last;
+    __device__ void init(const Operand &o, int rows)
+    {
+        base = o.base;
+        stride = (unsigned)o.stride;
+        last = rows - 1;
+    }
+    // the runs from value k on, 4 bytes a lane; past k_end, a multiple of 128, the last one of the row again.  Addresses are made here each time and not kept in
+    // registers.
+    __device__ __forceinline__ void copy(unsigned at, int k, int k_end) const
+    {
+        unsigned tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        const unsigned off = (unsigned)min(k + (int)(tid % RUNS) * MX_RUN, k_end - MX_RUN) / MX_BLOCK;
+        at += (unsigned)__builtin_amdgcn_readfirstlane(tid & ~63u) * 4u;
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            copy4_to_lds(base, (unsigned)min((int)(tid / RUNS) + r * (THREADS / RUNS), last) * stride + off, at + r * THREADS * 4);
+    }
+};
+
+// Scales of hidden states in 8 bits, one for 128 values: those of HELD runs in LDS at a time.
+constexpr int HELD = 32, HELD_PITCH = HELD + 4;
 
 __device__ __forceinline__ i32x8 wide(i32x4 v) { return __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1); }
 
+// Of a row's 8 scales of a step of two halves those of the blocks that lane group g multiplies, g of either half: bytes 0 and 1.
+__device__ __forceinline__ int scales_of(const char *row, unsigned pick)
+{
+    const uint2 v = *reinterpret_cast<const uint2 *>(row);
+    return (int)__builtin_amdgcn_perm(v.y, v.x, pick);
+}
+
 // Logits of a tile.  BITS: of the hidden states.
 template <typename S, int BITS, int DT>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::WAVES_PER_EU))) void k_mx_logits(MxLogitsArgs a)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::THREADS / 256 > S::WAVES_PER_EU ? S::THREADS / 256 : S::WAVES_PER_EU))) void k_mx_logits(MxLogitsArgs a)
 {
-    constexpr int PLANES = BITS / 4;                   // a step of 8-bit hidden states is two tiles of 128 bytes a row
-    constexpr int STAGE = (S::BM + PLANES * S::BN) * STEP_BYTES, SCALES = (S::BM + (BITS == 4 ? S::BN : 0)) * 8;
-    __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * (STAGE + SCALES)];
-    __shared__ __attribute__((aligned(4))) unsigned char held[BITS == 8 ? S::BN * HELD_PITCH : 4];
+    constexpr int STEP = MX_STEP<BITS>, HALVES = STEP / MX_RUN;
+    constexpr int CODES_A = S::BM * STEP / 2, STAGE = CODES_A + S::BN * STEP_BYTES, SCALED = S::BM + (BITS == 4 ? S::BN : 0), ROOM = S::STAGES * STAGE > 81920 ? 163840 : 81920;
+    // steps to a group: 4 if there is room, 2 or 8 where the threads take so many
+    constexpr int GROUP = S::BM * HALVES * 4 < S::THREADS || S::BN * HALVES * 4 < S::THREADS ? 8
+                          : S::STAGES * STAGE + 2 * SCALED * HALVES * 16 + (BITS == 8 ? S::BN * HELD_PITCH : 0) <= ROOM ? 4 : 2;
+    static_assert(S::STAGES - 2 < GROUP, "the wait for a group's first step covers the group's scales");
+    static_assert(S::STAGES * STAGE >= S::BM * S::BN * 2, "store_rows lays the tile out where the codes were");
+    using ScaleA = ScaleStager<S::BM, S::THREADS, GROUP * HALVES>;
+    using ScaleB = ScaleStager<S::BN, S::THREADS, GROUP * HALVES>;
+    constexpr int SCALES = SCALED * ScaleA::PITCH;
+    struct Lds {
+        char codes[S::STAGES][STAGE], scales[2][SCALES];
+        unsigned char held[BITS == 8 ? S::BN * HELD_PITCH : 0];
+    };
+    __shared__ __attribute__((aligned(1024))) Lds lds;
+    char *const smem = lds.codes[0];
     const unsigned tiles = (unsigned)a.tiles.m * (unsigned)a.tiles.n, split = blockIdx.x / tiles;
     int tm, tn;
     tile_of(blockIdx.x - split * tiles, a.tiles, 4, tm, tn);
@@ -216,17 +261,17 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
         o.base += (long long)row * o.stride;
         return o;
     };
-    Stager<KC, S::BM, S::THREADS, 1> sa;
+    std::conditional_t<BITS == 4, Stager<KC, S::BM, S::THREADS, 1>, CodeStager<S::BM, S::THREADS>> sa;
     Stager<KC, S::BN, S::THREADS, 1> sb;
-    ScaleStager<S::BM, S::THREADS> sw;
-    ScaleStager<S::BN, S::THREADS> sh;
+    ScaleA sw;
+    ScaleB sh;
     sa.init(from(a.weight, v0), a.V - v0);
     sb.init(from(a.hidden, n0), a.N - n0);
     sw.init(from(a.weight_scale, v0), a.V - v0);
     if (BITS == 4) sh.init(from(a.hidden_scale, n0), a.N - n0);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = (wave % S::WAVES_M) * S::WM, wn = (wave / S::WAVES_M) * S::WN, g = lane >> 4, l16 = lane & 15;
-    const unsigned pick = 0x0c0c0400u + 0x0101u * (unsigned)g;
+    const unsigned pick = 0x0c0c0400u + 0x0101u * (unsigned)g, place = mx_place(l16, g);
     Reader<KC, S::BM, 1> ra;
     Reader<KC, S::BN, 1> rb;
     ra.init(lane);
@@ -237,39 +282,42 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
 #pragma unroll
         for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int COPIES = decltype(sa)::ROUNDS + PLANES * decltype(sb)::ROUNDS + decltype(sw)::ROUNDS + (BITS == 4 ? decltype(sh)::ROUNDS : 0);
-    const int steps = (k_end - k0 + MX_STEP - 1) / MX_STEP;
+    constexpr int COPIES = decltype(sa)::ROUNDS + decltype(sb)::ROUNDS;
+    const int steps = (k_end - k0 + STEP - 1) / STEP, groups = (steps + GROUP - 1) / GROUP;
     const unsigned lds0 = (unsigned)(uintptr_t)smem;
-    auto copy = [&](int s) {
-        const unsigned at = lds0 + (unsigned)(s % S::STAGES) * (STAGE + SCALES);
-        const int k = k0 + s * MX_STEP;
-        sa.copy(at, k / 2, k_end / 2, 0);
-        if (BITS == 4) {
-            sb.copy(at + S::BM * STEP_BYTES, k / 2, k_end / 2, 0);
-        } else {
-#pragma unroll
-            for (int p = 0; p < 2; ++p) sb.copy(at + (S::BM + p * S::BN) * STEP_BYTES, k + p * MX_RUN, k_end, 0);
-        }
-        sw.copy(at + STAGE, k, k_end);
-        if (BITS == 4) sh.copy(at + STAGE + S::BM * 8, k, k_end);
+    // The last step of an odd K has one of two halves.  The other is zeros, with the last scales of its row again: a NaN among them stands in the first half too.
+    auto copy = [&](int s, unsigned buffer) {
+        const int k = k0 + s * STEP;
+        sa.copy(lds0 + buffer, k / 2, k_end / 2, 0);
+        if (BITS == 4)
+            sb.copy(lds0 + buffer + CODES_A, k / 2, k_end / 2, 0);
+        else
+            sb.copy(lds0 + buffer + CODES_A, k, k_end, 0);
+    };
+    auto copy_scales = [&](int group) {
+        const unsigned at = (unsigned)(uintptr_t)lds.scales[group & 1];
+        sw.copy(at, k0 + group * GROUP * STEP, k_end);
+        if (BITS == 4) sh.copy(at + ScaleA::BYTES, k0 + group * GROUP * STEP, k_end);
     };
     // (8 bits) the scales of the steps from s0 on; nobody reads those of the steps before any more
     auto hold = [&](int s0) {
-        const int count = min(2 * HELD, (k_end - k0) / MX_RUN - 2 * s0);
-        for (int i = threadIdx.x; i < S::BN * HELD / 2; i += S::THREADS) {
-            const int r = i / (HELD / 2), q = i % (HELD / 2) * 4, n = min(n0 + r, a.N - 1);
-            const char *p = a.hidden_scale.base + n * a.hidden_scale.stride + k0 / MX_RUN + 2 * s0 + q;
+        const int count = min(HELD, steps - s0);
+        for (int i = threadIdx.x; i < S::BN * HELD / 4; i += S::THREADS) {
+            const int r = i / (HELD / 4), q = i % (HELD / 4) * 4, n = min(n0 + r, a.N - 1);
+            const char *p = a.hidden_scale.base + n * a.hidden_scale.stride + k0 / MX_RUN + s0 + q;
             unsigned word = 0u;
             if (q + 4 <= count)
                 __builtin_memcpy(&word, p, 4);
             else
                 for (int e = 0; e < count - q; ++e) word |= (unsigned)(unsigned char)p[e] << (8 * e);
-            *reinterpret_cast<unsigned *>(held + r * HELD_PITCH + q) = word;
+            *reinterpret_cast<unsigned *>(lds.held + r * HELD_PITCH + q) = word;
         }
     };
+    copy_scales(0);
 #pragma unroll
     for (int s = 0; s < S::STAGES - 1; ++s)
-        if (s < steps) copy(s);
+        if (s < steps) copy(s, s * STAGE);
+    unsigned buffer = 0, next = (S::STAGES - 1) * STAGE;       // of this step, and of the one that is copied
     for (int s = 0; s < steps; ++s) {
         if (BITS == 8 && s % HELD == 0) {
             if (s) __syncthreads();
@@ -279,33 +327,37 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
             wait_copies_and_meet<(S::STAGES - 2) * COPIES>();
         else
             wait_copies_and_meet<0>();
-        if (s + S::STAGES - 1 < steps) copy(s + S::STAGES - 1);
-        const char *ta = smem + (s % S::STAGES) * (STAGE + SCALES), *tb = ta + S::BM * STEP_BYTES, *ts = ta + STAGE;
+        if (s + S::STAGES - 1 < steps) copy(s + S::STAGES - 1, next);
+        if (s % GROUP == 0 && s / GROUP + 1 < groups) copy_scales(s / GROUP + 1);
+        const char *ta = smem + buffer, *tb = ta + CODES_A, *scale = lds.scales[s / GROUP & 1] + l16 * ScaleA::PITCH + s % GROUP * (4 * HALVES);
         int sca[S::FM], scb[S::FN];
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) sca[i] = scales_of(ts, wm + 16 * i + l16, pick);
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j) {
-            const int n = wn + 16 * j + l16;
-            scb[j] = BITS == 4 ? scales_of(ts + S::BM * 8, n, pick) : *reinterpret_cast<const unsigned short *>(held + n * HELD_PITCH + s % HELD * 2);
+        for (int i = 0; i < S::FM; ++i) {
+            const char *p = scale + (wm + 16 * i) * ScaleA::PITCH;
+            sca[i] = BITS == 4 ? scales_of(p, pick) : *reinterpret_cast<const unsigned char *>(p + g);
         }
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+            scb[j] = BITS == 4 ? scales_of(scale + (S::BM + wn + 16 * j) * ScaleA::PITCH, pick) : lds.held[(wn + 16 * j + l16) * HELD_PITCH + s % HELD];
         const auto half = [&](auto which) {
             constexpr int H = decltype(which)::value;
             i32x8 fa[S::FM], fb[S::FN];
+            s16x8 v;
 #pragma unroll
             for (int j = 0; j < S::FN; ++j) {
                 if constexpr (BITS == 4) {
-                    s16x8 v;
                     rb.half(tb, wn + 16 * j, H, v);
                     fb[j] = wide(__builtin_bit_cast(i32x4, v));
                 } else {
-                    fb[j] = rb.whole(tb + H * S::BN * STEP_BYTES, wn + 16 * j);
+                    fb[j] = rb.whole(tb, wn + 16 * j);
                 }
             }
 #pragma unroll
             for (int i = 0; i < S::FM; ++i) {
-                s16x8 v;
-                ra.half(ta, wm + 16 * i, H, v);
+                if constexpr (BITS == 4)
+                    ra.half(ta, wm + 16 * i, H, v);
+                else
+                    v = *reinterpret_cast<const s16x8 *>(ta + (wm + 16 * i) * MX_HALF + place);
                 fa[i] = wide(__builtin_bit_cast(i32x4, v));
             }
 #pragma unroll
@@ -315,7 +367,9 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::W
                     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 4, BITS == 4 ? 4 : 0, H, sca[i], H, scb[j]);
         };
         half(std::integral_constant<int, 0>{});
-        half(std::integral_constant<int, 1>{});
+        if constexpr (HALVES == 2) half(std::integral_constant<int, 1>{});
+        buffer = buffer + STAGE == S::STAGES * STAGE ? 0 : buffer + STAGE;
+        next = next + STAGE == S::STAGES * STAGE ? 0 : next + STAGE;
     }
     using X = typename Stored<DT>::type;
     if (a.part) {

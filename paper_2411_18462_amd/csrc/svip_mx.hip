@@ -6,27 +6,41 @@
 
 namespace svip {
 
-using MxLarge = TileShape<256, 128, 4, 2, 2>;         // one workgroup a CU
-using MxMiddle = TileShape<128, 128, 2, 2, 2>;
-using MxSmall = TileShape<128, 64, 4, 1, 3>;          // up to 64 rows, which wait for the weight's bytes
-using MxNarrow = TileShape<64, 32, 4, 1, 4>;          // up to 32
+template <int BITS> struct MxShapes;
+template <> struct MxShapes<4> {
+    using Large = TileShape<256, 256, 4, 4, 2>;        // one workgroup a CU
+    using Middle = TileShape<128, 128, 2, 2, 2>;       // two
+    using Few = TileShape<128, 64, 4, 1, 3>;           // up to 64 rows, which wait for the weight's bytes: two
+    using Fewer = TileShape<128, 32, 4, 1, 3>;         // up to 32: two
+    using Narrow = TileShape<64, 32, 4, 1, 3>;         // and of a small vocabulary: three
+};
+template <> struct MxShapes<8> {
+    using Large = TileShape<256, 128, 2, 2, 2>;        // two
+    using Middle = TileShape<128, 128, 2, 2, 3>;
+    using Few = TileShape<128, 64, 4, 1, 4>;
+    using Fewer = TileShape<128, 32, 4, 1, 4>;
+    using Narrow = TileShape<64, 32, 4, 1, 5>;
+};
 
+constexpr int MX_UNIT = 512;                           // values: a split of K has a multiple of it: its scales begin on 16 bytes where a row's do
 constexpr int MX_FEW_ROWS = 64, MX_FEWER_ROWS = 32, MX_CUS = 256;
 
 struct MxPlan {
     int splits, per_split;
     size_t part, bytes;
 };
-static bool mx_narrow(int N, int V) { return N <= MX_FEWER_ROWS && ceil_div(V, MxSmall::BM) < 2 * MX_CUS; }
+// Up to 32 rows and fewer tiles of 128 than CUs: tiles of 64 (8 rows of 8 bits, 32000 x 4096: 15.6 us, with tiles of 128 18.8; 50257 x 5120, 32 rows: 44.8
+// against 37.9)
+static bool mx_narrow(int N, int V) { return N <= MX_FEWER_ROWS && ceil_div(V, 128) < MX_CUS; }
 static MxPlan mx_plan(int N, int V, int K)
 {
     MxPlan p = {};
-    const int steps = ceil_div(K, MX_STEP);
-    const long long tiles = mx_narrow(N, V) ? ceil_div(V, MxNarrow::BM) : ceil_div(V, MxSmall::BM), places = mx_narrow(N, V) ? 3 * MX_CUS : 2 * MX_CUS;
+    const int units = ceil_div(K, MX_UNIT);
+    const long long tiles = ceil_div(V, mx_narrow(N, V) ? 64 : 128), places = (mx_narrow(N, V) ? 3 : 2) * MX_CUS;
     long long splits = N <= MX_FEW_ROWS ? places / tiles : 1;
-    if (splits > steps / 4) splits = steps / 4;
+    if (splits > units / 2) splits = units / 2;
     if (splits < 1) splits = 1;
-    p.per_split = ceil_div(steps, splits) * MX_STEP;
+    p.per_split = ceil_div(units, splits) * MX_UNIT;
     p.splits = ceil_div(K, p.per_split);
     p.part = 512;
     p.bytes = p.part + (p.splits > 1 ? up256((size_t)p.splits * N * up(V, 4) * sizeof(float)) : 0);
@@ -122,9 +136,15 @@ svip_status svip_head_logits_mx(const void *hidden_q, const void *hidden_scale, 
             a.tiles = {ceil_div(V, S::BM), ceil_div(N, S::BN)};
             return launch(k_mx_logits<S, BITS, DT>, (long long)a.tiles.m * a.tiles.n * p.splits, S::THREADS, st, a);
         };
-        if (mx_narrow(N, V)) return in(MxNarrow{});
-        if (N <= MX_FEW_ROWS) return in(MxSmall{});
-        return (long long)ceil_div(V, MxLarge::BM) * ceil_div(N, MxLarge::BN) >= 2 * MX_CUS ? in(MxLarge{}) : in(MxMiddle{});
+        using Shapes = MxShapes<BITS>;
+        if (mx_narrow(N, V)) return in(typename Shapes::Narrow{});
+        if (N <= MX_FEWER_ROWS) return in(typename Shapes::Fewer{});
+        if (N <= MX_FEW_ROWS) return in(typename Shapes::Few{});
+        // rounds over the card, of which one of Large tiles takes 1.75 times as long as one of Middle tiles (4 bits, 128256 x 4096, 192 rows: 94 against 115 us,
+        // 65 rows: 89 against 67; 32000 x 4096, 600 rows: 83 against 73; 8 bits, 128256 x 4096, 128 rows: 78 against 92; 32000 x 4096, 100 rows: 38 against 29)
+        const auto rounds = [&](auto shape, int places) { return ceil_div((long long)ceil_div(V, decltype(shape)::BM) * ceil_div(N, decltype(shape)::BN), places); };
+        const auto large = rounds(typename Shapes::Large{}, (BITS == 4 ? 1 : 2) * MX_CUS), middle = rounds(typename Shapes::Middle{}, 2 * MX_CUS);
+        return 7 * large <= 4 * middle ? in(typename Shapes::Large{}) : in(typename Shapes::Middle{});
     };
     constexpr std::integral_constant<int, 4> four{};
     constexpr std::integral_constant<int, 8> eight{};

@@ -247,6 +247,15 @@ def test_logits_of_many_tiles(svip, N, V):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("N,V,K", [(200, 33000, 1408), (20, 33000, 4736), (20, 33000, 128), (64, 33000, 640), (300, 33000, 4480)])
+def test_logits_of_a_vocabulary(svip, bits, N, V, K):
+    """The tiles of large vocabularies over several groups of scales, and ends inside of a step."""
+    w, h = matrix4(V, K, seed=V + K), (matrix4 if bits == 4 else matrix8)(N, K, seed=N + K, spread=3)
+    got = logits(svip, h, w, BF, V, N)
+    check_logits(got, h[2], w[2], K, BF, bits)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
 def test_logits_scales_at_the_ends(svip, bits):
     """Scales from 2^-127 up to 2^127 whose product is about one, and the NaN of e8m0 on either side."""
     N, V, K = 40, 200, 256
