@@ -194,10 +194,12 @@ struct CodeStager {
 };
 
 // The scales of RUNS runs of 128 values of ROWS rows in 4 bits: [ROWS][4 RUNS] in LDS.  Rows past the end are read as the last one.
+// Rows of 32 bytes: in rows 8 to 15 of 16 neighbours the words are swapped in pairs, so that the same ones of all 16 lie in different banks.
 template <int ROWS, int THREADS, int RUNS>
 struct ScaleStager {
     static constexpr int PITCH = 4 * RUNS, BYTES = ROWS * PITCH, ROUNDS = ROWS * RUNS / THREADS;
-    static_assert(ROWS * RUNS % THREADS == 0 && THREADS % RUNS == 0, "whole rounds");
+    static_assert(ROWS * RUNS % THREADS == 0 && THREADS / RUNS % 16 == 0 && RUNS <= 8, "whole rounds, and a thread's rows swap alike");
+    __device__ static __forceinline__ unsigned place(int row, int byte) { return (unsigned)(row * PITCH + (RUNS == 8 ? byte ^ (row & 8) : byte)); }
     const char *base;
     unsigned stride;
     int last;
@@ -213,7 +215,8 @@ struct ScaleStager {
     {
         unsigned tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
-        const unsigned off = (unsigned)min(k + (int)(tid % RUNS) * MX_RUN, k_end - MX_RUN) / MX_BLOCK;
+        const unsigned run = RUNS == 8 ? tid % RUNS ^ (tid / RUNS & 8u) / 4u : tid % RUNS;
+        const unsigned off = (unsigned)min(k + (int)run * MX_RUN, k_end - MX_RUN) / MX_BLOCK;
         at += (unsigned)__builtin_amdgcn_readfirstlane(tid & ~63u) * 4u;
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r)
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::T
             wait_copies_and_meet<0>();
         if (s + S::STAGES - 1 < steps) copy(s + S::STAGES - 1, next);
         if (s % GROUP == 0 && s / GROUP + 1 < groups) copy_scales(s / GROUP + 1);
-        const char *ta = smem + buffer, *tb = ta + CODES_A, *scale = lds.scales[s / GROUP & 1] + l16 * ScaleA::PITCH + s % GROUP * (4 * HALVES);
+        const char *ta = smem + buffer, *tb = ta + CODES_A, *scale = lds.scales[s / GROUP & 1] + ScaleA::place(l16, s % GROUP * (4 * HALVES));
         int sca[S::FM], scb[S::FN];
 #pragma unroll
         for (int i = 0; i < S::FM; ++i) {
