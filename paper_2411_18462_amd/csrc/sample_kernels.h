@@ -429,31 +429,7 @@ __device__ __forceinline__ unsigned wave_inclusive_sum_u32(unsigned v)
     return v;
 }
 
-// Appends to the list those of a vector's logits that pass; L.n_list counts them all, also those that have no place.  All lanes of a wave.
-template <int N, typename P>
-__device__ __forceinline__ void append(SampleLds &L, const float (&z)[N], int index, P pass)
-{
-    unsigned at = 0u;
-#pragma unroll
-    for (int e = 0; e < N; ++e) at |= pass(z[e]) ? 1u << e : 0u;
-    if (!__ballot(at != 0u)) return;
-    const unsigned count = (unsigned)__popc(at), incl = wave_inclusive_sum_u32(count), all = (unsigned)read_lane((int)incl, 63);
-    unsigned slot = (threadIdx.x & 63) == 0 ? lds_add(&L.n_list, all) : 0u;
-    slot = (unsigned)__builtin_amdgcn_readfirstlane((int)slot) + incl - count;
-    for (; at; at &= at - 1u) {
-        const int e = __ffs((int)at) - 1;
-        float v = z[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) v = e == i ? z[i] : v;
-        if (slot < SAMPLE_LIST) {
-            L.key[slot] = value_key(v);
-            L.index[slot] = (unsigned)(index + e);
-        }
-        ++slot;
-    }
-}
-
-// The same for a list that has four threads for each candidate: every candidate against every other, in place of selects.
+// All settings decided on a list of up to SMALL_LIST candidates, with four threads each: every candidate against every other, in place of selects.
 __device__ __forceinline__ void row_by_small_list(const SampleArgs &a, int n, const Settings &s, const SampleWeights &w, SampleLds &L)
 {
     static_assert(SAMPLE_WG == 4 * SMALL_LIST && SMALL_LIST <= SAMPLE_BINS, "");
@@ -493,7 +469,7 @@ __device__ __forceinline__ void row_by_small_list(const SampleArgs &a, int n, co
         sample_answer(a, n, (int)index, (float)(w(key_value(key)) / ldexp((double)total, -a.unit_bits)), (int)count);
 }
 
-// All settings decided on the list of candidates, which holds every logit from the top_k-th largest on.
+// The same on any list of candidates.  It holds every logit from the top_k-th largest on.
 template <typename DT>
 __device__ __forceinline__ void row_by_list(const SampleArgs &a, int n, const DT *row, const Settings &s, const SampleWeights &w, unsigned lo, SampleLds &L)
 {
@@ -575,7 +551,8 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
     unsigned long long before, total;
     const int bin = find_bin<false>(L, [&](unsigned long long) { return (unsigned long long)top_k; }, &before, &total);
     const unsigned pivot = bin < 0 ? none + 1u : least + ((unsigned)bin << shift);
-    // the chunks that reach the pivot, then their logits (the chunks' numbers where other settings have the tiles' masses)
+    // the chunks that reach the pivot (their numbers where other settings have the tiles' masses), then the indices of their logits that do, with one addition to the
+    // list's length for 32 logits of each lane, then the keys (64 rows of 128256 with top_k 1000: 28 us, 37 with an addition for 8 logits and the key picked there)
     unsigned short *const reach = reinterpret_cast<unsigned short *>(L.tile_mass);
     constexpr unsigned MOST = sizeof(L.tile_mass) / 2;
     each([&](int chunk, float z) {         // (a slot for each lane from one addition to the count: 64 additions to one address take 64 turns)
@@ -589,32 +566,45 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
     __syncthreads();
     if (L.count > MOST || chunks > 65536) return false;
     const int items = (int)L.count * U;
-    constexpr int AT_ONCE = 4;
+    constexpr int AT_ONCE = 32 / N;        // a bit for each logit of a lane
+    const float least_kept = key_value(pivot);
     for (int i0 = 0; i0 < items; i0 += AT_ONCE * SAMPLE_WG) {
         typename RawOf<DT>::type raw[AT_ONCE];
-        int at[AT_ONCE];
+        bool mine[AT_ONCE];
+        const auto vector_of = [&](int i) { return reach[i / U] * U + i % U; };
 #pragma unroll
         for (int b = 0; b < AT_ONCE; ++b) {
             if (i0 + b * SAMPLE_WG >= items) break;
-            const int i = i0 + b * SAMPLE_WG + tid, chunk = reach[min(i, items - 1) / U];
-            at[b] = chunk * U + i % U;
-            const bool mine = i < items && at[b] * N < a.V;
-            raw[b] = warp_load<DT>(row, mine ? at[b] : 0, a.V);
-            if (!mine) at[b] = -1;
+            const int i = i0 + b * SAMPLE_WG + tid, at = vector_of(min(i, items - 1));
+            mine[b] = i < items && at * N < a.V;
+            raw[b] = warp_load<DT>(row, mine[b] ? at : 0, a.V);
         }
+        unsigned bits = 0u;
 #pragma unroll
         for (int b = 0; b < AT_ONCE; ++b) {
             if (i0 + b * SAMPLE_WG >= items) break;
             float z[N];
             unpack<DT>(raw[b], z);
+            unsigned some = 0u;
 #pragma unroll
-            for (int e = 0; e < N; ++e) z[e] = at[b] < 0 ? neg_inf() : sample_logit(z[e]);
-            append<N>(L, z, at[b] * N, [&](float x) { return x > neg_inf() && value_key(x) >= pivot; });
+            for (int e = 0; e < N; ++e) some |= z[e] >= least_kept ? 1u << e : 0u;
+            bits |= mine[b] ? some << (b * N) : 0u;
+        }
+        if (!__ballot(bits != 0u)) continue;
+        const unsigned count = (unsigned)__popc(bits), incl = wave_inclusive_sum_u32(count), all = (unsigned)read_lane((int)incl, 63);
+        unsigned slot = lane == 0 ? lds_add(&L.n_list, all) : 0u;
+        slot = (unsigned)__builtin_amdgcn_readfirstlane((int)slot) + incl - count;
+        for (; bits; bits &= bits - 1u, ++slot) {
+            const int q = __ffs((int)bits) - 1;
+            if (slot < SAMPLE_LIST) L.index[slot] = (unsigned)(vector_of(i0 + q / N * SAMPLE_WG + tid) * N + q % N);
         }
     }
     __syncthreads();
+    if (L.n_list > SAMPLE_LIST) return false;
+    for (unsigned i = tid; i < L.n_list; i += SAMPLE_WG) L.key[i] = value_key(sample_logit(widen(row[L.index[i]])));
+    __syncthreads();
     *lowest = pivot;
-    return L.n_list <= SAMPLE_LIST;
+    return true;
 }
 
 // Which step of log2 w a logit lies in, counted upwards from an arbitrary zero: one function for all tiles of a row.
