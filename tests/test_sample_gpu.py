@@ -122,6 +122,13 @@ def test_each_setting(svip, dtype, setting):
     check(svip, logits(N, V, dtype, seed=7), torch.rand(N, generator=gen(9)), T, k, p, m)
 
 
+@pytest.mark.parametrize("V,dtype", [(300001, BF), (1 << 22, F16), ((1 << 22) - 3, F32)])
+def test_large_vocabularies(svip, V, dtype):
+    """More chunks than a workgroup's threads keep, and as many as there may be."""
+    T, k, p, m = zip((1.0, 0, 1.0, 0.0), (1.0, 50, 0.9, 0.0), (0.7, 0, 0.9, 0.0), (1.2, 0, 1.0, 0.05), (0.9, 1024, 0.99, 0.0), (0.0, 0, 1.0, 0.0), (1.0, 1025, 1.0, 0.01))
+    check(svip, logits(7, V, dtype, seed=2), torch.rand(7, generator=gen(4)), T, k, p, m)
+
+
 @pytest.mark.parametrize("scale", [0.0, 1e-3, 0.05, 0.5])
 @pytest.mark.parametrize("setting", [(1.0, 0, 0.9, 0.0), (1.0, 60000, 0.5, 0.0), (1.0, 0, 1.0, 1e-4), (1.0, 0, 1.0, 0.0), (0.1, 30000, 1.0, 0.0), (1.0, 9000, 0.97, 0.2)])
 def test_flat_rows(svip, scale, setting):
