@@ -45,7 +45,7 @@ struct MxQuantizeArgs {
 };
 
 constexpr int MX_WG = 256;
-// 16 lanes (fp32: 32) a run, one load and one store a lane.
+// 16 lanes (fp32: 32) a run, one load and one store a lane.  HBM: 128256 x 4096 in bf16 252 us, 5.3 TB/s (a copy: 5.1); 64 x 4096 2.4 us, a launch.
 template <int DT>
 __global__ __launch_bounds__(MX_WG) void k_mx_quantize(MxQuantizeArgs a)
 {
@@ -103,7 +103,8 @@ struct MxRowsArgs {
     long long out_stride;      // elements
 };
 
-// 8 values a lane: 4 bytes of codes, 16 or 32 bytes of values.
+// 8 values a lane: 4 bytes of codes, 16 or 32 bytes of values.  HBM: 128256 x 4096 to bf16 242 us, 5.5 TB/s; 8192 rows of 4096 by their ids 21 us, 4.0 TB/s; 64 rows
+// of 2048 2.6 us, a launch.
 template <int DT>
 __global__ __launch_bounds__(MX_WG) void k_mx_rows(MxRowsArgs a)
 {
@@ -142,8 +143,17 @@ __global__ __launch_bounds__(MX_WG) void k_mx_rows(MxRowsArgs a)
 // ---- logits --------------------------------------------------------------------------------------------------------------------------------
 //
 // Tiles of the product as in head_tile.h, copied into LDS step by step of K, two buffers deep or more.  A step is 128 bytes of a row: 256 values of 4-bit
-// hidden states, multiplied in two halves, and 128 values of 8-bit ones, with 64 bytes of the weight.  A copy takes a compute unit 7 cycles for each cache
-// line that it touches, whether 128 bytes of it or 4, and scales copied step by step would be as many lines as the codes; they come in groups of GROUP steps.
+// hidden states, multiplied in two halves, and 128 values of 8-bit ones, with 64 bytes of the weight.
+//
+// Few rows wait for the weight's bytes (64 x 128256 x 2048, 8-bit hidden states: 40 us, 3.9 TB/s; 1 row: 28 us, 5.0).  Large tiles wait for what feeds the products.
+// A copy takes a compute unit about 7 cycles for each cache line that it touches, whether 128 bytes of it or 4:
+// - The scales of a row and a step are 8 bytes, and copied step by step they would be as many lines as the codes.  They come in groups of GROUP steps.
+// - 4 bits: steps of whole lines, 256 x 256 tiles.  1088 x 128256 x 4096: 385-413 us, 2.8-3.0 PFLOP/s (the library's largest 4-bit products reach 2.3 here),
+//   products under way in 41 % of the cycles at 1.9 GHz.  Leaving out one thing at a time of 434 us then: the copies 371, the reads of the scales 381 (bank
+//   conflicts, now gone), the stores 388.  16 waves of 64 x 64 take 440, 8 of 128 x 64 453, 8 that replace each fragment as soon as its products are under way
+//   512 (they spill), 4 of 128 x 128 488, two workgroups with 128 x 128 479, two with 256 x 128 in steps of 128 values 513.
+// - 8 bits: the products take twice as long, and what counts is a second workgroup that multiplies while one waits: 256 x 128 tiles twice a unit leave room
+//   for steps of 128 values only.  The same sizes: 540 us (without copies 353), in steps of 256 values with one workgroup 606-637, 256 x 256 tiles 583-605.
 
 template <int BITS> constexpr int MX_STEP = BITS == 4 ? 2 * MX_RUN : MX_RUN;       // values of K to a step; BITS: of the hidden states
 
@@ -238,10 +248,11 @@ __device__ __forceinline__ int scales_of(const char *row, unsigned pick)
 
 // Logits of a tile.  BITS: of the hidden states.
 template <typename S, int BITS, int DT>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::THREADS / 256 > S::WAVES_PER_EU ? S::THREADS / 256 : S::WAVES_PER_EU))) void k_mx_logits(MxLogitsArgs a)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::THREADS > 512 ? 4 : S::WAVES_PER_EU))) void k_mx_logits(MxLogitsArgs a)
 {
     constexpr int STEP = MX_STEP<BITS>, HALVES = STEP / MX_RUN;
-    constexpr int CODES_A = S::BM * STEP / 2, STAGE = CODES_A + S::BN * STEP_BYTES, SCALED = S::BM + (BITS == 4 ? S::BN : 0), ROOM = S::STAGES * STAGE > 81920 ? 163840 : 81920;
+    constexpr int CODES_A = S::BM * STEP / 2, STAGE = CODES_A + S::BN * STEP_BYTES, SCALED = S::BM + (BITS == 4 ? S::BN : 0);
+    constexpr int ROOM = S::STAGES * STAGE > 81920 ? 163840 : 81920;           // of LDS: all of a CU's, or half
     // steps to a group: 4 if there is room, 2 or 8 where the threads take so many
     constexpr int GROUP = S::BM * HALVES * 4 < S::THREADS || S::BN * HALVES * 4 < S::THREADS ? 8
                           : S::STAGES * STAGE + 2 * SCALED * HALVES * 16 + (BITS == 8 ? S::BN * HELD_PITCH : 0) <= ROOM ? 4 : 2;

@@ -2,21 +2,29 @@
 //
 // Weights are w = exp2((z - m) c) with c = log2(e) / T and m the row's largest logit, in 64 bits: which token a uniform falls on, and which
 // value the nucleus ends at, are borders between sums of up to V weights, and a rounding of 2^-24 in each weight moves such a border by more than
-// the narrowest cells are wide.  The fp64 pipe takes a fused multiply-add in four cycles, as the fp32 pipe does, so a weight costs about
-// 17 instructions against 7.  Sums that decide are integers in units of 2^-S of the largest weight (S = 62 - ceil(log2 V)), so that no
-// order of additions changes a result and atomics may be used.
+// the narrowest cells are wide.  A weight costs about 17 instructions of 5.3 cycles (measured; in fp32 7 of 2.7).  Sums that decide are integers in
+// units of 2^-S of the largest weight (S = 62 - ceil(log2 V), at most 51), so that no order of additions changes a result and atomics may be used.
 //
 // Two launches, three where a call has top_p or min_p.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, in chunks
 // of 64 neighbours.  k_sample_rows, a workgroup each row, does what the row's settings need beside that.  What a wave leaves for the row:
 //   T = 0         the tile's maximum
 //   no filter     and its mass; the draw finds the tile by the masses and goes through that tile alone again
 //   top-k         and the maximum of every chunk.  The k-th largest of those is no larger than the k-th largest logit, so chunks below it hold no
-//                 candidate: the others are read again, what is at or above it goes into a list in LDS, and all settings are decided on the list
-//   top-p, min-p  and the mass of the tile's logits from the top down to each of 512 equal steps of log2 w, which reach as far as the border can be.  From the tiles' masses follows the step
-//                 that holds the border, exactly; k_sample_border reads such rows again, without exponentials, counts what lies above that step and
-//                 marks what lies in it, tile by tile; a list of those decides what of them stays, and the draw goes by the tiles' masses and through one tile.
-// Rows that do not fit these (a top_k of more than 1024, a list that runs over, +inf, logits of more than 2^18 octaves) are swept as often as a
-// radix select over their keys needs (row_by_sweeps).
+//                 candidate: the others are read again, what is at or above it goes into a list in LDS, and all settings are decided on the list.  Where there
+//                 are fewer chunks than that (or more than 1024 are asked for) the row's own keys tell what goes into the list
+//   top-p, min-p  and the mass of the tile's logits from the top down to each of 512 equal steps of log2 w, which reach as far as the border can be.  From the
+//                 tiles' masses follows the step that holds the border, exactly; k_sample_border reads such rows again, without exponentials, counts what
+//                 lies above that step and marks what lies in it, tile by tile; a list of those decides what of them stays, and the draw goes by the tiles'
+//                 masses and through one tile.
+// Rows that do not fit these (a list of more than 4096, +inf, logits of more than 2^18 octaves) are swept as often as a radix select over their keys
+// needs (row_by_sweeps: 44 rows of 32000 with mixed settings took 79 us when those with a top_k of 1000 came here, and 38 by lists).
+//
+// What bounds them (us, launches of k_sample_tiles + _border + _rows; bf16):
+//   1088 x 128256   T = 0: 50 + 5 + 15, the memory (279 MB at 5.6 TB/s); no filter: 107 + 5 + 22, the fp64 pipe (83 us of weights at 2.3 GHz);
+//                   top-k 50, top-p 0.9: 57 + 7 + 31; top-p 0.9: 135 + 87 + 43, beside that the LDS additions of the steps and the second reading
+//   64 x 128256     top-k 50, top-p 0.9: 5 + 3 + 12; top-p 0.9: 15 + 12 + 16; mixed settings: 13 + 10 + 21.  A row is one workgroup's in the last
+//                   launch: latencies, one after the other
+//   1 x 32000 fp32  top-k 50, top-p 0.9: 3.9 + 1.5 + 9.4
 #pragma once
 #include "../../include/svip.h"
 #include "warp_kernels.h"
@@ -184,7 +192,7 @@ struct SampleLds {
     float tile_top[SAMPLE_MAX_TILES];
     unsigned long long wave_tot[SAMPLE_WAVES], wave_sum[3][SAMPLE_WAVES];
     float best[SAMPLE_WAVES];
-    unsigned long long found_before, total;          // (total: of draw_by_tiles)
+    unsigned long long found_before, found_upto, total;          // (total: of draw_by_tiles)
     int found;
     unsigned count, n_list;
     unsigned low;
@@ -261,6 +269,7 @@ __device__ __forceinline__ int find_bin(SampleLds &L, T target_of, unsigned long
         if (run < target && run + h[i] >= target) {
             L.found = UP ? tid * PER + i : SAMPLE_BINS - 1 - (tid * PER + i);
             L.found_before = run;
+            L.found_upto = run + h[i];
         }
         run += h[i];
     }
@@ -509,6 +518,51 @@ __device__ __forceinline__ void row_by_list(const SampleArgs &a, int n, const DT
     }
 }
 
+// What of `items` vectors of the row is not below the key `pivot` goes into the list: the indices, with one addition to the list's length for 32 logits of each lane,
+// then the keys (64 rows of 128256 with top_k 1000: 28 us, 37 with an addition for 8 logits and the key picked there).  false: the list has no room.
+template <typename DT, typename F>
+__device__ __forceinline__ bool list_from(const SampleArgs &a, const DT *row, int items, F vector_of, unsigned pivot, SampleLds &L)
+{
+    constexpr int N = VecOf<DT>::N, AT_ONCE = 32 / N;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const float least_kept = key_value(pivot);
+    for (int i0 = 0; i0 < items; i0 += AT_ONCE * SAMPLE_WG) {
+        typename RawOf<DT>::type raw[AT_ONCE];
+        bool mine[AT_ONCE];
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) {
+            if (i0 + b * SAMPLE_WG >= items) break;
+            const int i = i0 + b * SAMPLE_WG + tid, at = vector_of(min(i, items - 1));
+            mine[b] = i < items && at * N < a.V;
+            raw[b] = warp_load<DT>(row, mine[b] ? at : 0, a.V);
+        }
+        unsigned bits = 0u;
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) {
+            if (i0 + b * SAMPLE_WG >= items) break;
+            float z[N];
+            unpack<DT>(raw[b], z);
+            unsigned some = 0u;
+#pragma unroll
+            for (int e = 0; e < N; ++e) some |= z[e] >= least_kept ? 1u << e : 0u;
+            bits |= mine[b] ? some << (b * N) : 0u;
+        }
+        if (!__ballot(bits != 0u)) continue;
+        const unsigned count = (unsigned)__popc(bits), incl = wave_inclusive_sum_u32(count), all = (unsigned)read_lane((int)incl, 63);
+        unsigned slot = lane == 0 ? lds_add(&L.n_list, all) : 0u;
+        slot = (unsigned)__builtin_amdgcn_readfirstlane((int)slot) + incl - count;
+        for (; bits; bits &= bits - 1u, ++slot) {
+            const int q = __ffs((int)bits) - 1;
+            if (slot < SAMPLE_LIST) L.index[slot] = (unsigned)(vector_of(i0 + q / N * SAMPLE_WG + tid) * N + q % N);
+        }
+    }
+    __syncthreads();
+    if (L.n_list > SAMPLE_LIST) return false;
+    for (unsigned i = tid; i < L.n_list; i += SAMPLE_WG) L.key[i] = value_key(sample_logit(widen(row[L.index[i]])));
+    __syncthreads();
+    return true;
+}
+
 // Candidates of a top_k by the chunks' maxima.  false: they do not fit the list.
 template <typename DT>
 __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, const TileData *tiles, int top_k, float top, unsigned *lowest, SampleLds &L)
@@ -550,9 +604,9 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
     __syncthreads();
     unsigned long long before, total;
     const int bin = find_bin<false>(L, [&](unsigned long long) { return (unsigned long long)top_k; }, &before, &total);
+    if (bin < 0 && total * SAMPLE_CHUNK > SAMPLE_LIST) return false;       // fewer chunks than that
     const unsigned pivot = bin < 0 ? none + 1u : least + ((unsigned)bin << shift);
-    // the chunks that reach the pivot (their numbers where other settings have the tiles' masses), then the indices of their logits that do, with one addition to the
-    // list's length for 32 logits of each lane, then the keys (64 rows of 128256 with top_k 1000: 28 us, 37 with an addition for 8 logits and the key picked there)
+    // the chunks that reach the pivot (their numbers where other settings have the tiles' masses)
     unsigned short *const reach = reinterpret_cast<unsigned short *>(L.tile_mass);
     constexpr unsigned MOST = sizeof(L.tile_mass) / 2;
     each([&](int chunk, float z) {         // (a slot for each lane from one addition to the count: 64 additions to one address take 64 turns)
@@ -565,46 +619,48 @@ __device__ __forceinline__ bool list_top_k(const SampleArgs &a, const DT *row, c
     });
     __syncthreads();
     if (L.count > MOST || chunks > 65536) return false;
-    const int items = (int)L.count * U;
-    constexpr int AT_ONCE = 32 / N;        // a bit for each logit of a lane
-    const float least_kept = key_value(pivot);
-    for (int i0 = 0; i0 < items; i0 += AT_ONCE * SAMPLE_WG) {
-        typename RawOf<DT>::type raw[AT_ONCE];
-        bool mine[AT_ONCE];
-        const auto vector_of = [&](int i) { return reach[i / U] * U + i % U; };
-#pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b) {
-            if (i0 + b * SAMPLE_WG >= items) break;
-            const int i = i0 + b * SAMPLE_WG + tid, at = vector_of(min(i, items - 1));
-            mine[b] = i < items && at * N < a.V;
-            raw[b] = warp_load<DT>(row, mine[b] ? at : 0, a.V);
-        }
-        unsigned bits = 0u;
-#pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b) {
-            if (i0 + b * SAMPLE_WG >= items) break;
-            float z[N];
-            unpack<DT>(raw[b], z);
-            unsigned some = 0u;
-#pragma unroll
-            for (int e = 0; e < N; ++e) some |= z[e] >= least_kept ? 1u << e : 0u;
-            bits |= mine[b] ? some << (b * N) : 0u;
-        }
-        if (!__ballot(bits != 0u)) continue;
-        const unsigned count = (unsigned)__popc(bits), incl = wave_inclusive_sum_u32(count), all = (unsigned)read_lane((int)incl, 63);
-        unsigned slot = lane == 0 ? lds_add(&L.n_list, all) : 0u;
-        slot = (unsigned)__builtin_amdgcn_readfirstlane((int)slot) + incl - count;
-        for (; bits; bits &= bits - 1u, ++slot) {
-            const int q = __ffs((int)bits) - 1;
-            if (slot < SAMPLE_LIST) L.index[slot] = (unsigned)(vector_of(i0 + q / N * SAMPLE_WG + tid) * N + q % N);
-        }
-    }
-    __syncthreads();
-    if (L.n_list > SAMPLE_LIST) return false;
-    for (unsigned i = tid; i < L.n_list; i += SAMPLE_WG) L.key[i] = value_key(sample_logit(widen(row[L.index[i]])));
-    __syncthreads();
+    if (!list_from<DT>(a, row, (int)L.count * U, [&](int i) { return reach[i / U] * U + i % U; }, pivot, L)) return false;
     *lowest = pivot;
     return true;
+}
+
+// The same by the row's own keys, for a top_k that the chunks do not decide: from the key `least` on, if there are as many logits, a thousandth of the span at
+// a time, until what a bin and those above it hold fits the list.
+template <typename DT>
+__device__ __forceinline__ bool list_by_row(const SampleArgs &a, const DT *row, unsigned top_k, unsigned least, float top, SampleLds &L, unsigned *lowest)
+{
+    constexpr int N = VecOf<DT>::N;
+    const unsigned first = value_key(neg_inf()) + 1u;
+    unsigned lo = least, hi = value_key(top), pivot;
+    unsigned long long above = 0ull, before, total;
+    __syncthreads();                       // (who still looks at the length of a list that ran over)
+    for (;;) {
+        const int shift = max(0, 22 - __clz((int)(hi - lo)));
+        sample_sweep(row, a.V, [&](int, const float(&z)[N]) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const unsigned key = value_key(z[e]);
+                if (key >= lo && key <= hi) atomicAdd(&L.hist[(key - lo) >> shift], 1ull);
+            }
+        });
+        if (threadIdx.x == 0) L.n_list = 0u;
+        __syncthreads();
+        const int bin = find_bin<false>(L, [&](unsigned long long) { return top_k - above; }, &before, &total);
+        if (bin < 0 && lo > first) {
+            above += total;
+            hi = lo - 1u;
+            lo = first;
+            continue;
+        }
+        pivot = bin < 0 ? lo : lo + ((unsigned)bin << shift);
+        if (above + (bin < 0 ? total : L.found_upto) <= SAMPLE_LIST) break;
+        if (shift == 0) return false;
+        above += before;
+        hi = lo + min(hi - lo, (((unsigned)bin + 1u) << shift) - 1u);
+        lo = pivot;
+    }
+    *lowest = pivot;
+    return list_from<DT>(a, row, (a.V + N - 1) / N, [](int i) { return i; }, pivot, L);
 }
 
 // Which step of log2 w a logit lies in, counted upwards from an arbitrary zero: one function for all tiles of a row.
@@ -1024,9 +1080,12 @@ __global__ __launch_bounds__(SAMPLE_WG) void k_sample_rows(SampleArgs a)
             draw_by_tiles<DT>(a, n, row, s, {value_key(neg_inf()) + 1u, -INFINITY, w}, (int)count, L);
             return;
         }
-        if (s.mode == SAMPLE_TOPK) {
+        if (s.top_k && s.top_k <= SAMPLE_LIST) {
             unsigned lowest;
-            if (list_top_k<DT>(a, row, tiles, s.top_k, top, &lowest, L)) {
+            const bool by_chunks = s.mode == SAMPLE_TOPK;
+            const unsigned first = value_key(neg_inf()) + 1u;
+            if ((by_chunks && list_top_k<DT>(a, row, tiles, s.top_k, top, &lowest, L)) ||
+                list_by_row<DT>(a, row, (unsigned)s.top_k, by_chunks ? L.low : first, top, L, &lowest)) {
                 row_by_list<DT>(a, n, row, s, w, lowest, L);
                 return;
             }

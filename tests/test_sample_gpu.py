@@ -122,6 +122,19 @@ def test_each_setting(svip, dtype, setting):
     check(svip, logits(N, V, dtype, seed=7), torch.rand(N, generator=gen(9)), T, k, p, m)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+@pytest.mark.parametrize("V", [1500, 5003, 32000, 70001])
+@pytest.mark.parametrize("kind", ["plain", "masked", "ties"])
+def test_top_k_that_the_chunks_do_not_decide(svip, dtype, V, kind):
+    """More tokens than chunks of 64 logits, up to what the list of candidates holds and beyond, all but so many masked, and on values that repeat."""
+    T, k, p, m = zip((1.0, 24, 1.0, 0.0), (1.5, 600, 0.9, 0.0), (0.9, 1000, 0.99, 0.0), (1.0, 1024, 1.0, 0.01), (2.0, 1025, 0.95, 0.0), (1.0, 3000, 1.0, 0.0), (3.0, 4096, 0.8, 0.001),
+                     (1.0, 4097, 0.9, 0.0), (1.0, V - 1, 1.0, 0.0))
+    z = logits(len(T), V, dtype, seed=V + 1, masked=0.97 if kind == "masked" else 0.0)
+    if kind == "ties":
+        z.copy_((z.float() * 4).round() / 4)
+    check(svip, z, torch.rand(len(T), generator=gen(V)), T, k, p, m)
+
+
 @pytest.mark.parametrize("V,dtype", [(300001, BF), (1 << 22, F16), ((1 << 22) - 3, F32)])
 def test_large_vocabularies(svip, V, dtype):
     """More chunks than a workgroup's threads keep, and as many as there may be."""
