@@ -36,8 +36,10 @@ static MxPlan mx_plan(int N, int V, int K)
 {
     MxPlan p = {};
     const int units = ceil_div(K, MX_UNIT);
-    const long long tiles = ceil_div(V, mx_narrow(N, V) ? 64 : 128), places = (mx_narrow(N, V) ? 3 : 2) * MX_CUS;
-    long long splits = N <= MX_FEW_ROWS ? places / tiles : 1;
+    const long long tiles = N > MX_FEW_ROWS ? (long long)ceil_div(V, 128) * ceil_div(N, 128) : ceil_div(V, mx_narrow(N, V) ? 64 : 128);
+    // Splits of K that fill the chip; of more than 64 rows where a quarter of it would have work (8 bits, 512 x 2000 x 4096: 64 tiles, 27 us, in splits 18; 4 bits,
+    // 168 x 8481 x 2560: 134 tiles, 13.4 us, in splits 15.2; 100 x 32000 x 4096: 250 tiles, 21 us, in splits 30).
+    long long splits = N > MX_FEW_ROWS && tiles > MX_CUS / 2 ? 1 : (mx_narrow(N, V) ? 3 : 2) * MX_CUS / tiles;
     if (splits > units / 2) splits = units / 2;
     if (splits < 1) splits = 1;
     p.per_split = ceil_div(units, splits) * MX_UNIT;

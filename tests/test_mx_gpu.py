@@ -247,7 +247,7 @@ def test_logits_of_many_tiles(svip, N, V):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("N,V,K", [(200, 33000, 1408), (20, 33000, 4736), (20, 33000, 128), (64, 33000, 640), (300, 33000, 4480)])
+@pytest.mark.parametrize("N,V,K", [(200, 33000, 1408), (20, 33000, 4736), (20, 33000, 128), (64, 33000, 640), (300, 33000, 4480), (66, 1003, 5248), (257, 2001, 2176)])
 def test_logits_of_a_vocabulary(svip, bits, N, V, K):
     """The tiles of large vocabularies over several groups of scales, and ends inside of a step."""
     w, h = matrix4(V, K, seed=V + K), (matrix4 if bits == 4 else matrix8)(N, K, seed=N + K, spread=3)
