@@ -364,6 +364,53 @@ def test_a_drafting_loop_in_a_graph(svip):
                 assert torch.equal(captured["z"][j], eager["z"][j]) and torch.equal(captured["hidden"][j], eager["hidden"][j])
 
 
+def test_two_graphs_share_workspaces(svip):
+    """Calls of two sizes, K in splits, captured into a graph each on the same two workspaces, replayed in turn on one stream with eager calls between."""
+    E4, S8 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu
+    V, K = 3001, 2176
+    sizes = (70, 5)
+    wq, wsc = torch.empty(V, K // 2, dtype=torch.uint8, device="cuda").view(E4), torch.empty(V, K // 32, dtype=torch.uint8, device="cuda").view(S8)
+    svip.quantize_mx((torch.randn(V, K, generator=gen(1)) * 0.2).bfloat16().cuda(), q_out=wq, scale_out=wsc)
+    hw = torch.empty(max(svip.head_workspace_bytes(svip.HEAD_LOGITS_MX, BF, n, V, K) for n in sizes), dtype=torch.uint8, device="cuda")
+    sw = svip.new_sample_workspace(BF, max(sizes), V)
+    state = []
+    for N in sizes:
+        T, k, p, m = (torch.as_tensor(x, dtype=t).cuda() for x, t in zip(zip(*[SETTINGS[n % len(SETTINGS)] for n in range(N)]), (F32, torch.int32, F32, F32)))
+        state.append(dict(x=torch.empty(N, K, dtype=BF, device="cuda"), u=torch.empty(N, device="cuda"), T=T, k=k, p=p, m=m,
+                          hq=torch.empty(N, K // 2, dtype=torch.uint8, device="cuda").view(E4), hs=torch.empty(N, K // 32, dtype=torch.uint8, device="cuda").view(S8),
+                          z=torch.empty(N, 3008, dtype=BF, device="cuda")[:, :V], token=torch.empty(N, dtype=torch.int32, device="cuda"),
+                          kept=torch.empty(N, dtype=torch.int32, device="cuda")))
+
+    def step(s, hw, sw):
+        svip.quantize_mx(s["x"], q_out=s["hq"], scale_out=s["hs"])
+        svip.head_logits_mx(s["hq"], s["hs"], wq, wsc, logits_out=s["z"], workspace=hw)
+        svip.sample(s["z"], u=s["u"], temperature=s["T"], top_k=s["k"], top_p=s["p"], min_p=s["m"], token_out=s["token"], kept_out=s["kept"], workspace=sw)
+
+    graphs = []
+    for s in state:
+        s["x"].normal_()
+        s["u"].uniform_()
+        step(s, hw, sw)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            step(s, hw, sw)
+    for turn in range(4):
+        want = []
+        for N, s in zip(sizes, state):
+            s["x"].copy_(torch.randn(N, K, generator=gen(turn)))
+            s["u"].copy_(torch.rand(N, generator=gen(50 + turn)))
+            step(s, svip.new_head_workspace(svip.HEAD_LOGITS_MX, BF, N, V, K), svip.new_sample_workspace(BF, N, V))
+            want.append([s[x].clone() for x in ("z", "token", "kept")])
+            for x in ("z", "token", "kept"):
+                s[x].zero_()
+        for i in (0, 1) if turn % 2 else (1, 0):
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for s, w in zip(state, want):
+            assert all(torch.equal(s[x], y) for x, y in zip(("z", "token", "kept"), w))
+
+
 def test_sampled_tokens_go_on_to_verification(svip):
     """The sampler's probability is that of svip_warp_logits' row: what svip_draft_step and svip_verify call q(x) of the filtered row."""
     N, V = 16, 9000
