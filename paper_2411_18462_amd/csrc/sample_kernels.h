@@ -5,7 +5,7 @@
 // the narrowest cells are wide.  A weight costs about 17 instructions of 5.3 cycles (measured; in fp32 7 of 2.7).  Sums that decide are integers in
 // units of 2^-S of the largest weight (S = 62 - ceil(log2 V), at most 51), so that no order of additions changes a result and atomics may be used.
 //
-// Two launches, three where a call has top_p or min_p.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, in chunks
+// Two launches, three or four where a call has top_p or min_p.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, in chunks
 // of 64 neighbours.  k_sample_rows, a workgroup each row, does what the row's settings need beside that.  What a wave leaves for the row:
 //   T = 0         the tile's maximum
 //   no filter     and its mass; the draw finds the tile by the masses and goes through that tile alone again
@@ -77,7 +77,9 @@ struct RowData {
     int by_mass;                           // top_p's border is in the step (or min_p alone decides)
     float upper, lower;                    // logits from upper on are above the step, from lower on in it (and not below min_p)
     unsigned long long target;             // top_p: the mass that what stays has to reach
-    unsigned long long pad[5];
+    int step;                              // counted from that of the largest logit, downwards
+    float top;
+    unsigned long long pad[4];
 };
 __host__ __device__ inline size_t row_bytes(int tiles) { return sizeof(RowData) + (size_t)tiles * sizeof(TileData); }
 __device__ __forceinline__ RowData *row_data(char *data, int n, int tiles) { return reinterpret_cast<RowData *>(data + n * row_bytes(tiles)); }
@@ -900,8 +902,11 @@ __device__ __forceinline__ float least_that(P pass)
 __device__ unsigned llvm_writelane(unsigned value, unsigned lane, unsigned v) __asm("llvm.amdgcn.writelane.i32");
 __device__ __forceinline__ unsigned write_lane(unsigned v, unsigned lane, unsigned value) { return llvm_writelane(value, lane, v); }
 
-// Rows with top_p or min_p and no top_k: the step that holds the border, by every workgroup of the row for itself, and what its tiles have in it.
-template <typename DT>
+// Rows with top_p or min_p and no top_k: the step that holds the border, and what the tiles have in it.  BORDER_BOTH: every workgroup of the row finds the step for
+// itself, 6 us, while its tiles' logits come.  Where there are many, BORDER_FIND by one workgroup to a row and BORDER_MARK behind it, which reads no tile that lies
+// below (top-p 0.9, 512 rows of 128256 in fp32 166 -> 153 us, 250 in bf16 90 -> 81; 64 rows 43 and 45).
+enum { BORDER_BOTH, BORDER_FIND, BORDER_MARK };
+template <typename DT, int PART>
 __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
 {
     constexpr int N = VecOf<DT>::N, U = SAMPLE_CHUNK / N;
@@ -925,16 +930,21 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
         }
     };
     int tile = group * TILES_WAVES + wave;
-    if (tile < a.tiles) load(tile);        // (they arrive while the border is looked for)
+    if (PART == BORDER_BOTH && tile < a.tiles) load(tile);        // (they arrive while the border is looked for)
     RowData *const found = row_data(a.data, n, a.tiles);
     TileData *const tiles = tiles_of(found);
+    if (PART == BORDER_MARK && !found->found) return;
     float top = neg_inf();
-    for (int t = tid; t < a.tiles; t += TILES_WG) top = vmax(top, tile_top[t] = tiles[t].top);
-    top = wave_max(top);
-    if (lane == 0) wave_top[wave] = top;
-    __syncthreads();
+    if (PART == BORDER_MARK) {
+        top = found->top;
+    } else {
+        for (int t = tid; t < a.tiles; t += TILES_WG) top = vmax(top, tile_top[t] = tiles[t].top);
+        top = wave_max(top);
+        if (lane == 0) wave_top[wave] = top;
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < TILES_WAVES; ++i) top = vmax(top, wave_top[i]);
+        for (int i = 0; i < TILES_WAVES; ++i) top = vmax(top, wave_top[i]);
+    }
     const SampleWeights w(top, s.c, a.unit_bits);
     const float scale = s.step_scale, first = step_of(top, scale);
     const auto give_up = [&]() {
@@ -942,66 +952,81 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
     };
     if (!(top > neg_inf() && fabsf(first) < 8388608.f && w.near)) return give_up();      // (numbers of steps are whole numbers in fp32)
     // mass of tile t down to the end of the row's step r (counted from its first, downwards; of the last: all of it), in the row's units
-    const auto tile_down_to = [&](int t, int r) -> unsigned long long {
-        if (!(tile_top[t] > neg_inf())) return 0ull;
-        const float i = r < SAMPLE_STEPS - 1 ? (float)r - (first - step_of(tile_top[t], scale)) : (float)(SAMPLE_STEPS - 1);
+    const auto tile_down_to = [&](int t, float its_top, int r) -> unsigned long long {
+        if (!(its_top > neg_inf())) return 0ull;
+        const float i = r < SAMPLE_STEPS - 1 ? (float)r - (first - step_of(its_top, scale)) : (float)(SAMPLE_STEPS - 1);
         if (!(i >= 0.f)) return 0ull;
         const unsigned long long mass = tiles[t].down_to[(int)i];
-        return (unsigned long long)rint(in_row((double)mass, tile_top[t], w, a.unit_bits - TILE_UNIT_BITS));
+        return (unsigned long long)rint(in_row((double)mass, its_top, w, a.unit_bits - TILE_UNIT_BITS));
     };
     // of the row down to the end of eight steps side by side: threads 32 i .. 32 i + 31 have the sum of r(i)
     static_assert(TILES_WG == 8 * 32 && SAMPLE_STEPS == 8 * 8 * 8, "a step each, three times");
     const auto row_down_to = [&](int r) {
         unsigned long long mass = 0ull;
-        for (int t = tid & 31; t < a.tiles; t += 32) mass += tile_down_to(t, r);
+        for (int t = tid & 31; t < a.tiles; t += 32) mass += tile_down_to(t, tile_top[t], r);
         mass = row_reduce(mass, OpSum{});
         const auto lo = __builtin_amdgcn_permlane16_swap((unsigned)mass, (unsigned)mass, false, false);
         const auto hi = __builtin_amdgcn_permlane16_swap((unsigned)(mass >> 32), (unsigned)(mass >> 32), false, false);
         return ((unsigned long long)hi[0] << 32 | lo[0]) + ((unsigned long long)hi[1] << 32 | lo[1]);
     };
     int step = SAMPLE_STEPS;               // above it all stays, below nothing
-    unsigned long long target = 0ull;
-    if (s.top_p < 1.0) {
-        unsigned long long mass = row_down_to(64 * (tid / 32) + 63);
-        if (tid == TILES_WG - 1) all = mass;
-        __syncthreads();
-        target = max(1ull, (unsigned long long)ceil(s.top_p * (double)all));
-        step = 0;
+    float lower = neg_inf(), upper;
+    if (PART == BORDER_MARK) {
+        step = found->step;
+        lower = found->lower;
+        upper = found->upper;
+    } else {
+        unsigned long long target = 0ull;
+        if (s.top_p < 1.0) {
+            unsigned long long mass = row_down_to(64 * (tid / 32) + 63);
+            if (tid == TILES_WG - 1) all = mass;
+            __syncthreads();
+            target = max(1ull, (unsigned long long)ceil(s.top_p * (double)all));
+            step = 0;
 #pragma unroll 1
-        for (int width = 64;; width /= 8) {
-            if (tid == 0) first_group = 8;
-            __syncthreads();
-            if ((tid & 31) == 0 && mass >= target) atomicMin(&first_group, tid / 32);
-            __syncthreads();
-            step += first_group * width;
-            if (first_group == 8 || width == 1) break;
-            mass = row_down_to(step + width / 8 * (tid / 32 + 1) - 1);
-            __syncthreads();
+            for (int width = 64;; width /= 8) {
+                if (tid == 0) first_group = 8;
+                __syncthreads();
+                if ((tid & 31) == 0 && mass >= target) atomicMin(&first_group, tid / 32);
+                __syncthreads();
+                step += first_group * width;
+                if (first_group == 8 || width == 1) break;
+                mass = row_down_to(step + width / 8 * (tid / 32 + 1) - 1);
+                __syncthreads();
+            }
+        }
+        bool by_mass = s.top_p < 1.0;
+        if (s.log2_min_p > -INFINITY) {
+            lower = least_that([&](float z) { return w.log2_of(z) >= s.log2_min_p; });
+            const float its = first - step_of(lower, scale);
+            if (its < (float)step) {
+                step = (int)its;
+                by_mass = false;
+            }
+        }
+        if (step >= SAMPLE_STEPS - 1) return give_up();    // (the last step of a tile is all that lies below it too)
+        upper = least_that([&](float z) { return step_of(z, scale) >= first - (float)step + 1.f; });
+        lower = fmaxf(lower, least_that([&](float z) { return step_of(z, scale) >= first - (float)step; }));
+        if (group == 0 && tid == 0) {
+            found->found = 1;
+            found->by_mass = by_mass;
+            found->upper = upper;
+            found->lower = lower;
+            found->target = target;
+            found->step = step;
+            found->top = top;
         }
     }
-    float lower = neg_inf();
-    bool by_mass = s.top_p < 1.0;
-    if (s.log2_min_p > -INFINITY) {
-        lower = least_that([&](float z) { return w.log2_of(z) >= s.log2_min_p; });
-        const float its = first - step_of(lower, scale);
-        if (its < (float)step) {
-            step = (int)its;
-            by_mass = false;
-        }
-    }
-    if (step >= SAMPLE_STEPS - 1) return give_up();    // (the last step of a tile is all that lies below it too)
-    const float upper = least_that([&](float z) { return step_of(z, scale) >= first - (float)step + 1.f; });
-    lower = fmaxf(lower, least_that([&](float z) { return step_of(z, scale) >= first - (float)step; }));
-    if (group == 0 && tid == 0) {
-        found->found = 1;
-        found->by_mass = by_mass;
-        found->upper = upper;
-        found->lower = lower;
-        found->target = target;
-    }
+    if (PART == BORDER_FIND) return;
     for (; tile < a.tiles; tile += a.border_groups * TILES_WAVES) {
-        if (tile >= a.border_groups * TILES_WAVES) load(tile);
         TileData *const mine = tiles + tile;
+        const float its_top = mine->top;
+        if (!(its_top >= lower)) {         // nothing of it stays
+            mine->in_step[lane] = 0ull;
+            if (lane == 0) mine->above = 0ull, mine->kept = mine->undecided = 0;
+            continue;
+        }
+        if (PART == BORDER_MARK || tile >= a.border_groups * TILES_WAVES) load(tile);
         int kept = 0;
         unsigned lo = 0u, hi = 0u;         // the word of each lane
 #pragma unroll
@@ -1021,7 +1046,7 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
         const int undecided = wave_reduce((int)(__popc(lo) + __popc(hi)), OpSum{});
         kept = wave_reduce(kept, OpSum{});
         if (lane == 0) {
-            mine->above = tile_down_to(tile, step - 1);
+            mine->above = tile_down_to(tile, its_top, step - 1);
             mine->kept = kept;
             mine->undecided = undecided;
         }

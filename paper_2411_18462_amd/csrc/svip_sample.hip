@@ -7,6 +7,8 @@ namespace svip {
 
 constexpr int SAMPLE_MAX_ROWS = 1 << 20, SAMPLE_MAX_VOCAB = 1 << 22;
 
+constexpr long long MANY_GROUPS = 1024;                  // of tiles, for the border (see k_sample_border)
+
 static int sample_tiles(int V) { return ceil_div(V, SAMPLE_TILE); }
 static svip_status check_sample_sizes(int N, int V)
 {
@@ -39,8 +41,7 @@ svip_status svip_sample(const void *logits, int dtype, int N, int V, long long r
     a.unit_bits = 62 - log2_v < 51 ? 62 - log2_v : 51;
     a.tiles = sample_tiles(V);
     a.groups = ceil_div(a.tiles, TILES_WAVES);
-    // a workgroup looks for the border for itself, 6 us: where there are many, for eight tiles at a time and not for four
-    a.border_groups = (long long)N * a.groups <= 2048 ? a.groups : ceil_div(a.groups, 2);
+    a.border_groups = a.groups;
     a.data = static_cast<char *>(workspace) + 512;
     const bool ok = by_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
@@ -48,7 +49,16 @@ svip_status svip_sample(const void *logits, int dtype, int N, int V, long long r
         const hipStream_t st = static_cast<hipStream_t>(hip_stream);
         const long long grid = (long long)N * a.groups;
         if (!launch(k_sample_tiles<X>, grid, TILES_WG, st, a)) return false;
-        if ((top_p || min_p) && !launch(k_sample_border<X>, (long long)N * a.border_groups, TILES_WG, st, a)) return false;
+        if (top_p || min_p) {
+            if (grid <= MANY_GROUPS) {
+                if (!launch(k_sample_border<X, BORDER_BOTH>, grid, TILES_WG, st, a)) return false;
+            } else {
+                a.border_groups = 1;
+                if (!launch(k_sample_border<X, BORDER_FIND>, N, TILES_WG, st, a)) return false;
+                a.border_groups = a.groups;
+                if (!launch(k_sample_border<X, BORDER_MARK>, grid, TILES_WG, st, a)) return false;
+            }
+        }
         return launch(k_sample_rows<X>, N, SAMPLE_WG, st, a);
     });
     return ok ? SVIP_OK : SVIP_ERR_HIP;
