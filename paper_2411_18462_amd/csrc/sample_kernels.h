@@ -124,8 +124,11 @@ struct SampleWeights {
     int R;
     bool near;                 // |m c| < 2^30: of_tile may be used
     Exp2Series exp2;
-    __device__ __forceinline__ SampleWeights(float top, double c_, int unit_bits) : m(top), c(c_), unit(unit_of(unit_bits))
+    __device__ __forceinline__ SampleWeights(float top, double c_, int unit_bits) : c(c_) { set(top, unit_bits); }
+    __device__ __forceinline__ void set(float top, int unit_bits)
     {
+        m = top;
+        unit = unit_of(unit_bits);
         const double mc = m * c;
         near = fabs(mc) < 1073741824.0;
         R = near ? (int)rint(mc) : 0;
@@ -195,11 +198,10 @@ struct SampleLds {
     float tile_top[SAMPLE_MAX_TILES];
     unsigned long long wave_tot[SAMPLE_WAVES], wave_sum[3][SAMPLE_WAVES];
     float best[SAMPLE_WAVES];
-    unsigned long long found_before, found_upto, total;          // (total: of draw_by_tiles)
+    unsigned long long found_before, found_upto, total;          // (total: of draw_by_tiles, whose tile has the mass found_upto)
     int found;
     unsigned count, n_list;
     unsigned low;
-    int last;
 };
 
 constexpr int DPP_HALF_MIRROR = 0x141;  // row_half_mirror: lane i of 8 has lane 7 - i's
@@ -323,55 +325,45 @@ struct Keep {
     __device__ __forceinline__ bool operator()(float z) const { return value_key(z) >= low && w.log2_of(z) >= log2_min_p; }
 };
 
-// The draw from vectors v0 .. v1 - 1 of the row, `left` units behind the mass in front of them: the first token at which the sum exceeds that, or, where
-// roundings leave none, the last that has weight.  total: of the row, in units.
+// The draw from vectors v0 .. v1 - 1 of the row, whose kept logits have `mass` and which it is to go into at `left`, less than that: the first token at which
+// their running sum, over all of it, exceeds left / mass, compared as products of whole numbers.  `measure` says in which units they are summed here: the row's,
+// for a mass that is a sum of just these (then it is compared with `left` itself), or, for a tile's mass, which was rounded as a whole, units of the tile's own, so
+// that logits of less than a unit of the row's are drawn by their weights too.  A token without a unit is never drawn.  total: of the row, in its units.
 template <typename DT>
-__device__ __forceinline__ void draw_in_range(const SampleArgs &a, int n, const DT *row, int v0, int v1, const Keep &keep, unsigned long long left,
-                                              unsigned long long total, int kept, SampleLds &L)
+__device__ __forceinline__ void draw_in_range(const SampleArgs &a, int n, const DT *row, int v0, int v1, const Keep &keep, const SampleWeights &measure,
+                                              unsigned long long left, unsigned long long mass, unsigned long long total, int kept, SampleLds &L)
 {
     constexpr int N = VecOf<DT>::N;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (v1 - v0 + SAMPLE_WG - 1) / SAMPLE_WG, first = v0 + tid * per, end = min(v1, first + per);
-    unsigned long long mass = 0ull;
-    int last = -1;
+    unsigned long long mine = 0ull;
     for (int v = first; v < end; ++v) {
         float z[N];
         unpack<DT>(warp_load<DT>(row, v, a.V), z);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if (!keep(sample_logit(z[e]))) continue;
-            mass += keep.w.units(z[e]);
-            last = v * N + e;
-        }
+        for (int e = 0; e < N; ++e)
+            if (keep(sample_logit(z[e]))) mine += measure.units(z[e]);
     }
-    const unsigned long long incl = wave_inclusive_sum_u64(mass);
+    const unsigned long long incl = wave_inclusive_sum_u64(mine);
     if (lane == 63) L.wave_tot[wave] = incl;
-    if (tid == 0) L.last = -1;
     __syncthreads();
-    unsigned long long run = incl - mass, all = 0ull;
+    unsigned long long run = incl - mine, all = 0ull;
     for (int w = 0; w < SAMPLE_WAVES; ++w) {
         if (w < wave) run += L.wave_tot[w];
         all += L.wave_tot[w];
     }
-    const auto answer = [&](int i) {
-        const float z = sample_logit(widen(row[i]));
-        sample_answer(a, n, i, (float)(keep.w(z) / ldexp((double)total, -a.unit_bits)), kept);
-    };
-    if (all <= left) {
-        atomicMax(&L.last, last);
-        __syncthreads();
-        if (tid == 0) answer(L.last);
-        return;
-    }
-    if (run > left || run + mass <= left) return;
+    typedef unsigned __int128 wide_sum;
+    const wide_sum at = (wide_sum)left * all;
+    const auto reaches = [&](unsigned long long sum) { return (wide_sum)sum * mass > at; };
+    if (reaches(run) || !reaches(run + mine)) return;
     for (int v = first; v < end; ++v) {
         float z[N];
         unpack<DT>(warp_load<DT>(row, v, a.V), z);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             if (!keep(sample_logit(z[e]))) continue;
-            const unsigned long long x = keep.w.units(z[e]);
-            if (run <= left && run + x > left) answer(v * N + e);
+            const unsigned long long x = measure.units(z[e]);
+            if (!reaches(run) && reaches(run + x)) sample_answer(a, n, v * N + e, (float)(keep.w(z[e]) / ldexp((double)total, -a.unit_bits)), kept);
             run += x;
         }
     }
@@ -421,7 +413,7 @@ __device__ __forceinline__ void row_by_sweeps(const SampleArgs &a, int n, const 
     unsigned long long before, total;
     const auto at = [&](unsigned long long all) { return (unsigned long long)(s.u * (double)all); };
     const int bin = find_bin<true>(L, [&](unsigned long long all) { return at(all) + 1ull; }, &before, &total);
-    draw_in_range<DT>(a, n, row, bin * per * 64, min(nvec, (bin + 1) * per * 64), keep, at(total) - before, total, (int)kept, L);
+    draw_in_range<DT>(a, n, row, bin * per * 64, min(nvec, (bin + 1) * per * 64), keep, w, at(total) - before, L.found_upto - before, total, (int)kept, L);
 }
 
 template <int CTRL, int ROW_MASK>
@@ -710,6 +702,7 @@ __device__ __forceinline__ void draw_by_tiles(const SampleArgs &a, int n, const 
                 if (tid == lane) {
                     L.found = t0 + lane;
                     L.found_before = at - (ahead + incl - mass);
+                    L.found_upto = mass;
                     L.total = total;
                 }
                 break;
@@ -719,8 +712,9 @@ __device__ __forceinline__ void draw_by_tiles(const SampleArgs &a, int n, const 
     }
     __syncthreads();
     const int t = L.found, v0 = t * (SAMPLE_TILE / N);
-    const unsigned long long left = L.found_before, total = L.total;
-    draw_in_range<DT>(a, n, row, v0, min((a.V + N - 1) / N, v0 + SAMPLE_TILE / N), keep, left, total, kept, L);
+    SampleWeights measure = keep.w;        // (one series for both: its coefficients are 20 scalar registers)
+    measure.set(L.tile_top[t], max(TILE_UNIT_BITS, a.unit_bits));      // (51 in rows of up to half a tile)
+    draw_in_range<DT>(a, n, row, v0, min((a.V + N - 1) / N, v0 + SAMPLE_TILE / N), keep, measure, L.found_before, L.found_upto, L.total, kept, L);
 }
 
 // top_p and min_p by what k_sample_border found.
