@@ -499,7 +499,8 @@ svip_status svip_head_loss_grad(
  *   scale_out[r, c / 32] = e + 127                          (e8m0: a power of two)
  * so that the value kept is code * 2^e.  A block that holds a value that is not finite has the scale 255 (the NaN of e8m0) and codes of zero:
  * all its values are NaN.  Bytes of q_out past column K / 2 and of scale_out past column K / 32 are not written.  No workspace.
- * rows <= 2^22, cols <= 2^17, fewer than 2^27 runs of 128 columns in all; row strides of codes and scales are at most 2^24 bytes.
+ * rows <= 2^22, cols <= 2^17, fewer than 2^27 runs of 128 columns in all (fp32: 2^27 - 8 at most); row strides of codes and scales are at most
+ * 2^24 bytes.
  */
 svip_status svip_quantize_mx(
     const void *x, int dtype,        /* device, row r at element offset r * row_stride (any from cols on; x on its type's alignment) */

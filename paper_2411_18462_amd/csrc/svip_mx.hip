@@ -69,6 +69,8 @@ svip_status svip_quantize_mx(const void *x, int dtype, int rows, int cols, long 
     if (rows <= 0 || rows > HEAD_MAX_VOCAB || cols <= 0 || cols > HEAD_MAX_WIDTH || row_stride < cols) return SVIP_ERR_SHAPE;
     const int runs = ceil_div(cols, MX_RUN);
     if ((long long)rows * runs >= 1LL << 27) return SVIP_ERR_SHAPE;
+    // (fp32, 32 lanes a run: whole workgroups of 2^27 - 7 runs and more would be 2^32 threads)
+    if (dtype == SVIP_F32 && (long long)rows * runs > (1LL << 27) - MX_WG * Stored<SVIP_F32>::VEC / MX_RUN) return SVIP_ERR_SHAPE;
     if (svip_status s = check_mx(q_out, q_stride, scale_out, scale_stride, runs * MX_RUN)) return s;
     if (reinterpret_cast<uintptr_t>(x) % size_of(dtype) != 0) return SVIP_ERR_ALIGN;
     const MxQuantizeArgs a = {x, row_stride, rows, cols, runs, static_cast<unsigned char *>(q_out), q_stride, static_cast<unsigned char *>(scale_out), scale_stride};
