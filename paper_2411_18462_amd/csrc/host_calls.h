@@ -49,4 +49,6 @@ static inline svip_status check_workspace(const void *ws, size_t bytes, size_t n
     return !ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || bytes < need ? SVIP_ERR_WORKSPACE : SVIP_OK;
 }
 
+size_t mx_logits_workspace(int N, int V, int K);       // of svip_head_logits_mx
+
 }  // namespace svip

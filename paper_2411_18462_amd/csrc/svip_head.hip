@@ -7,7 +7,6 @@
 
 #include "head_kernels.h"
 #include "host_calls.h"
-#include "svip_internal.h"
 
 namespace svip {
 

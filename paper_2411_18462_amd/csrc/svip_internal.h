@@ -105,6 +105,5 @@ svip_status greedy_stream_call(const DraftCall &c, const void *target, int group
                                Mail active, Mail running, Mail rounds);
 constexpr int STREAM_MAX_GROUP = 128;
 svip_status verify_call(const VerifyCall &c);
-size_t mx_logits_workspace(int N, int V, int K);      // of svip_head_logits_mx
 
 }  // namespace svip

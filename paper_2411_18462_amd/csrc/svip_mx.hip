@@ -2,7 +2,6 @@
 #include "mx_kernels.h"
 
 #include "host_calls.h"
-#include "svip_internal.h"
 
 namespace svip {
 
