@@ -46,7 +46,6 @@ struct SampleArgs {
     unsigned *flags;
     int unit_bits;             // S
     int tiles, groups;         // of a row; groups: workgroups of k_sample_tiles
-    int border_groups;         // of k_sample_border
     char *data;                // [N] RowData, [tiles] TileData
 };
 
@@ -909,7 +908,7 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
     __shared__ float wave_top[TILES_WAVES];
     __shared__ unsigned long long all;
     __shared__ int first_group;
-    const int n = blockIdx.x / (unsigned)a.border_groups, group = blockIdx.x - n * a.border_groups;
+    const int groups = PART == BORDER_FIND ? 1 : a.groups, n = blockIdx.x / (unsigned)groups, group = blockIdx.x - n * groups;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = a.V;
     const Settings s = settings_of(a, n);
     if (s.mode != SAMPLE_STEPPED) return;
@@ -924,7 +923,7 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
             load_raw_tail<DT, U, 64>(row, v0, V, raw);
         }
     };
-    int tile = group * TILES_WAVES + wave;
+    const int tile = group * TILES_WAVES + wave;
     if (PART == BORDER_BOTH && tile < a.tiles) load(tile);        // (they arrive while the border is looked for)
     RowData *const found = row_data(a.data, n, a.tiles);
     TileData *const tiles = tiles_of(found);
@@ -1012,39 +1011,37 @@ __global__ __launch_bounds__(TILES_WG) void k_sample_border(SampleArgs a)
             found->top = top;
         }
     }
-    if (PART == BORDER_FIND) return;
-    for (; tile < a.tiles; tile += a.border_groups * TILES_WAVES) {
-        TileData *const mine = tiles + tile;
-        const float its_top = mine->top;
-        if (!(its_top >= lower)) {         // nothing of it stays
-            mine->in_step[lane] = 0ull;
-            if (lane == 0) mine->above = 0ull, mine->kept = mine->undecided = 0;
-            continue;
-        }
-        if (PART == BORDER_MARK || tile >= a.border_groups * TILES_WAVES) load(tile);
-        int kept = 0;
-        unsigned lo = 0u, hi = 0u;         // the word of each lane
+    if (PART == BORDER_FIND || tile >= a.tiles) return;
+    TileData *const mine = tiles + tile;
+    const float its_top = mine->top;
+    if (!(its_top >= lower)) {             // nothing of it stays
+        mine->in_step[lane] = 0ull;
+        if (lane == 0) mine->above = 0ull, mine->kept = mine->undecided = 0;
+        return;
+    }
+    if (PART == BORDER_MARK) load(tile);
+    int kept = 0;
+    unsigned lo = 0u, hi = 0u;             // the word of each lane
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float z[N];
-            unpack<DT>(raw[u], z);
+    for (int u = 0; u < U; ++u) {
+        float z[N];
+        unpack<DT>(raw[u], z);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                kept += z[e] >= upper;
-                const unsigned long long in = __ballot(z[e] >= lower && !(z[e] >= upper));
-                lo = write_lane(lo, u * N + e, (unsigned)in);
-                hi = write_lane(hi, u * N + e, (unsigned)(in >> 32));
-                __builtin_amdgcn_sched_barrier(0);     // (or 128 scalar registers are held for the words)
-            }
+        for (int e = 0; e < N; ++e) {
+            kept += z[e] >= upper;
+            const unsigned long long in = __ballot(z[e] >= lower && !(z[e] >= upper));
+            lo = write_lane(lo, u * N + e, (unsigned)in);
+            hi = write_lane(hi, u * N + e, (unsigned)(in >> 32));
+            __builtin_amdgcn_sched_barrier(0);         // (or 128 scalar registers are held for the words)
         }
-        mine->in_step[lane] = (unsigned long long)hi << 32 | lo;
-        const int undecided = wave_reduce((int)(__popc(lo) + __popc(hi)), OpSum{});
-        kept = wave_reduce(kept, OpSum{});
-        if (lane == 0) {
-            mine->above = tile_down_to(tile, its_top, step - 1);
-            mine->kept = kept;
-            mine->undecided = undecided;
-        }
+    }
+    mine->in_step[lane] = (unsigned long long)hi << 32 | lo;
+    const int undecided = wave_reduce((int)(__popc(lo) + __popc(hi)), OpSum{});
+    kept = wave_reduce(kept, OpSum{});
+    if (lane == 0) {
+        mine->above = tile_down_to(tile, its_top, step - 1);
+        mine->kept = kept;
+        mine->undecided = undecided;
     }
 }
 

@@ -41,7 +41,6 @@ svip_status svip_sample(const void *logits, int dtype, int N, int V, long long r
     a.unit_bits = 62 - log2_v < 51 ? 62 - log2_v : 51;
     a.tiles = sample_tiles(V);
     a.groups = ceil_div(a.tiles, TILES_WAVES);
-    a.border_groups = a.groups;
     a.data = static_cast<char *>(workspace) + 512;
     const bool ok = by_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
@@ -52,11 +51,8 @@ svip_status svip_sample(const void *logits, int dtype, int N, int V, long long r
         if (top_p || min_p) {
             if (grid <= MANY_GROUPS) {
                 if (!launch(k_sample_border<X, BORDER_BOTH>, grid, TILES_WG, st, a)) return false;
-            } else {
-                a.border_groups = 1;
-                if (!launch(k_sample_border<X, BORDER_FIND>, N, TILES_WG, st, a)) return false;
-                a.border_groups = a.groups;
-                if (!launch(k_sample_border<X, BORDER_MARK>, grid, TILES_WG, st, a)) return false;
+            } else if (!launch(k_sample_border<X, BORDER_FIND>, N, TILES_WG, st, a) || !launch(k_sample_border<X, BORDER_MARK>, grid, TILES_WG, st, a)) {
+                return false;
             }
         }
         return launch(k_sample_rows<X>, N, SAMPLE_WG, st, a);
