@@ -554,6 +554,10 @@ svip_status svip_head_logits_mx(
  * that (2^-45 of the largest weight per token at V = 128256) to a border may differ from an exact evaluation; top-k is exact.  Same inputs
  * give bit-identical outputs.
  *
+ * A round that goes on to svip_verify: that call has one temperature and no filter, so it takes tokens of rows that share their temperature, top_k and top_p
+ * and have no min_p, over the drafter's and the target's rows as svip_warp_logits leaves them with those settings, with draft_lse NULL (T = 0: svip_verify_greedy).  Sequences of
+ * other settings go in a call of their own; for min_p there is none.  The stop test of a draft is svip_draft_step's: this call gives no entropy.
+ *
  * logits: as everywhere, row n at element offset n * row_stride.  temperature, top_k, top_p, min_p: device [N], each or NULL (1, off, off, off).
  * 1 <= N <= 2^20, 1 <= V <= 2^22, N * ceil(V / 16384) < 2^24.  workspace: svip_sample_workspace_bytes of the call's sizes or more, 256-byte aligned, that
  * svip_workspace_reset has cleared once (for its flag word).  As with the head's calls it is not the one of the calls above, it holds nothing between
