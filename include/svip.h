@@ -550,9 +550,11 @@ svip_status svip_head_logits_mx(
  * -inf and NaN are tokens without weight; +inf, where there is one, leaves weight to nothing else.  A row without any weight gets token -1, prob 0,
  * kept 0; so does one whose settings are out of range (T negative or not finite, top_k negative, top_p <= 0 or NaN, min_p outside [0, 1], u outside
  * [0, 1)), which also sets SVIP_FLAG_BAD_SETTING in the workspace.
- * Weights are 64-bit exponentials summed exactly as integers in units of 2^-S, S = min(51, 62 - ceil(log2 V)): a draw or a nucleus closer than
- * that (2^-45 of the largest weight per token at V = 128256) to a border may differ from an exact evaluation; top-k is exact.  Same inputs
- * give bit-identical outputs.
+ * Weights are 64-bit exponentials; a unit is 2^-S, S = min(51, 62 - ceil(log2 V)), of a power of two within a factor of 2^1/2 of the row's largest
+ * weight.  Sums that decide are whole numbers of units: of weights that are each rounded to units where candidates of a top-k or the whole row are gone
+ * through one by one, and otherwise of masses of tiles of 4096 logits, which are summed finer and rounded to units as a whole; a draw within a tile goes by units of
+ * 2^-50 or less of that tile's own.  A draw or a nucleus closer than a unit for each token (2^-45 of the largest weight at V = 128256) to a border may
+ * differ from an exact evaluation; top-k is exact.  Same inputs give bit-identical outputs.
  *
  * A round that goes on to svip_verify: that call has one temperature and no filter, so it takes tokens of rows that share their temperature, top_k and top_p
  * and have no min_p, over the drafter's and the target's rows as svip_warp_logits leaves them with those settings, with draft_lse NULL (T = 0: svip_verify_greedy).  Sequences of
@@ -560,8 +562,10 @@ svip_status svip_head_logits_mx(
  *
  * logits: as everywhere, row n at element offset n * row_stride.  temperature, top_k, top_p, min_p: device [N], each or NULL (1, off, off, off).
  * 1 <= N <= 2^20, 1 <= V <= 2^22, N * ceil(V / 16384) < 2^24.  workspace: svip_sample_workspace_bytes of the call's sizes or more, 256-byte aligned, that
- * svip_workspace_reset has cleared once (for its flag word).  As with the head's calls it is not the one of the calls above, it holds nothing between
- * calls, one for calls of several sizes has the most bytes that one of them needs, and calls that run concurrently must use different ones.
+ * svip_workspace_reset has cleared once (for its flag word).  That is 512 + N * (64 + 4896 * ceil(V / 4096)) bytes, the last 256 begun filled up, whatever the
+ * settings: 0.6 of the bytes of long rows in 16 bits, and far more than short rows have (5 KB each).  As with the head's calls it is not the one of the calls
+ * above, it holds nothing between calls, one for calls of several sizes has the most bytes that one of them needs, and calls that run concurrently must use
+ * different ones.
  */
 size_t svip_sample_workspace_bytes(int dtype, int N, int V);          /* pure host function; 0 on bad arguments */
 svip_status svip_sample(

@@ -3,7 +3,10 @@
 // Weights are w = exp2((z - m) c) with c = log2(e) / T and m the row's largest logit, in 64 bits: which token a uniform falls on, and which
 // value the nucleus ends at, are borders between sums of up to V weights, and a rounding of 2^-24 in each weight moves such a border by more than
 // the narrowest cells are wide.  A weight costs about 17 instructions of 5.3 cycles (measured; in fp32 7 of 2.7).  Sums that decide are integers in
-// units of 2^-S of the largest weight (S = 62 - ceil(log2 V), at most 51), so that no order of additions changes a result and atomics may be used.
+// units of 2^-S (S = 62 - ceil(log2 V), at most 51) of 2^R, a power of two within 2^1/2 of the largest weight, so that no order of additions changes a result and
+// atomics may be used.  Where single logits are summed, each is rounded to units.  A tile's mass is rounded to them as a whole: it comes from a sum in fp64 in a
+// fixed order (rows without filter) or of integers in units of 2^-50 of the tile's own 2^R, 53 bits of which count (steps); and the draw inside a tile goes by
+// its share of that mass, in the tile's own units.
 //
 // Two launches, three or four where a call has top_p or min_p.  k_sample_tiles reads the rows once: a wave has a tile of 4096 logits in registers, in chunks
 // of 64 neighbours.  k_sample_rows, a workgroup each row, does what the row's settings need beside that.  What a wave leaves for the row:
@@ -64,8 +67,8 @@ constexpr int SAMPLE_MAX_TILES = (1 << 22) / SAMPLE_TILE;
 struct TileData {
     float top;                             // the largest logit
     int count;                             // logits above -inf
-    double mass;                           // relative to 2^R of its own
-    unsigned long long down_to[SAMPLE_STEPS];      // mass from the top down to the end of each step
+    double mass;                           // relative to 2^R of its own (rows without filter)
+    unsigned long long down_to[SAMPLE_STEPS];      // mass from the top down to the end of each step, in units of 2^-50 of that
     float chunk_top[64];
     unsigned long long above;              // k_sample_border: mass above the row's border step, in the row's units
     int kept, undecided;                   // logits above it and in it
@@ -106,7 +109,7 @@ struct Exp2Series {
         return __hiloint2double(__double2hiint(r) + ((__double2loint(rounded) - from) << 20), __double2loint(r));
     }
 };
-// 2^(52 - bits): added to a weight of at most 1 it leaves the weight in units of 2^-bits, rounded, in the low bits of the sum
+// 2^(52 - bits), bits <= 51: added to a weight below 2 it leaves the weight in units of 2^-bits, rounded, in the low bits of the sum
 __device__ __forceinline__ double unit_of(int bits) { return __longlong_as_double((long long)(1023 + 52 - bits) << 52); }
 __device__ __forceinline__ unsigned long long units_of(double w, double unit)
 {

@@ -17,3 +17,13 @@ def test_runs_of_quantize_mx(rows, runs, fp32, others):
     p = (ctypes.addressof(buf) + 255) & ~255                     # a fake, aligned "device" pointer, never dereferenced
     call = lambda dtype: lib.svip_quantize_mx(p, dtype, rows, 128 * runs, 128 * runs, p + 8, 64 * runs, p, 4 * runs, None)  # noqa: E731
     assert call(0) == fp32 and call(1) == call(2) == others
+
+
+def test_workspace_of_the_sampler():
+    """What svip.h says of its size."""
+    import torch
+
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        for N, V in ((1, 1), (1, 4096), (1, 4097), (7, 9000), (1088, 151936), (1 << 20, 8), (3, 1 << 22)):
+            need = N * (64 + 4896 * -(-V // 4096))
+            assert svip.sample_workspace_bytes(dtype, N, V) == 512 + -(-need // 256) * 256
