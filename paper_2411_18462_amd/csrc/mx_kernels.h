@@ -148,12 +148,12 @@ __global__ __launch_bounds__(MX_WG) void k_mx_rows(MxRowsArgs a)
 // Few rows wait for the weight's bytes (64 x 128256 x 2048, 8-bit hidden states: 40 us, 3.9 TB/s; 1 row: 28 us, 5.0).  Large tiles wait for what feeds the products.
 // A copy takes a compute unit about 7 cycles for each cache line that it touches, whether 128 bytes of it or 4:
 // - The scales of a row and a step are 8 bytes, and copied step by step they would be as many lines as the codes.  They come in groups of GROUP steps.
-// - 4 bits: steps of whole lines, 256 x 256 tiles.  1088 x 128256 x 4096: 385-413 us, 2.8-3.0 PFLOP/s (the library's largest 4-bit products reach 2.3 here),
-//   products under way in 41 % of the cycles at 1.9 GHz.  Leaving out one thing at a time of 434 us then: the copies 371, the reads of the scales 381 (bank
+// - 4 bits: steps of whole lines, 256 x 256 tiles.  1088 x 128256 x 4096: 385-413 us, 2.8-3.0 PFLOP/s (the library's largest 4-bit products reach 2.3 here,
+//   its 8-bit ones 2.9; in fp32 450 us, 558 MB of logits), products under way in 40 % of the cycles at 1.9 GHz.  Leaving out one thing at a time of 434 us then: the copies 371, the reads of the scales 381 (bank
 //   conflicts, now gone), the stores 388.  16 waves of 64 x 64 take 440, 8 of 128 x 64 453, 8 that replace each fragment as soon as its products are under way
 //   512 (they spill), 4 of 128 x 128 488, two workgroups with 128 x 128 479, two with 256 x 128 in steps of 128 values 513.
 // - 8 bits: the products take twice as long, and what counts is a second workgroup that multiplies while one waits: 256 x 128 tiles twice a unit leave room
-//   for steps of 128 values only.  The same sizes: 540 us (without copies 353), in steps of 256 values with one workgroup 606-637, 256 x 256 tiles 583-605.
+//   for steps of 128 values only.  The same sizes: 529-540 us (without copies 353), in steps of 256 values with one workgroup 606-637, 256 x 256 tiles 583-605.
 
 template <int BITS> constexpr int MX_STEP = BITS == 4 ? 2 * MX_RUN : MX_RUN;       // values of K to a step; BITS: of the hidden states
 

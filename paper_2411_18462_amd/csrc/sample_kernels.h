@@ -23,10 +23,12 @@
 // needs (row_by_sweeps: 44 rows of 32000 with mixed settings took 79 us when those with a top_k of 1000 came here, and 38 by lists).
 //
 // What bounds them (us, launches of k_sample_tiles + _border + _rows; bf16):
-//   1088 x 128256   T = 0: 50 + 10 + 15, the memory (279 MB at 5.6 TB/s); no filter: 105 + 10 + 22, fp64 instructions (83 us at the rate they reach alone, 2.3 GHz);
-//                   top-k 50, top-p 0.9: 57 + 14 + 32; top-p 0.9: 140 + 14 + 59 + 44, beside that the LDS additions of the steps and the second reading
-//                   (a border launch that has nothing to do takes 5, and is left out where no top_p and min_p are given)
-//   64 x 128256     top-k 50, top-p 0.9: 5 + 2 + 12; top-p 0.9: 15 + 12 + 17; mixed settings: 13 + 11 + 22.  A row is one workgroup's in the last
+//   1088 x 128256   T = 0: 50 + 5 + 5 + 15, the memory (279 MB at 5.6 TB/s); no filter: 110 + 5 + 5 + 24, fp64 instructions (83 us at the rate they reach alone,
+//                   2.3 GHz); top-k 50, top-p 0.9: 57 + 5 + 9 + 30; top-p 0.9: 138 + 14 + 67 + 50.  (A border launch that has nothing to do takes 5, and is left
+//                   out where no top_p and min_p are given.)  Of the 149 that the tiles of top-p 0.9 take launched alone, 142 are left without the stores of
+//                   their steps' masses (144 MB), 92 without the weights, 94 without the weights and the LDS additions, 50 for the reading: the weights first,
+//                   then the steps' numbers and sums
+//   64 x 128256     top-k 50, top-p 0.9: 5 + 2 + 12; top-p 0.9: 15 + 12 + 18; mixed settings: 13 + 10 + 21.  A row is one workgroup's in the last
 //                   launch: latencies, one after the other
 //   1 x 32000 fp32  top-k 50, top-p 0.9: 4 + 1.5 + 10
 #pragma once
